@@ -66,7 +66,7 @@ enum {
     SPEC_STATUS_INDEX = 16       /* a context index could not take a window: that sequence is drafted by scanning until the index is rebuilt */
 };
 
-enum { SPEC_F32 = 0, SPEC_BF16 = 1 };
+enum { SPEC_F32 = 0, SPEC_BF16 = 1, SPEC_E4M3 = 2 };
 enum { SPEC_FLAG_DEDUP = 1, SPEC_FLAG_MODEL_FILL = 2, SPEC_FLAG_KEY_NEXT_TOKEN = 4, SPEC_FLAG_PARTIAL_TAIL = 8 };
 /* OR into the draft flags to reserve n (0..255) of the B draft rows for the model strategy */
 #define SPEC_FLAG_RESERVE(n) (((n) & 0xFF) << 8)
@@ -282,6 +282,96 @@ int spec_quantize_head_fp8(spec_ctx* ctx, uint8_t* d_wq, float* d_wscale, void* 
 int spec_set_head_fp8(spec_ctx* ctx, const uint8_t* d_wq, const float* d_wscale);
 int verify_lmhead_argmax_fp8(spec_ctx* ctx, const void* d_hidden, int M, uint8_t* d_hq, float* d_hscale,
                              int32_t* d_argmax, float* d_max, void* stream);
+
+/*
+ * Attention of a verification call (Section 3: one model call on the (B, w+1) block behind the context).
+ *
+ * The block holds N nodes per sequence - drafted tokens, arranged as a forest: the framework's draft rows are B chains
+ * of w+1 nodes (node b*(w+1) + j, column 0 = the last context token); any other tree will do.  Its keys and values
+ * stay outside the cache; what acceptance keeps is written with spec_cache_write.
+ *
+ * The cache is paged.  Position p of sequence s lies in page d_table[s, p / page], slot p % page; a page holds all
+ * heads' keys (or values): [n_pages, heads, page, head_dim].  SPEC_BF16 stores bfloat16.  SPEC_E4M3 stores one byte per
+ * element (1-4-3 bits, bias 7, no infinities) and one scale per vector of head_dim elements, a power of two kept as
+ * its exponent + 127: the smallest with max |x| <= 448 * scale, exponent in [-120, 7]; code = E4M3 nearest to
+ * x / scale, ties to the even code.  Larger magnitudes and infinities are held as 448 * 2^7; a vector with a NaN has
+ * scale byte 255 and reads as NaN.
+ *
+ * Limits: head_dim 64 or 128; page 16, 32, 64 or 128; n_pages * heads * page < 2^31; all pointers to elements 16-byte
+ * aligned.  Strides count elements, are multiples of 8, and head vectors are contiguous; node i of sequence s is token
+ * s*N + i.  A length or position outside a sequence's pages, or a page outside [0, n_pages), sets
+ * SPEC_STATUS_CAPACITY: such a position is skipped, such a length leaves the sequence's outputs as for an empty row.
+ */
+typedef struct spec_kv_cache {
+    void* d_k;              /* [n_pages, heads, page, head_dim] */
+    void* d_v;
+    uint8_t* d_k_exp;       /* SPEC_E4M3: [n_pages, heads, page] scale exponent + 127; else NULL */
+    uint8_t* d_v_exp;
+    const int32_t* d_table; /* [S, max_pages] page numbers */
+    int dtype;              /* SPEC_BF16 or SPEC_E4M3 */
+    int n_pages, max_pages, page, heads, head_dim;
+} spec_kv_cache;
+
+/*
+ * Rotary positions: pair i of a head is turned by position * d_freq[i] and multiplied by `factor` (1, or the gain of a
+ * rule that stretches positions; the rule itself is in d_freq).  The pairs are elements (i, i + rot/2), or (2i, 2i+1)
+ * if interleaved, of the first `rot` elements; the others pass unchanged.  rot % 16 == 0.
+ */
+typedef struct spec_rope {
+    const float* d_freq;    /* [rot / 2] radians per position */
+    int rot, interleaved;
+    float factor;
+} spec_rope;
+
+/*
+ * Rotates queries and keys of T tokens at positions d_pos[T] in one launch (fp32 arithmetic, the angle reduced in
+ * 64 bits, rounded once to bfloat16).  Outputs are contiguous [T, heads, head_dim]; an output may be its own input if
+ * that is contiguous.  Hk = 0: queries only.  head_dim % 16 == 0, at most 512.
+ */
+int spec_rope_rows(spec_ctx* ctx, const spec_rope* rope, const void* d_q, int Hq, long long q_tok, long long q_head, void* d_q_out,
+                   const void* d_k, int Hk, long long k_tok, long long k_head, void* d_k_out, int head_dim,
+                   const int32_t* d_pos, int T, void* stream);
+
+/*
+ * Writes keys and values into the cache: for i < d_count[s] (NULL: n), node d_nodes[s, i] (NULL: i) of sequence s goes
+ * to position d_start[s] + i.  A node outside [0, N) is skipped (the committed path of a step is padded with -1).
+ * rope (or NULL): keys are rotated at the position they are written to, and rounded to bfloat16, first.
+ * Lengths are the caller's: all layers of a model share them.
+ */
+int spec_cache_write(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_k, long long k_tok, long long k_head, const void* d_v,
+                     long long v_tok, long long v_head, int S, int N, int n, const int32_t* d_nodes, const int32_t* d_start,
+                     const int32_t* d_count, const spec_rope* rope, void* stream);
+
+/* Positions d_start[s] + i, i < d_count[s] (NULL: n), as contiguous bfloat16 [S, n, heads, head_dim] (exact); 0 beyond. */
+int spec_cache_read(spec_ctx* ctx, const spec_kv_cache* cache, int S, int n, const int32_t* d_start, const int32_t* d_count,
+                    void* d_k_out, void* d_v_out, void* stream);
+
+/*
+ * Ancestors of each node of a draft forest, itself included, as bits: word j/32 bit j%32 of d_mask[s, i, :] says that
+ * node i attends to node j; d_mask is [S, N, ceil(N/32)].  d_parent[s, i] < i, or -1 for a root.  A node beyond
+ * d_nnodes[s] (NULL: N), or whose path to a root breaks that order, gets an empty mask and depth -1.  N <= 4096.
+ *   d_depth [S, N] out or NULL: distance from the root (position of the node = context length + depth).
+ */
+int spec_tree_mask(spec_ctx* ctx, const int32_t* d_parent, int S, int N, const int32_t* d_nnodes, int32_t* d_mask, int32_t* d_depth,
+                   void* stream);
+
+/*
+ * Tree attention.  Row (s, i, hq) attends, with key head hq / (Hq / heads), to cache positions [0, d_len[s]) and to the
+ * block's nodes j with mask bit (i, j), j < d_nnodes[s] (NULL: N):
+ *   out = sum_j softmax_j(scale <q, k_j>) v_j,   lse = log sum_j exp(scale <q, k_j>).
+ * Rows that attend to nothing, and nodes from d_nnodes[s] on, give out = 0 and lse = -inf; what a row does not attend to
+ * does not reach it, NaN and infinities included.  N = 1 is plain decoding of one token.
+ *   d_q [S*N, Hq, head_dim], d_k / d_v [S*N, heads, head_dim] strided, bfloat16 (keys already rotated).
+ *   d_out [S, N, Hq, head_dim] bfloat16, d_lse [S, N, Hq] float32 or NULL, contiguous.
+ *   d_work: spec_tree_attention_bytes() of scratch, 16-byte aligned, for this call alone; needs no initial value.
+ * Products are bf16 x bf16 with fp32 accumulation; statistics are fp32; the weights exp(s - max) are rounded to
+ * bfloat16 for their product with the values.  Results do not depend on the order in which blocks of work finish.
+ */
+size_t spec_tree_attention_bytes(spec_ctx* ctx, const spec_kv_cache* cache, int S, int N, int Hq);
+int spec_tree_attention(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_q, long long q_tok, long long q_head, const void* d_k,
+                        long long k_tok, long long k_head, const void* d_v, long long v_tok, long long v_head, int S, int N, int Hq,
+                        const int32_t* d_mask, const int32_t* d_len, const int32_t* d_nnodes, float scale, void* d_out,
+                        float* d_lse, void* d_work, size_t work_bytes, void* stream);
 
 /*
  * Test aid: the same tensor-core main loop as the two head calls with a plain store epilogue.

@@ -11,7 +11,7 @@ from .build import LIB, build_library
 
 FLAG_DEDUP, FLAG_MODEL_FILL, FLAG_KEY_NEXT_TOKEN, FLAG_PARTIAL_TAIL = 1, 2, 4, 8
 STATUS_TOKEN_RANGE, STATUS_CAPACITY, STATUS_TIMEOUT, STATUS_GROUPS, STATUS_INDEX = 1, 2, 4, 8, 16
-SPEC_F32, SPEC_BF16 = 0, 1
+SPEC_F32, SPEC_BF16, SPEC_E4M3 = 0, 1, 2
 
 _HEADER = os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "include", "ngram_spec.h")
 _lib = None
@@ -24,6 +24,16 @@ def flag_reserve(n: int) -> int:
 
 class SpecError(RuntimeError):
     pass
+
+
+class _KVCacheStruct(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_exp", C.c_void_p), ("d_v_exp", C.c_void_p), ("d_table", C.c_void_p),
+                ("dtype", C.c_int), ("n_pages", C.c_int), ("max_pages", C.c_int), ("page", C.c_int), ("heads", C.c_int),
+                ("head_dim", C.c_int)]
+
+
+class _RopeStruct(C.Structure):
+    _fields_ = [("d_freq", C.c_void_p), ("rot", C.c_int), ("interleaved", C.c_int), ("factor", C.c_float)]
 
 
 def declared_symbols() -> list[str]:
@@ -77,6 +87,15 @@ def load_library(build: bool = True) -> C.CDLL:
                                                  C.c_int, i32p, i32p, i32p, i32p, vp]
     lib.accept_and_commit_indexed.argtypes = [vp, vp, i32p, i32p, i32p, C.c_int, C.c_int, C.c_int, i32p, i32p, C.c_int, i32p,
                                               i32p, i32p, vp]
+    i, ll, cachep, ropep = C.c_int, C.c_longlong, C.POINTER(_KVCacheStruct), C.POINTER(_RopeStruct)
+    rows = [vp, ll, ll]
+    lib.spec_rope_rows.argtypes = [vp, ropep, vp, i, ll, ll, vp, vp, i, ll, ll, vp, i, i32p, i, vp]
+    lib.spec_cache_write.argtypes = [vp, cachep, *rows, *rows, i, i, i, i32p, i32p, i32p, ropep, vp]
+    lib.spec_cache_read.argtypes = [vp, cachep, i, i, i32p, i32p, vp, vp, vp]
+    lib.spec_tree_mask.argtypes = [vp, i32p, i, i, i32p, i32p, i32p, vp]
+    lib.spec_tree_attention_bytes.argtypes = [vp, cachep, i, i, i]
+    lib.spec_tree_attention_bytes.restype = C.c_size_t
+    lib.spec_tree_attention.argtypes = [vp, cachep, *rows, *rows, *rows, i, i, i, i32p, i32p, i32p, C.c_float, vp, fp, vp, C.c_size_t, vp]
     lib.spec_launch_count.argtypes = [vp]
     lib.spec_launch_count.restype = C.c_longlong
     _lib = lib
@@ -96,6 +115,70 @@ def _ptr(t, dtype=None):
 
 def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise SpecError(what)
+
+
+def _rows(t: torch.Tensor, name: str):
+    """Pointer, token stride and head stride of ``t[S, N, heads, D]`` or ``t[T, heads, D]`` whose head vectors are
+    contiguous and whose sequences follow one another at N token strides."""
+    _need(t.is_cuda and t.dtype == torch.bfloat16, f"{name}: expected a bfloat16 CUDA tensor")
+    st = t.stride()
+    _need(st[-1] == 1 and (t.dim() == 3 or t.shape[0] <= 1 or st[0] == st[1] * t.shape[1]),
+          f"{name}: head vectors must be contiguous, and sequences N tokens apart")
+    return t.data_ptr(), st[-3], st[-2]
+
+
+def _i32(t: torch.Tensor | None, name: str, shape):
+    if t is None:
+        return None
+    _need(t.is_cuda and t.dtype == torch.int32 and t.shape == shape and t.is_contiguous(),
+          f"{name}: expected a contiguous int32 CUDA tensor of shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+class KVCache:
+    """A paged key/value cache in the caller's tensors (see ``spec_kv_cache`` in the header).
+
+    ``k``, ``v`` are ``[n_pages, heads, page, head_dim]``, bfloat16 or uint8 (E4M3 codes); ``table[S, max_pages]`` int32
+    holds each sequence's pages; an E4M3 cache has ``k_exp``, ``v_exp`` ``[n_pages, heads, page]`` uint8.
+    """
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k_exp: torch.Tensor | None = None, v_exp: torch.Tensor | None = None):
+        _need(k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.dtype in (torch.bfloat16, torch.uint8),
+              "KVCache: k and v must be [n_pages, heads, page, head_dim], both bfloat16 or both uint8")
+        _need((k.dtype == torch.uint8) == (k_exp is not None) == (v_exp is not None), "KVCache: k_exp and v_exp belong to uint8 codes")
+        _need(table.dim() == 2 and table.dtype == torch.int32, "KVCache: table must be int32 [S, max_pages]")
+        for t in (k_exp, v_exp):
+            _need(t is None or (t.dtype == torch.uint8 and t.shape == k.shape[:3]), "KVCache: scales must be uint8 [n_pages, heads, page]")
+        for t in (k, v, table, k_exp, v_exp):
+            _need(t is None or (t.is_cuda and t.is_contiguous()), "KVCache: tensors must be contiguous CUDA tensors")
+        self.k, self.v, self.table, self.k_exp, self.v_exp = k, v, table, k_exp, v_exp
+        self.n_pages, self.heads, self.page, self.head_dim = (int(x) for x in k.shape)
+        ptr = lambda t: None if t is None else t.data_ptr()
+        self._struct = _KVCacheStruct(ptr(k), ptr(v), ptr(k_exp), ptr(v_exp), ptr(table), SPEC_BF16 if k.dtype == torch.bfloat16 else SPEC_E4M3,
+                                      self.n_pages, int(table.shape[1]), self.page, self.heads, self.head_dim)
+        self._ref = C.byref(self._struct)
+
+    @classmethod
+    def empty(cls, n_pages: int, heads: int, page: int, head_dim: int, table: torch.Tensor, quantised: bool = False) -> "KVCache":
+        shape = (n_pages, heads, page, head_dim)
+        k, v = (torch.empty(shape, dtype=torch.uint8 if quantised else torch.bfloat16, device=table.device) for _ in range(2))
+        ke, ve = (torch.empty(shape[:3], dtype=torch.uint8, device=table.device) if quantised else None for _ in range(2))
+        return cls(k, v, table, ke, ve)
+
+
+class Rope:
+    """Rotary positions: ``freq[rot / 2]`` float32 radians per position (see ``spec_rope`` in the header)."""
+
+    def __init__(self, freq: torch.Tensor, interleaved: bool = False, scale: float = 1.0):
+        _need(freq.is_cuda and freq.dtype == torch.float32 and freq.dim() == 1 and freq.is_contiguous(), "Rope: freq must be a contiguous float32 CUDA vector")
+        self.freq = freq
+        self._struct = _RopeStruct(freq.data_ptr(), 2 * int(freq.shape[0]), int(interleaved), float(scale))
+        self._ref = C.byref(self._struct)
 
 
 class SpecContext:
@@ -341,6 +424,80 @@ class SpecContext:
                                                        _ptr(scratch[1], torch.float32), _ptr(am), _ptr(mx), _stream()),
                     "verify_lmhead_argmax_fp8")
         return am, mx
+
+    def rope_rows(self, rope: Rope, q: torch.Tensor, k: torch.Tensor | None, pos: torch.Tensor, out=None):
+        """Rotates ``q[T, Hq, D]`` and ``k[T, Hk, D]`` (or ``[S, N, heads, D]``; ``k`` may be None) at ``pos`` [T] (or [S, N]).
+
+        Returns contiguous ``(q_out, k_out)``, or writes to ``out``, whose tensors may be ``q`` and ``k`` themselves.
+        """
+        if out is None:
+            out = (torch.empty(q.shape, dtype=q.dtype, device=q.device), None if k is None else torch.empty(k.shape, dtype=k.dtype, device=k.device))
+        D, T = q.shape[-1], q.shape[:-2].numel()
+        _need(k is None or (k.shape[-1] == D and k.shape[:-2] == q.shape[:-2]), "rope_rows: q and k must have the same tokens and head size")
+        for x, y in zip((q, k), out):
+            _need(x is None or (y.shape == x.shape and y.dtype == x.dtype and y.is_contiguous()), "rope_rows: outputs must be contiguous, of the inputs' shapes")
+        qp, qt, qh = _rows(q, "q")
+        kp, kt, kh = (None, 0, 0) if k is None else _rows(k, "k")
+        self._check(self._lib.spec_rope_rows(self._h, rope._ref, qp, q.shape[-2], qt, qh, out[0].data_ptr(), kp, 0 if k is None else k.shape[-2],
+                                             kt, kh, None if k is None else out[1].data_ptr(), D, _i32(pos, "pos", q.shape[:-2]), T, _stream()),
+                    "spec_rope_rows")
+        return out
+
+    def cache_write(self, cache: KVCache, k: torch.Tensor, v: torch.Tensor, start: torch.Tensor, count: torch.Tensor | None = None,
+                    nodes: torch.Tensor | None = None, rope: Rope | None = None):
+        """Writes ``k``, ``v`` ``[S, N, heads, D]`` to positions ``start[s] + i``, ``i < count[s]`` (all N): node ``nodes[s, i]`` or ``i``."""
+        S, N = int(k.shape[0]), int(k.shape[1])
+        _need(k.dim() == 4 and k.shape == v.shape and tuple(k.shape[2:]) == (cache.heads, cache.head_dim) and S == cache.table.shape[0],
+              "cache_write: k and v must be [S, N, heads, head_dim] of the cache")
+        n = N if nodes is None else int(nodes.shape[1])
+        self._check(self._lib.spec_cache_write(self._h, cache._ref, *_rows(k, "k"), *_rows(v, "v"), S, N, n, _i32(nodes, "nodes", (S, n)),
+                                               _i32(start, "start", (S,)), _i32(count, "count", (S,)), None if rope is None else rope._ref,
+                                               _stream()), "spec_cache_write")
+
+    def cache_read(self, cache: KVCache, start: torch.Tensor, n: int, count: torch.Tensor | None = None, out=None):
+        """Positions ``start[s] + i``, ``i < count[s]`` (``n``), as bfloat16 ``(k, v)`` ``[S, n, heads, D]``; zeros beyond."""
+        S = int(cache.table.shape[0])
+        if out is None:
+            out = tuple(torch.empty((S, n, cache.heads, cache.head_dim), dtype=torch.bfloat16, device=cache.k.device) for _ in range(2))
+        for t in out:
+            _need(tuple(t.shape) == (S, n, cache.heads, cache.head_dim) and t.is_contiguous(), "cache_read: outputs must be contiguous [S, n, heads, head_dim]")
+        self._check(self._lib.spec_cache_read(self._h, cache._ref, S, n, _i32(start, "start", (S,)), _i32(count, "count", (S,)),
+                                              _ptr(out[0], torch.bfloat16), _ptr(out[1], torch.bfloat16), _stream()), "spec_cache_read")
+        return out
+
+    def tree_mask(self, parent: torch.Tensor, n_nodes: torch.Tensor | None = None):
+        """Mask words ``[S, N, ceil(N / 32)]`` and depths ``[S, N]`` (int32) of the forests ``parent[S, N]`` (-1 = root)."""
+        S, N = int(parent.shape[0]), int(parent.shape[1])
+        mask = torch.empty((S, N, (N + 31) // 32), dtype=torch.int32, device=parent.device)
+        depth = torch.empty((S, N), dtype=torch.int32, device=parent.device)
+        self._check(self._lib.spec_tree_mask(self._h, _i32(parent, "parent", (S, N)), S, N, _i32(n_nodes, "n_nodes", (S,)), mask.data_ptr(),
+                                             depth.data_ptr(), _stream()), "spec_tree_mask")
+        return mask, depth
+
+    def tree_attention(self, cache: KVCache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, mask: torch.Tensor, lens: torch.Tensor,
+                       n_nodes: torch.Tensor | None = None, scale: float | None = None, with_lse: bool = False, out=None,
+                       work: torch.Tensor | None = None):
+        """Attention of the block ``q[S, N, Hq, D]``, ``k``, ``v`` ``[S, N, heads, D]`` over the cache and its own ancestors (``mask``).
+
+        Returns ``(out[S, N, Hq, D] bfloat16, lse[S, N, Hq] float32 or None)``; ``scale`` defaults to ``D ** -0.5``.
+        """
+        S, N, Hq, D = q.shape
+        _need(k.shape == v.shape and tuple(k.shape) == (S, N, cache.heads, cache.head_dim) and D == cache.head_dim and S == cache.table.shape[0],
+              "tree_attention: q must be [S, N, Hq, head_dim], k and v [S, N, heads, head_dim] of the cache")
+        if out is None:
+            out = (torch.empty((S, N, Hq, D), dtype=torch.bfloat16, device=q.device),
+                   torch.empty((S, N, Hq), dtype=torch.float32, device=q.device) if with_lse else None)
+        else:
+            _need(out[0].shape == q.shape and (out[1] is None or out[1].shape == q.shape[:3]), "tree_attention: outputs must be [S, N, Hq, head_dim] and [S, N, Hq]")
+        need = self._lib.spec_tree_attention_bytes(self._h, cache._ref, S, N, Hq)
+        if work is None:
+            work = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        self._check(self._lib.spec_tree_attention(self._h, cache._ref, *_rows(q, "q"), *_rows(k, "k"), *_rows(v, "v"), S, N, Hq,
+                                                  _i32(mask, "mask", (S, N, (N + 31) // 32)), _i32(lens, "lens", (S,)),
+                                                  _i32(n_nodes, "n_nodes", (S,)), D ** -0.5 if scale is None else scale,
+                                                  _ptr(out[0], torch.bfloat16), _ptr(out[1], torch.float32), work.data_ptr(), work.numel(),
+                                                  _stream()), "spec_tree_attention")
+        return out
 
     def debug_logits(self, rows: torch.Tensor) -> torch.Tensor:
         m = int(rows.shape[0])

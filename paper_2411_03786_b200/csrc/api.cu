@@ -7,6 +7,7 @@
 #include <cuda_bf16.h>
 
 #include "accept.cuh"
+#include "cache.cuh"
 #include "common.cuh"
 #include "draft_common.cuh"
 
@@ -474,6 +475,143 @@ int spec_debug_expire_wait(spec_ctx* ctx, unsigned long long limit_ns, int mark_
     if (limit_ns > 1000000000ull) return fail(ctx, SPEC_ERR_ARG, "spec_debug_expire_wait: the limit may not exceed one second");
     cudaSetDevice(ctx->device);
     return launch_wait_probe(ctx, limit_ns, mark_verify_incomplete ? 1 : 0, (cudaStream_t)stream);
+}
+
+// ------------------------------------------------------------------------------------------ attention and its cache
+static int check_cache(spec_ctx* ctx, const spec_kv_cache* c, const char* who, CacheArgs* out) {
+    if (!c || !c->d_k || !c->d_v || !c->d_table) return fail(ctx, SPEC_ERR_ARG, "%s: NULL cache pointer", who);
+    if (!aligned16(c->d_k) || !aligned16(c->d_v)) return fail(ctx, SPEC_ERR_ARG, "%s: cache pointers must be 16-byte aligned", who);
+    if (c->dtype != SPEC_BF16 && c->dtype != SPEC_E4M3) return fail(ctx, SPEC_ERR_ARG, "%s: cache dtype must be SPEC_BF16 or SPEC_E4M3", who);
+    if (c->dtype == SPEC_E4M3 && (!c->d_k_exp || !c->d_v_exp)) return fail(ctx, SPEC_ERR_ARG, "%s: an E4M3 cache needs its scales", who);
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(ctx, SPEC_ERR_UNSUPPORTED, "%s: head_dim must be 64 or 128", who);
+    if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128)
+        return fail(ctx, SPEC_ERR_UNSUPPORTED, "%s: page must be 16, 32, 64 or 128 tokens", who);
+    if (c->heads < 1 || c->n_pages < 1 || c->max_pages < 1 || (long long)c->n_pages * c->heads * c->page >= (1ll << 31) ||
+        (long long)c->max_pages * c->page >= (1ll << 31))
+        return fail(ctx, SPEC_ERR_ARG, "%s: need heads, n_pages, max_pages >= 1, n_pages * heads * page < 2^31 and max_pages * page < 2^31", who);
+    int shift = 4;
+    while ((1 << shift) < c->page) ++shift;
+    *out = CacheArgs{c->d_k, c->d_v, c->d_k_exp, c->d_v_exp, c->d_table, c->n_pages, c->max_pages, shift, c->heads, c->head_dim, c->dtype == SPEC_E4M3};
+    return SPEC_OK;
+}
+static int check_rope(spec_ctx* ctx, const spec_rope* r, int head_dim, const char* who, RopeArgs* out) {
+    if (!r->d_freq) return fail(ctx, SPEC_ERR_ARG, "%s: rope frequencies are NULL", who);
+    if (r->rot < 16 || r->rot > head_dim || r->rot % 16 != 0) return fail(ctx, SPEC_ERR_ARG, "%s: need 16 <= rot <= head_dim, rot %% 16 == 0", who);
+    *out = RopeArgs{r->d_freq, r->rot, r->interleaved != 0, r->factor};
+    return SPEC_OK;
+}
+// Rows of heads that the kernels read 16 bytes at a time.
+static int check_rows(spec_ctx* ctx, const void* d, long long tok, long long head, const char* who, const char* what) {
+    if (!d) return fail(ctx, SPEC_ERR_ARG, "%s: %s is NULL", who, what);
+    if (!aligned16(d) || tok % 8 != 0 || head % 8 != 0 || tok < 0 || head < 0)
+        return fail(ctx, SPEC_ERR_ARG, "%s: %s must be 16-byte aligned with strides >= 0 that are multiples of 8 elements", who, what);
+    return SPEC_OK;
+}
+
+int spec_rope_rows(spec_ctx* ctx, const spec_rope* rope, const void* d_q, int Hq, long long q_tok, long long q_head, void* d_q_out,
+                   const void* d_k, int Hk, long long k_tok, long long k_head, void* d_k_out, int head_dim, const int32_t* d_pos, int T,
+                   void* stream) {
+    const char* who = "spec_rope_rows";
+    if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
+    if (!rope || !d_pos) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
+    if (head_dim < 16 || head_dim > 512 || head_dim % 16 != 0) return fail(ctx, SPEC_ERR_ARG, "%s: need 16 <= head_dim <= 512, head_dim %% 16 == 0", who);
+    if (T < 0 || Hq < 1 || Hk < 0 || Hq > 4096 || Hk > 4096) return fail(ctx, SPEC_ERR_ARG, "%s: need T >= 0, 1 <= Hq <= 4096, 0 <= Hk <= 4096", who);
+    RopeArgs r;
+    int rc = check_rope(ctx, rope, head_dim, who, &r);
+    if (rc || (rc = check_rows(ctx, d_q, q_tok, q_head, who, "q")) || (rc = check_rows(ctx, d_q_out, 0, 0, who, "q_out"))) return rc;
+    if (Hk && ((rc = check_rows(ctx, d_k, k_tok, k_head, who, "k")) || (rc = check_rows(ctx, d_k_out, 0, 0, who, "k_out")))) return rc;
+    if (T == 0) return SPEC_OK;
+    cudaSetDevice(ctx->device);
+    return launch_rope_rows(ctx, r, d_q, Hq, q_tok, q_head, d_q_out, d_k, Hk, k_tok, k_head, d_k_out, head_dim, d_pos, T, (cudaStream_t)stream);
+}
+
+int spec_cache_write(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_k, long long k_tok, long long k_head, const void* d_v,
+                     long long v_tok, long long v_head, int S, int N, int n, const int32_t* d_nodes, const int32_t* d_start,
+                     const int32_t* d_count, const spec_rope* rope, void* stream) {
+    const char* who = "spec_cache_write";
+    if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
+    CacheArgs c;
+    RopeArgs r{nullptr, 0, 0, 1.0f};
+    int rc = check_cache(ctx, cache, who, &c);
+    if (rc || (rc = check_rows(ctx, d_k, k_tok, k_head, who, "k")) || (rc = check_rows(ctx, d_v, v_tok, v_head, who, "v"))) return rc;
+    if (!d_start) return fail(ctx, SPEC_ERR_ARG, "%s: d_start is NULL", who);
+    if (S < 0 || S > 65535 || N < 0 || n < 0 || (!d_nodes && n > N)) return fail(ctx, SPEC_ERR_ARG, "%s: need 0 <= S <= 65535, N >= 0, n >= 0, and n <= N without d_nodes", who);
+    if (rope && (rc = check_rope(ctx, rope, c.head_dim, who, &r))) return rc;
+    if (S == 0 || n == 0) return SPEC_OK;
+    cudaSetDevice(ctx->device);
+    return launch_cache_write(ctx, c, d_k, k_tok, k_head, d_v, v_tok, v_head, S, N, n, d_nodes, d_start, d_count, r, (cudaStream_t)stream);
+}
+
+int spec_cache_read(spec_ctx* ctx, const spec_kv_cache* cache, int S, int n, const int32_t* d_start, const int32_t* d_count,
+                    void* d_k_out, void* d_v_out, void* stream) {
+    const char* who = "spec_cache_read";
+    if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
+    CacheArgs c;
+    int rc = check_cache(ctx, cache, who, &c);
+    if (rc || (rc = check_rows(ctx, d_k_out, 0, 0, who, "k_out")) || (rc = check_rows(ctx, d_v_out, 0, 0, who, "v_out"))) return rc;
+    if (!d_start) return fail(ctx, SPEC_ERR_ARG, "%s: d_start is NULL", who);
+    if (S < 0 || S > 65535 || n < 0) return fail(ctx, SPEC_ERR_ARG, "%s: need 0 <= S <= 65535, n >= 0", who);
+    if (S == 0 || n == 0) return SPEC_OK;
+    cudaSetDevice(ctx->device);
+    return launch_cache_read(ctx, c, S, n, d_start, d_count, d_k_out, d_v_out, (cudaStream_t)stream);
+}
+
+int spec_tree_mask(spec_ctx* ctx, const int32_t* d_parent, int S, int N, const int32_t* d_nnodes, int32_t* d_mask, int32_t* d_depth,
+                   void* stream) {
+    if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "spec_tree_mask: ctx is NULL");
+    if (!d_parent || !d_mask) return fail(ctx, SPEC_ERR_ARG, "spec_tree_mask: NULL pointer");
+    if (S < 0 || S > 65535 || N < 1 || N > kMaxNodes) return fail(ctx, SPEC_ERR_ARG, "spec_tree_mask: need 0 <= S <= 65535, 1 <= N <= %d", kMaxNodes);
+    if (S == 0) return SPEC_OK;
+    cudaSetDevice(ctx->device);
+    return launch_tree_mask(ctx, d_parent, S, N, d_nnodes, d_mask, d_depth, (cudaStream_t)stream);
+}
+
+static int check_block(spec_ctx* ctx, const spec_kv_cache* cache, int S, int N, int Hq, const char* who, CacheArgs* c) {
+    int rc = check_cache(ctx, cache, who, c);
+    if (rc) return rc;
+    if (S < 0 || S > 65535 || N < 1 || N > kMaxNodes) return fail(ctx, SPEC_ERR_ARG, "%s: need 0 <= S <= 65535, 1 <= N <= %d", who, kMaxNodes);
+    if (Hq < c->heads || Hq % c->heads != 0 || Hq > 4096) return fail(ctx, SPEC_ERR_ARG, "%s: Hq must be a multiple of the cache's heads, at most 4096", who);
+    return SPEC_OK;
+}
+
+size_t spec_tree_attention_bytes(spec_ctx* ctx, const spec_kv_cache* cache, int S, int N, int Hq) {
+    CacheArgs c;
+    if (!ctx || check_block(ctx, cache, S, N, Hq, "spec_tree_attention_bytes", &c)) return 0;
+    return tree_attention_bytes(ctx->num_sms, S, N, Hq, c.heads, c.head_dim);
+}
+
+int spec_tree_attention(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_q, long long q_tok, long long q_head, const void* d_k,
+                        long long k_tok, long long k_head, const void* d_v, long long v_tok, long long v_head, int S, int N, int Hq,
+                        const int32_t* d_mask, const int32_t* d_len, const int32_t* d_nnodes, float scale, void* d_out, float* d_lse,
+                        void* d_work, size_t work_bytes, void* stream) {
+    const char* who = "spec_tree_attention";
+    if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
+    TreeAttnArgs a{};
+    int rc = check_block(ctx, cache, S, N, Hq, who, &a.cache);
+    if (rc || (rc = check_rows(ctx, d_q, q_tok, q_head, who, "q")) || (rc = check_rows(ctx, d_k, k_tok, k_head, who, "k")) ||
+        (rc = check_rows(ctx, d_v, v_tok, v_head, who, "v")) || (rc = check_rows(ctx, d_out, 0, 0, who, "out")) ||
+        (rc = check_rows(ctx, d_work, 0, 0, who, "work")))
+        return rc;
+    if (!d_mask || !d_len) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
+    if (!(scale > 0.0f) || scale > 3e38f) return fail(ctx, SPEC_ERR_ARG, "%s: scale must be positive and finite", who);
+    const size_t need = tree_attention_bytes(ctx->num_sms, S, N, Hq, a.cache.heads, a.cache.head_dim);
+    if (work_bytes < need) return fail(ctx, SPEC_ERR_ARG, "%s: %zu bytes of scratch given, %zu needed", who, work_bytes, need);
+    if (S == 0) return SPEC_OK;
+    a.q = d_q; a.k = d_k; a.v = d_v;
+    a.q_tok = q_tok; a.q_head = q_head;
+    a.k_tok = k_tok; a.k_head = k_head;
+    a.v_tok = v_tok; a.v_head = v_head;
+    a.S = S; a.N = N; a.Hq = Hq;
+    a.mask = d_mask;
+    a.len = d_len;
+    a.n_nodes = d_nnodes;
+    a.scale = scale;
+    a.out = d_out;
+    a.lse = d_lse;
+    a.work = d_work;
+    a.status = ctx->d_status;
+    cudaSetDevice(ctx->device);
+    return launch_tree_attention(ctx, a, (cudaStream_t)stream);
 }
 
 }  // extern "C"
