@@ -284,6 +284,22 @@ int verify_lmhead_argmax_fp8(spec_ctx* ctx, const void* d_hidden, int M, uint8_t
                              int32_t* d_argmax, float* d_max, void* stream);
 
 /*
+ * Scores of given tokens.  For every row z = <hidden[m, :], unembed[y, :]>, y < V, in one pass over the head; the
+ * [M, V] logits are never written.
+ *   d_logp     [M] float32 out: log softmax of z at d_tokens[m]; 0 for token -1 (an unused draft row); -inf, and
+ *              SPEC_STATUS_TOKEN_RANGE, for any other id outside [0, V).
+ *   d_entropy  [M] float32 out: entropy of softmax(z), in nats.
+ *   d_alt_idx  [M, n_alt] int32 out, d_alt_logp [M, n_alt] float32 out: the n_alt likeliest tokens and their log
+ *              probabilities, descending, equal ones by ascending id.  0 <= n_alt <= min(32, V); NULL if 0.
+ *   d_work     spec_score_bytes() of scratch, 16-byte aligned, for this call alone; needs no initial value.
+ * bf16 x bf16 products accumulate in fp32 on the tensor cores; the statistics are fp32, relative to the running
+ * maximum.  If a bounded device-side wait expires (SPEC_STATUS_TIMEOUT) the outputs mean nothing.
+ */
+size_t spec_score_bytes(spec_ctx* ctx, int M, int n_alt);
+int score_tokens(spec_ctx* ctx, const void* d_hidden, int M, const int32_t* d_tokens, int n_alt, float* d_logp, float* d_entropy,
+                 int32_t* d_alt_idx, float* d_alt_logp, void* d_work, size_t work_bytes, void* stream);
+
+/*
  * Attention of a verification call (Section 3: one model call on the (B, w+1) block behind the context).
  *
  * The block holds N nodes per sequence - drafted tokens, arranged as a forest: the framework's draft rows are B chains

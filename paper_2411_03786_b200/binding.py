@@ -92,6 +92,9 @@ def load_library(build: bool = True) -> C.CDLL:
     lib.spec_rope_rows.argtypes = [vp, ropep, vp, i, ll, ll, vp, vp, i, ll, ll, vp, i, i32p, i, vp]
     lib.spec_cache_write.argtypes = [vp, cachep, *rows, *rows, i, i, i, i32p, i32p, i32p, ropep, vp]
     lib.spec_cache_read.argtypes = [vp, cachep, i, i, i32p, i32p, vp, vp, vp]
+    lib.spec_score_bytes.argtypes = [vp, i, i]
+    lib.spec_score_bytes.restype = C.c_size_t
+    lib.score_tokens.argtypes = [vp, vp, i, i32p, i, fp, fp, i32p, fp, vp, C.c_size_t, vp]
     lib.spec_tree_mask.argtypes = [vp, i32p, i, i, i32p, i32p, i32p, vp]
     lib.spec_tree_attention_bytes.argtypes = [vp, cachep, i, i, i]
     lib.spec_tree_attention_bytes.restype = C.c_size_t
@@ -424,6 +427,24 @@ class SpecContext:
                                                        _ptr(scratch[1], torch.float32), _ptr(am), _ptr(mx), _stream()),
                     "verify_lmhead_argmax_fp8")
         return am, mx
+
+    def score_tokens(self, hidden: torch.Tensor, tokens: torch.Tensor, n_alt: int = 0, out=None, work: torch.Tensor | None = None):
+        """Log probability of ``tokens[M]`` after ``hidden[M, d]``, entropy, and the ``n_alt`` likeliest tokens.
+
+        Returns ``(logp[M], entropy[M], alt_ids[M, n_alt] or None, alt_logp[M, n_alt] or None)``.
+        """
+        M, dev = hidden.shape[0], hidden.device
+        _need(hidden.dim() == 2 and hidden.shape[1] == self.d, "score_tokens: hidden must be [M, d]")
+        if out is None:
+            out = (torch.empty(M, dtype=torch.float32, device=dev), torch.empty(M, dtype=torch.float32, device=dev),
+                   torch.empty((M, n_alt), dtype=torch.int32, device=dev) if n_alt else None,
+                   torch.empty((M, n_alt), dtype=torch.float32, device=dev) if n_alt else None)
+        if work is None:
+            work = torch.empty(max(16, self._lib.spec_score_bytes(self._h, M, n_alt)), dtype=torch.uint8, device=dev)
+        self._check(self._lib.score_tokens(self._h, _ptr(hidden, torch.bfloat16), M, _i32(tokens, "tokens", (M,)), n_alt, _ptr(out[0], torch.float32),
+                                           _ptr(out[1], torch.float32), _ptr(out[2], torch.int32), _ptr(out[3], torch.float32), work.data_ptr(),
+                                           work.numel(), _stream()), "score_tokens")
+        return out
 
     def rope_rows(self, rope: Rope, q: torch.Tensor, k: torch.Tensor | None, pos: torch.Tensor, out=None):
         """Rotates ``q[T, Hq, D]`` and ``k[T, Hk, D]`` (or ``[S, N, heads, D]``; ``k`` may be None) at ``pos`` [T] (or [S, N]).

@@ -477,6 +477,26 @@ int spec_debug_expire_wait(spec_ctx* ctx, unsigned long long limit_ns, int mark_
     return launch_wait_probe(ctx, limit_ns, mark_verify_incomplete ? 1 : 0, (cudaStream_t)stream);
 }
 
+size_t spec_score_bytes(spec_ctx* ctx, int M, int n_alt) {
+    if (!ctx || M < 1 || M > SPEC_MAX_VERIFY_ROWS || n_alt < 0 || n_alt > kMaxKTab || n_alt > ctx->V) return 0;
+    return score_bytes(ctx, M, n_alt);
+}
+
+int score_tokens(spec_ctx* ctx, const void* d_hidden, int M, const int32_t* d_tokens, int n_alt, float* d_logp, float* d_entropy,
+                 int32_t* d_alt_idx, float* d_alt_logp, void* d_work, size_t work_bytes, void* stream) {
+    if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "score_tokens: ctx is NULL");
+    if (!d_hidden || !d_tokens || !d_logp || !d_entropy || !d_work) return fail(ctx, SPEC_ERR_ARG, "score_tokens: NULL pointer");
+    if (!aligned16(d_hidden) || !aligned16(d_work)) return fail(ctx, SPEC_ERR_ARG, "score_tokens: d_hidden and d_work must be 16-byte aligned");
+    if (M < 0 || M > SPEC_MAX_VERIFY_ROWS) return fail(ctx, SPEC_ERR_ARG, "score_tokens: need 0 <= M <= %d", SPEC_MAX_VERIFY_ROWS);
+    if (n_alt < 0 || n_alt > kMaxKTab || n_alt > ctx->V || (n_alt > 0 && (!d_alt_idx || !d_alt_logp)))
+        return fail(ctx, SPEC_ERR_ARG, "score_tokens: need 0 <= n_alt <= min(%d, V), with both outputs for n_alt > 0", kMaxKTab);
+    if (M == 0) return SPEC_OK;
+    const size_t need = score_bytes(ctx, M, n_alt);
+    if (work_bytes < need) return fail(ctx, SPEC_ERR_ARG, "score_tokens: %zu bytes of scratch given, %zu needed", work_bytes, need);
+    cudaSetDevice(ctx->device);
+    return launch_score(ctx, d_hidden, M, d_tokens, n_alt, d_logp, d_entropy, d_alt_idx, d_alt_logp, d_work, (cudaStream_t)stream);
+}
+
 // ------------------------------------------------------------------------------------------ attention and its cache
 static int check_cache(spec_ctx* ctx, const spec_kv_cache* c, const char* who, CacheArgs* out) {
     if (!c || !c->d_k || !c->d_v || !c->d_table) return fail(ctx, SPEC_ERR_ARG, "%s: NULL cache pointer", who);

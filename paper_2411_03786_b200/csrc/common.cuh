@@ -163,6 +163,9 @@ int launch_table(spec_ctx* ctx, const void* d_rows, int n_rows, int k_tab, int32
 int launch_extend_table(spec_ctx* ctx, const int32_t* d_tab_idx, int k_tab, int w_ext, int32_t* d_ext, cudaStream_t st);
 int launch_logits(spec_ctx* ctx, const void* d_rows, int m, float* d_logits, cudaStream_t st);
 int launch_unigram(spec_ctx* ctx, int k_uni, int32_t* d_uni_idx, float* d_dist2, cudaStream_t st);
+size_t score_bytes(spec_ctx* ctx, int M, int n_alt);
+int launch_score(spec_ctx* ctx, const void* d_hidden, int M, const int32_t* d_tokens, int n_alt, float* d_logp, float* d_entropy,
+                 int32_t* d_alt_idx, float* d_alt_logp, void* d_work, cudaStream_t st);
 int launch_wait_probe(spec_ctx* ctx, unsigned long long limit_ns, int mark_incomplete, cudaStream_t st);
 // ctx_index.cu
 size_t context_index_bytes(int S, int cap, int n_q);

@@ -6,6 +6,7 @@
 //   MODE_STORE   plain fp32 store, for the logits tolerance check            (spec_debug_logits)
 //   MODE_SUMSQ   model unigram: per row the sum of squares over all columns  (build_model_unigram)
 //   MODE_ARGMAX_Q8  verification over the 8-bit (E4M3) copy of the head          (verify_lmhead_argmax_fp8)
+//   MODE_SCORE   per row the softmax statistics, one entry and the k largest     (score_tokens)
 //
 // A is [a_rows, d] and W is [V, d], both bf16 and K-major, so both operands use the same
 // 128-byte-swizzled K-major shared-memory layout.  (The 8-bit mode reads one-byte elements: a
@@ -53,7 +54,8 @@ constexpr int TMEM_COLS = 512;
 constexpr int GEMM_THREADS = 192;
 constexpr unsigned long long WAIT_LIMIT_NS = 2000000000ull;  // default limit of every device-side wait
 
-enum { MODE_ARGMAX = 0, MODE_TOPK = 1, MODE_STORE = 2, MODE_SUMSQ = 3, MODE_ARGMAX_Q8 = 4 };
+enum { MODE_ARGMAX = 0, MODE_TOPK = 1, MODE_STORE = 2, MODE_SUMSQ = 3, MODE_ARGMAX_Q8 = 4, MODE_SCORE = 5 };
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct GemmParams {
     int a_rows;    // rows of A
@@ -90,6 +92,8 @@ struct GemmParams {
     const float* col_scale;  // 8-bit mode: scale of each row of W (= column of the product)
     const float* row_scale;  // 8-bit mode: scale of each row of A (only the reported maximum needs it)
     unsigned long long wait_limit_ns;  // every mbarrier wait gives up after this long
+    const int32_t* tokens;   // score mode: the token of each row whose logit is kept
+    float4* part_stat;       // score mode: [n_chunks, a_rows] (m, l, t, z), see MODE_SCORE in the epilogue
     int prefetch_w;          // 1: the W tiles of the first ring fill are requested before the dependency wait
 };
 
@@ -224,6 +228,13 @@ __device__ __forceinline__ uint32_t orderable_f32(float v) {
 }
 __device__ __forceinline__ float from_orderable_f32(uint32_t u) {
     return __uint_as_float((u & 0x80000000u) ? (u & 0x7FFFFFFFu) : ~u);
+}
+
+// 2^x; the hardware's approximation (relative error about 2^-22).
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 // Arg max of 32 consecutive columns as a tree of independent comparisons (depth 5 instead of a chain
@@ -535,6 +546,10 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             // Sorted list, value descending, statically indexed so it stays in registers.  The k_tab live
             // entries sit at the bottom [KT - k_tab, KT); the slots above hold +inf, which nothing beats,
             // so the running threshold is always the last slot.
+            // Score mode: softmax statistics of the columns seen so far, with a_y = (z_y - m) log2(e):
+            // m = max z, sl = sum 2^a, st = sum a 2^a (so that entropy = ln(sl) - ln(2) st / sl), and the token's logit.
+            float sm = -INFINITY, sl = 0.0f, st = 0.0f, sz = -INFINITY;
+            const int tok = (MODE == MODE_SCORE && row < p.a_rows) ? p.tokens[row] : -1;
             float tv[KT];
             int ti[KT];
             const int k_off = KT - p.k_tab;
@@ -604,7 +619,36 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                     tmem_wait_ld();
                     const int cbase = col0 + c * 32;
                     const int lim = n_valid - c * 32;  // >= 1
-                    if (MODE == MODE_TOPK) {
+                    if (MODE == MODE_SCORE) {
+                        float cmax = -INFINITY;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) cmax = fmaxf(cmax, j < lim ? __uint_as_float(r[j]) : -INFINITY);
+                        if (cmax > sm) {  // the statistics so far, relative to the new maximum
+                            const float shift = sm == -INFINITY ? 0.0f : (sm - cmax) * LOG2E, f = exp2_approx(shift);
+                            st = (st + shift * sl) * f;
+                            sl *= f;
+                            sm = cmax;
+                        }
+                        // (a chunk is summed by itself, in four partial sums, before it joins the running sums: an fp32
+                        // error that grows with the root of 1/32 of the columns)
+                        float l4[4] = {0.0f, 0.0f, 0.0f, 0.0f}, t4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float a = j < lim ? (__uint_as_float(r[j]) - sm) * LOG2E : -200.0f;  // 2^-200 counts as 0
+                            const float e = exp2_approx(a);
+                            l4[j & 3] += e;
+                            t4[j & 3] = fmaf(a, e, t4[j & 3]);
+                        }
+                        sl += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+                        st += (t4[0] + t4[1]) + (t4[2] + t4[3]);
+                        const unsigned at = (unsigned)(tok - cbase);
+                        if (__any_sync(0xffffffffu, at < 32u)) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (at == (unsigned)j && j < lim) sz = __uint_as_float(r[j]);
+                        }
+                    }
+                    if (MODE == MODE_TOPK || MODE == MODE_SCORE) {
                         // Almost every chunk holds nothing that beats a row's current k-th value: one maximum over the
                         // 32 columns and one vote decide that.  Otherwise the columns that some row wants are fetched
                         // again one at a time (a column address is common to the warp) and offered to every row's list;
@@ -681,7 +725,8 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                     atomicMax(p.keys + row, key);
                 } else if (MODE == MODE_SUMSQ) {
                     p.part_val[(size_t)un.chunk * p.a_rows + row] = best_v;
-                } else if (MODE == MODE_TOPK) {
+                } else if (MODE == MODE_TOPK || MODE == MODE_SCORE) {
+                    if (MODE == MODE_SCORE) p.part_stat[(size_t)un.chunk * p.a_rows + row] = make_float4(sm, sl, st, sz);
                     const size_t base = ((size_t)un.chunk * p.a_rows + row) * p.k_tab;
 #pragma unroll
                     for (int j = 0; j < KT; ++j)
@@ -992,6 +1037,8 @@ static void fill_common(spec_ctx* ctx, GemmParams& p, int a_rows, const Shape& s
     p.col_scale = nullptr;
     p.row_scale = nullptr;
     p.wait_limit_ns = WAIT_LIMIT_NS;
+    p.tokens = nullptr;
+    p.part_stat = nullptr;
     p.prefetch_w = 1;
 }
 
@@ -1174,6 +1221,118 @@ int launch_extend_table(spec_ctx* ctx, const int32_t* d_tab_idx, int k_tab, int 
     extend_table_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(d_tab_idx, ctx->V, k_tab, w_ext, d_ext);
     ctx->launches += 1;
     return check_cuda(ctx, cudaGetLastError(), "table extension launch");
+}
+
+// ------------------------------------------------------------------------------------------ scores of given tokens
+constexpr int SCORE_MAX_CHUNKS = 256;  // partial results per row: what a warp merges with eight lists per lane
+
+static Shape score_shape(spec_ctx* ctx, int M) { return cached_shape(ctx, M, SCORE_MAX_CHUNKS); }
+
+size_t score_bytes(spec_ctx* ctx, int M, int n_alt) {
+    const Shape sh = score_shape(ctx, M);
+    return (size_t)sh.n_chunks * M * (sizeof(float4) + (size_t)n_alt * 8);
+}
+
+// One warp per row joins the row's partial results: the statistics relative to the common maximum, then n_alt times
+// the largest head of the chunks' sorted lists (a lane looks after chunks lane, lane + 32, ...).
+__global__ void __launch_bounds__(128) merge_score_kernel(const float4* __restrict__ stat, const float* __restrict__ val,
+                                                          const int32_t* __restrict__ idx, int n_chunks, int M, int V, int n_alt,
+                                                          const int32_t* __restrict__ tokens, float* __restrict__ logp,
+                                                          float* __restrict__ entropy, int32_t* __restrict__ alt_idx,
+                                                          float* __restrict__ alt_logp, int* status) {
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (row >= M) return;
+    float4 s[SCORE_MAX_CHUNKS / 32];
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < SCORE_MAX_CHUNKS / 32; ++i) {
+        const int c = lane + 32 * i;
+        s[i] = c < n_chunks ? stat[(size_t)c * M + row] : make_float4(-INFINITY, 0.0f, 0.0f, -INFINITY);
+        m = fmaxf(m, s[i].x);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float l = 0.0f, t = 0.0f, z = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < SCORE_MAX_CHUNKS / 32; ++i) {
+        const float shift = s[i].x == -INFINITY ? -200.0f : (s[i].x - m) * LOG2E, f = exp2f(shift);
+        l += s[i].y * f;
+        t += (s[i].z + shift * s[i].y) * f;
+        z = fmaxf(z, s[i].w);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        l += __shfl_xor_sync(0xffffffffu, l, o);
+        t += __shfl_xor_sync(0xffffffffu, t, o);
+        z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, o));
+    }
+    const float log_l = logf(l);
+    if (lane == 0) {
+        const int tok = tokens[row];
+        if (tok != -1 && (unsigned)tok >= (unsigned)V) atomicOr(status, SPEC_STATUS_TOKEN_RANGE);
+        logp[row] = tok == -1 ? 0.0f : (z - m) - log_l;  // (an id outside the vocabulary met no column: -inf)
+        entropy[row] = log_l - LN2 * (t / l);
+    }
+    int head[SCORE_MAX_CHUNKS / 32];
+#pragma unroll
+    for (int i = 0; i < SCORE_MAX_CHUNKS / 32; ++i) head[i] = 0;
+    for (int k = 0; k < n_alt; ++k) {
+        unsigned long long best = 0ull;
+        int from = 0;
+#pragma unroll
+        for (int i = 0; i < SCORE_MAX_CHUNKS / 32; ++i) {
+            const int c = lane + 32 * i;
+            if (c < n_chunks && head[i] < n_alt) {
+                const size_t at = ((size_t)c * M + row) * n_alt + head[i];
+                const unsigned long long key = ((unsigned long long)orderable_f32(val[at]) << 32) | (uint32_t)~idx[at];
+                if (key > best) {
+                    best = key;
+                    from = i;
+                }
+            }
+        }
+        unsigned long long top = best;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const unsigned long long other = __shfl_xor_sync(0xffffffffu, top, o);
+            top = other > top ? other : top;
+        }
+        if (best == top) {  // ids are distinct: one lane
+#pragma unroll
+            for (int i = 0; i < SCORE_MAX_CHUNKS / 32; ++i) head[i] += i == from;
+        }
+        if (lane == 0) {
+            alt_idx[(size_t)row * n_alt + k] = (int32_t)~(uint32_t)top;
+            alt_logp[(size_t)row * n_alt + k] = (from_orderable_f32((uint32_t)(top >> 32)) - m) - log_l;
+        }
+    }
+}
+
+int launch_score(spec_ctx* ctx, const void* d_hidden, int M, const int32_t* d_tokens, int n_alt, float* d_logp, float* d_entropy,
+                 int32_t* d_alt_idx, float* d_alt_logp, void* d_work, cudaStream_t st) {
+    int rc = n_alt == 0 ? set_smem_attr<MODE_SCORE, 1>(ctx) : (n_alt <= 8 ? set_smem_attr<MODE_SCORE, 8>(ctx) : set_smem_attr<MODE_SCORE, 32>(ctx));
+    if (rc) return rc;
+    const Shape sh = score_shape(ctx, M);
+    const WMaps* tmW;
+    if ((rc = w_map(ctx, &tmW))) return rc;
+    CUtensorMap tmA;
+    if ((rc = make_tensor_map(ctx, &tmA, d_hidden, M, ctx->d, sh.a_box_rows))) return rc;
+    GemmParams p;
+    fill_common(ctx, p, M, sh);
+    p.tokens = d_tokens;
+    p.k_tab = n_alt;
+    p.part_stat = (float4*)d_work;
+    p.part_val = (float*)(p.part_stat + (size_t)sh.n_chunks * M);
+    p.part_idx = (int32_t*)(p.part_val + (size_t)sh.n_chunks * M * n_alt);
+    auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(sh.grid), dim3(GEMM_THREADS), (size_t)sh.smem, st, tmA, tmA, *tmW, p); };
+    cudaError_t e = n_alt == 0 ? go(head_gemm_kernel<MODE_SCORE, 1>) : (n_alt <= 8 ? go(head_gemm_kernel<MODE_SCORE, 8>) : go(head_gemm_kernel<MODE_SCORE, 32>));
+    if ((rc = check_cuda(ctx, e, "score_tokens launch"))) return rc;
+    e = launch_pdl(merge_score_kernel, dim3((M + 3) / 4), dim3(128), 0, st, p.part_stat, p.part_val, p.part_idx, sh.n_chunks, M, ctx->V, n_alt,
+                   d_tokens, d_logp, d_entropy, d_alt_idx, d_alt_logp, ctx->d_status);
+    ctx->launches += 2;
+    return check_cuda(ctx, e, "score_tokens merge launch");
 }
 
 // ------------------------------------------------------------------------------------------ bounded-wait check
