@@ -502,7 +502,8 @@ static int check_cache(spec_ctx* ctx, const spec_kv_cache* c, const char* who, C
     if (!c || !c->d_k || !c->d_v || !c->d_table) return fail(ctx, SPEC_ERR_ARG, "%s: NULL cache pointer", who);
     if (!aligned16(c->d_k) || !aligned16(c->d_v)) return fail(ctx, SPEC_ERR_ARG, "%s: cache pointers must be 16-byte aligned", who);
     if (c->dtype != SPEC_BF16 && c->dtype != SPEC_E4M3) return fail(ctx, SPEC_ERR_ARG, "%s: cache dtype must be SPEC_BF16 or SPEC_E4M3", who);
-    if (c->dtype == SPEC_E4M3 && (!c->d_k_exp || !c->d_v_exp)) return fail(ctx, SPEC_ERR_ARG, "%s: an E4M3 cache needs its scales", who);
+    if (c->dtype == SPEC_E4M3 && (!c->d_k_exp || !c->d_v_exp || !aligned16(c->d_k_exp) || !aligned16(c->d_v_exp)))
+        return fail(ctx, SPEC_ERR_ARG, "%s: an E4M3 cache needs its scales, 16-byte aligned", who);
     if (c->head_dim != 64 && c->head_dim != 128) return fail(ctx, SPEC_ERR_UNSUPPORTED, "%s: head_dim must be 64 or 128", who);
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128)
         return fail(ctx, SPEC_ERR_UNSUPPORTED, "%s: page must be 16, 32, 64 or 128 tokens", who);

@@ -1,106 +1,893 @@
-// Attention of a block of drafted nodes over a paged cache and the block itself: plain first form, a warp per
-// (node, query head) that walks the keys one by one with a running maximum and sum.
+// Attention of a block of drafted nodes over a paged cache and the block itself (spec_tree_attention).
+//
+// For a sequence s and key head h the queries of all nodes and of the G = Hq / heads query heads that share h form the
+// rows of one matrix Q, row r = node * G + g; keys and values are the cache's `len` positions followed by the block's
+// nodes, cut into tiles of 128.  Per tile
+//     S = Q K^T,   m' = max(m, rowmax S),   P = exp(c S - c m'),   l = l exp(c m - c m') + rowsum P,   O = O exp(..) + P V
+// and o = O / l at the end.  Both products run on the tensor cores (tcgen05, bf16 x bf16 -> fp32): S and O live in tensor
+// memory, P goes back into tensor memory as bfloat16 (over S, which has been read by then) and is the A operand of
+// P V from there, so that no intermediate touches shared memory.  P is at most 2^8 and keeps 8 bits; its row sum is
+// taken before the rounding.  The running maximum only moves when it is exceeded by more than 2^8, so the
+// read-modify-write of O that a new maximum costs happens in the first tiles and hardly ever after.
+//
+// Two streams per CTA hide the softmax of one tile behind the products of another.  With more than 128 rows they are
+// two row tiles against the same keys; with at most 128 they are the even and the odd tiles of keys against the same
+// rows, joined at the end (O of both streams lies in the same lanes).
+//
+// Work: the tiles of all (s, h) in a row are cut into equal consecutive ranges, one per CTA (with several row-tile pairs:
+// per group of CTAs, one for each, which walk the same keys in step and so share them in L2).  A range that ends inside
+// an (s, h) leaves fp32 partial rows and their (m, l), which a second kernel joins in a fixed order.  Any mixture of
+// lengths thus occupies all SMs to within a tile, and nothing about the lengths is needed on the host.
+//
+// Warps (512 threads): 0-3 and 4-7 softmax of stream 0 and 1 (a thread owns a row); 8-11 write key and value tiles that
+// TMA cannot (the last tile of a context, zero-padded; the block's own; an E4M3 cache's, as bfloat16 code * scale, which
+// is exact); 12 TMA; 13 issues the products.
 #include <cuda_bf16.h>
-#include <cuda_fp16.h>
 #include <math.h>
 
 #include <algorithm>
 
 #include "cache.cuh"
+#include "tc100.cuh"
 
 namespace ngs {
 
-template <int D, bool QUANT>
-__global__ void __launch_bounds__(128) tree_attention_plain_kernel(TreeAttnArgs a) {
-    constexpr int E = D / 32;
-    const int lane = threadIdx.x & 31;
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);  // (s, node, query head)
-    grid_dependency_wait();
-    grid_launch_dependents();
-    if (row >= (long long)a.S * a.N * a.Hq) return;
-    const CacheArgs& c = a.cache;
-    const int hq = (int)(row % a.Hq), h = hq / (a.Hq / c.heads);
-    const long long sn = row / a.Hq;
-    const int s = (int)(sn / a.N), node = (int)(sn - (long long)s * a.N);
-    const int live = a.n_nodes ? min(a.n_nodes[s], a.N) : a.N;
-    int len = a.len[s];
-    if (len < 0 || len > (c.max_pages << c.page_shift)) {
-        if (lane == 0) atomicOr(a.status, SPEC_STATUS_CAPACITY);
-        len = -1;
+constexpr int ATT_THREADS = 512;
+constexpr int TILE = 128;  // keys of a tile and rows of a row tile
+constexpr int ATT_SMEM = 227 * 1024;
+constexpr int REGS_SOFTMAX = 176, REGS_LOADER = 80, REGS_CONTROL = 80;
+static_assert(128 * (2 * REGS_SOFTMAX + REGS_LOADER + REGS_CONTROL) <= ATT_THREADS * 128, "the warpgroups' shares exceed the launch's registers");
+constexpr float RESCALE = 8.0f;  // log2 of how far a row's weights may exceed 1 before the maximum is moved
+
+struct AttParams {
+    TreeAttnArgs a;
+    int G, n_qtiles, side, n_groups, passes;  // side: row-tile pairs that run side by side
+    int rows_cap;                             // rows of a partial result
+    float c;                                  // scale * log2(e)
+    long long* cum;                           // [S + 1] key tiles of the sequences before
+    float2* part_ml;                          // [grid * 2, rows_cap]
+    float* part_o;                            // [grid * 2, rows_cap, D]
+    unsigned long long wait_limit_ns;
+};
+
+template <int D, bool Q8>
+struct Geometry {
+    static constexpr int HALVES = D / 64;  // 128-byte swizzle rows per vector
+    static constexpr int TILE_BYTES = TILE * D * 2;
+    static constexpr int SLOTS = Q8 ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 8);  // bf16 tiles in flight
+    static constexpr int STAGES = Q8 ? (D == 128 ? 4 : 6) : 0;                  // E4M3 tiles in flight
+    static constexpr int STAGE_BYTES = TILE * D;
+    static constexpr int EXP_AT = 2 * TILE_BYTES + SLOTS * TILE_BYTES + STAGES * STAGE_BYTES;
+    static constexpr int MISC_AT = EXP_AT + STAGES * TILE;
+    static constexpr int SMEM = MISC_AT + 1024 + 512 + 1024;
+    static_assert(SMEM <= ATT_SMEM, "shared memory");
+};
+
+struct AttShared {  // after the 1024 bytes of the (m, l) exchange
+    uint64_t full[8], empty[8], stg_full[6], stg_empty[6], s_full[2], p_full[2], o_full, q_full, xch;
+    long long lo, hi, total;
+    int s, h, t, pass;
+    int nonfinite[16];
+    uint32_t tmem;
+    int abort_flag;
+};
+static_assert(sizeof(AttShared) <= 512, "shared control block");
+
+// Key tiles of sequence s; 0 if it has no live node (or a length that its pages cannot hold).
+__device__ __forceinline__ int sequence_tiles(const TreeAttnArgs& a, int s, int& len, int& live, int& n_prefix) {
+    len = a.len[s];
+    live = a.n_nodes ? min(max(a.n_nodes[s], 0), a.N) : a.N;
+    if (len < 0 || (long long)len > ((long long)a.cache.max_pages << a.cache.page_shift)) {
+        len = 0;
+        live = 0;
     }
-    float q[E], o[E], m = -INFINITY, l = 0.0f;
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-        q[j] = __bfloat162float(((const __nv_bfloat16*)a.q)[sn * a.q_tok + hq * a.q_head + lane * E + j]);
-        o[j] = 0.0f;
-    }
-    auto key = [&](const float (&k)[E], const float (&v)[E]) {
-        float t = 0.0f;
-#pragma unroll
-        for (int j = 0; j < E; ++j) t += q[j] * k[j];
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) t += __shfl_xor_sync(0xffffffffu, t, x);
-        t *= a.scale;
-        const float mn = fmaxf(m, t), f = m == -INFINITY ? 0.0f : expf(m - mn), p = expf(t - mn);
-        l = l * f + p;
-#pragma unroll
-        for (int j = 0; j < E; ++j) o[j] = o[j] * f + p * v[j];
-        m = mn;
-    };
-    if (node < live && len >= 0) {
-        for (int pos = 0; pos < len; ++pos) {
-            const int page = c.table[(long long)s * c.max_pages + (pos >> c.page_shift)];
-            if ((unsigned)page >= (unsigned)c.n_pages) {
-                if (lane == 0) atomicOr(a.status, SPEC_STATUS_CAPACITY);
-                continue;
-            }
-            const long long at = (((long long)page * c.heads + h) << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
-            float k[E], v[E];
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const long long i = at * D + lane * E + j;
-                if (QUANT) {
-                    uint32_t x;
-                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(x) : "h"((uint16_t)(((const uint8_t*)c.k)[i] | (((const uint8_t*)c.v)[i] << 8))));
-                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x));
-                    k[j] = f.x * (c.k_exp[at] == 255 ? NAN : ldexpf(1.0f, c.k_exp[at] - 127));
-                    v[j] = f.y * (c.v_exp[at] == 255 ? NAN : ldexpf(1.0f, c.v_exp[at] - 127));
-                } else {
-                    k[j] = __bfloat162float(((const __nv_bfloat16*)c.k)[i]);
-                    v[j] = __bfloat162float(((const __nv_bfloat16*)c.v)[i]);
-                }
-            }
-            key(k, v);
-        }
-        const int words = (a.N + 31) / 32;
-        for (int j = 0; j < live; ++j) {
-            if (!((a.mask[sn * words + (j >> 5)] >> (j & 31)) & 1)) continue;
-            const long long b = (long long)s * a.N + j;
-            float k[E], v[E];
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                k[i] = __bfloat162float(((const __nv_bfloat16*)a.k)[b * a.k_tok + h * a.k_head + lane * E + i]);
-                v[i] = __bfloat162float(((const __nv_bfloat16*)a.v)[b * a.v_tok + h * a.v_head + lane * E + i]);
-            }
-            key(k, v);
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < E; ++j) ((__nv_bfloat16*)a.out)[row * D + lane * E + j] = __float2bfloat16_rn(l == 0.0f ? 0.0f : o[j] / l);
-    if (a.lse && lane == 0) a.lse[row] = m + logf(l);
+    n_prefix = (len + TILE - 1) / TILE;
+    return live == 0 ? 0 : n_prefix + (live + TILE - 1) / TILE;
 }
 
-size_t tree_attention_bytes(int num_sms, int S, int N, int Hq, int heads, int head_dim) { return 16; }
+// Groups that get a range: with fewer tiles than groups, one tile each.
+__device__ __forceinline__ long long groups_used(const AttParams& p, long long total) { return min((long long)p.n_groups, total); }
+
+// A run of key tiles [t0, t1) of one (s, h) against one row-tile pair.
+struct Segment {
+    int s, h, qt, t0, t1, n_tiles, n_prefix, len, live, rows;
+    bool whole;  // all key tiles of the (s, h)
+    int slot;    // partial result: 0 = the CTA's range starts here, 1 = it ends here
+};
+struct SegmentIter {
+    long long pos, hi;
+    int pass, s, h, t;
+    bool first;
+    __device__ __forceinline__ explicit SegmentIter(const AttShared& sh) : pos(sh.lo), hi(sh.hi), pass(sh.pass), s(sh.s), h(sh.h), t(sh.t), first(true) {}
+    __device__ __forceinline__ bool next(const AttParams& p, Segment& g) {
+        while (pos < hi) {
+            g.n_tiles = sequence_tiles(p.a, s, g.len, g.live, g.n_prefix);
+            if (t >= g.n_tiles) {  // (only a sequence without tiles)
+                t = 0;
+                h = 0;
+                if (++s == p.a.S) {
+                    s = 0;
+                    ++pass;
+                }
+                continue;
+            }
+            const int take = (int)min((long long)(g.n_tiles - t), hi - pos);
+            g.s = s;
+            g.h = h;
+            g.t0 = t;
+            g.t1 = t + take;
+            g.whole = take == g.n_tiles;
+            g.slot = first ? 0 : 1;
+            first = false;
+            g.qt = pass * p.side + (int)(blockIdx.x % p.side);
+            g.rows = min(2 * TILE, g.live * p.G - g.qt * 2 * TILE);
+            pos += take;
+            t += take;
+            if (t == g.n_tiles) {
+                t = 0;
+                if (++h == p.a.cache.heads) {
+                    h = 0;
+                    if (++s == p.a.S) {
+                        s = 0;
+                        ++pass;
+                    }
+                }
+            }
+            if (g.rows > 0 && g.qt < p.n_qtiles) return true;
+        }
+        return false;
+    }
+};
+
+// Calls f(is_v, tile) for the key and value tiles of a segment in the order in which the products consume them;
+// `lead`: streams that start side by side on different tiles (2 if they split the keys).
+template <typename F>
+__device__ __forceinline__ bool for_each_tile(const Segment& g, F&& f) {
+    const int lead = g.rows > TILE ? 1 : 2;
+    for (int j = g.t0; j < min(g.t1, g.t0 + lead); ++j)
+        if (!f(false, j)) return false;
+    for (int j = g.t0; j < g.t1; ++j) {
+        if (!f(true, j)) return false;
+        if (j + lead < g.t1 && !f(false, j + lead)) return false;
+    }
+    return true;
+}
+
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Two E4M3 codes (bytes SEL of w) times a power of two as bfloat16: the code's sign, exponent and mantissa moved into
+// a bfloat16's fields read as its value times 2^-120 (subnormals as subnormals), and `f` holds scale * 2^120.
+template <uint32_t SEL>
+__device__ __forceinline__ uint32_t e4m3x2_bf16x2(uint32_t w, uint32_t f) {
+    const uint32_t x = __byte_perm(w, 0u, SEL);
+    return mul_bf16x2((x & 0x80008000u) | ((x >> 4) & 0x07F007F0u), f);
+}
+__device__ __forceinline__ uint32_t scale_bf16x2(uint32_t exp) {
+    const uint32_t b = exp > 127u + E8_MAX ? 0x7FC0u : (exp + 120u) << 7;  // beyond the largest: NaN
+    return b | (b << 16);
+}
+__device__ __forceinline__ void st_shared16(uint32_t addr, const uint4& v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+// Where 16-byte chunk `c` of row r lies in a tile: blocks of 64 elements, rows of 128 bytes, chunks swizzled by the row.
+__device__ __forceinline__ uint32_t tile_at(int r, int c) { return (uint32_t)((c >> 3) * (TILE * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t nonfinite_to_zero(uint32_t v, bool& found) {
+    if ((v & 0x7F80u) == 0x7F80u) {
+        v &= 0xFFFF0000u;
+        found = true;
+    }
+    if ((v & 0x7F800000u) == 0x7F800000u) {
+        v &= 0x0000FFFFu;
+        found = true;
+    }
+    return v;
+}
+
+template <int D, bool Q8>
+__global__ void __launch_bounds__(ATT_THREADS, 1)
+tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttParams p) {
+    using Geo = Geometry<D, Q8>;
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    unsigned char* smem = smem_raw + (base - raw);
+    const uint32_t q_at = base, ring_at = base + 2 * Geo::TILE_BYTES, stg_at = ring_at + Geo::SLOTS * Geo::TILE_BYTES;
+    const uint32_t exp_at = base + Geo::EXP_AT;
+    float2* xch = reinterpret_cast<float2*>(smem + Geo::MISC_AT);
+    AttShared& sh = *reinterpret_cast<AttShared*>(smem + Geo::MISC_AT + 1024);
+    volatile int* abort_flag = &sh.abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const TreeAttnArgs& a = p.a;
+    const CacheArgs& cache = a.cache;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < Geo::SLOTS; ++i) {
+            mbar_init(smem_u32(&sh.full[i]), 128);
+            mbar_init(smem_u32(&sh.empty[i]), 1);
+        }
+        for (int i = 0; i < Geo::STAGES; ++i) {
+            mbar_init(smem_u32(&sh.stg_full[i]), 1);
+            mbar_init(smem_u32(&sh.stg_empty[i]), 128);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&sh.s_full[i]), 1);
+            mbar_init(smem_u32(&sh.p_full[i]), 4);
+        }
+        mbar_init(smem_u32(&sh.o_full), 1);
+        mbar_init(smem_u32(&sh.q_full), 8);
+        mbar_init(smem_u32(&sh.xch), 128);
+        for (int i = 0; i < 16; ++i) sh.nonfinite[i] = 0;
+        sh.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 13) {
+        tmem_alloc(smem_u32(&sh.tmem), 512);
+        tmem_relinquish();
+    }
+    if (warp == 12 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? &tm_v : &tm_k)) : "memory");
+    grid_dependency_wait();
+    // ---------------------------------------------------------------- this CTA's range of key tiles
+    if (warp == 0) {
+        long long sum = 0;
+        int len, live, np;
+        for (int s = lane; s < a.S; s += 32) sum += sequence_tiles(a, s, len, live, np);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const long long per_pass = sum * cache.heads, total = per_pass * p.passes;
+        const long long n_groups = groups_used(p, total), group = min((long long)(blockIdx.x / p.side), n_groups);
+        const long long lo = total ? group * total / n_groups : 0, hi = group < n_groups ? (group + 1) * total / n_groups : lo;
+        const int pass = per_pass ? (int)(lo / per_pass) : 0;
+        const long long x = lo - pass * per_pass;  // < per_pass
+        if (lane == 0) {
+            sh.lo = lo;
+            sh.hi = hi;
+            sh.pass = pass;
+            sh.s = 0;
+            sh.h = 0;
+            sh.t = 0;
+        }
+        __syncwarp();
+        long long before = 0;
+        for (int s0 = 0; s0 < a.S; s0 += 32) {
+            const int s = s0 + lane;
+            const int n = s < a.S ? sequence_tiles(a, s, len, live, np) : 0;
+            long long upto = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long other = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += other;
+            }
+            upto += before;
+            if (blockIdx.x == 0 && s < a.S) {
+                p.cum[s + 1] = upto;
+                if (s == 0) p.cum[0] = 0;
+                if (a.len[s] < 0 || (long long)a.len[s] > ((long long)cache.max_pages << cache.page_shift)) atomicOr(a.status, SPEC_STATUS_CAPACITY);
+            }
+            const long long from = (upto - n) * cache.heads;
+            if (n > 0 && lo < hi && x >= from && x < upto * cache.heads) {
+                sh.s = s;
+                sh.h = (int)((x - from) / n);
+                sh.t = (int)((x - from) % n);
+            }
+            before = __shfl_sync(0xffffffffu, upto, 31);
+            if (blockIdx.x != 0 && before * cache.heads > x) break;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (threadIdx.x == 0) grid_launch_dependents();
+    const uint32_t tmem = sh.tmem;
+    const uint32_t full = smem_u32(&sh.full[0]), empty = smem_u32(&sh.empty[0]), stg_full = smem_u32(&sh.stg_full[0]), stg_empty = smem_u32(&sh.stg_empty[0]);
+    const uint32_t s_full = smem_u32(&sh.s_full[0]), p_full = smem_u32(&sh.p_full[0]), o_full = smem_u32(&sh.o_full), q_full = smem_u32(&sh.q_full);
+    const uint32_t xch_bar = smem_u32(&sh.xch);
+    auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, p.wait_limit_ns); };
+    Segment g;
+    SegmentIter it(sh);
+
+    if (warp < 8) {
+        // ------------------------------------------------------------------------------------ softmax
+        // (a warp gives up as a whole: what follows a wait is collective)
+        auto warp_wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+        set_regs_up<REGS_SOFTMAX>();
+        const int stream = warp >> 2, wq = warp & 3;
+        const uint32_t lanes = tmem + ((uint32_t)(wq * 32) << 16);
+        const uint32_t s_tm = lanes + stream * TILE, o_tm = lanes + 2 * TILE + stream * TILE;
+        uint32_t n_s = 0, n_seg = 0, n_xch = 0;  // tiles of this stream, segments, exchanges so far
+        bool ok = true;
+        while (ok && it.next(p, g)) {
+            const bool split = g.rows <= TILE;  // the streams split the keys
+            const int tile_row = (split ? 0 : stream * TILE) + wq * 32 + lane;
+            const bool valid = tile_row < g.rows;
+            const int R = g.qt * 2 * TILE + tile_row, node = R / p.G, gq = R - node * p.G;
+            const bool warp_on = (split ? 0 : stream * TILE) + wq * 32 < g.rows;
+            // ---- queries into shared memory (once: by stream 0 if both read the same rows)
+            if (!split || stream == 0) {
+                constexpr int LPR = D / 8, RPI = 32 / LPR;  // lanes per row, rows per instruction
+                const long long off = valid ? ((long long)g.s * a.N + node) * a.q_tok + (long long)(g.h * p.G + gq) * a.q_head : -1;
+                const uint32_t dst = q_at + stream * Geo::TILE_BYTES;
+                const int c = lane % LPR;
+#pragma unroll 8
+                for (int i = 0; i < LPR; ++i) {
+                    const int r = i * RPI + lane / LPR;
+                    const long long o = __shfl_sync(0xffffffffu, off, r);
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (o >= 0) v = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + c * 8);
+                    st_shared16(dst + tile_at(wq * 32 + r, c), v);
+                }
+                fence_async_smem();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full);
+            // ---- key tiles
+            float m = -INFINITY, l = 0.0f;
+            const int step = split ? 2 : 1;
+            for (int t = g.t0 + (split ? stream : 0); t < g.t1; t += step) {
+                if (!(ok = warp_wait(s_full + 8 * stream, n_s & 1u))) break;
+                ++n_s;
+                tc_fence_after();
+                if (warp_on) {
+                    uint32_t r[4][32];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) tmem_ld32(s_tm + 32 * i, r[i]);
+                    tmem_wait_ld();
+                    const int valid_keys = t < g.n_prefix ? g.len - t * TILE : g.live - (t - g.n_prefix) * TILE;
+                    if (t >= g.n_prefix || valid_keys < TILE) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int left = valid_keys - 32 * i;
+                            w[i] = left >= 32 ? 0xFFFFFFFFu : (left <= 0 ? 0u : (1u << left) - 1u);
+                            if (t >= g.n_prefix) {
+                                const int words = (a.N + 31) / 32, at = (t - g.n_prefix) * 4 + i;
+                                w[i] &= (valid && at < words) ? (uint32_t)a.mask[((long long)g.s * a.N + node) * words + at] : 0u;
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (!((w[i] >> j) & 1u)) r[i][j] = 0xFF800000u;
+                    }
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) top = fmaxf(top, fmaxf(__uint_as_float(r[i][j]), __uint_as_float(r[i][j + 1])));
+                    const bool first = t < g.t0 + step;
+                    if (first) {
+                        m = top;
+                    } else {
+                        const bool move = (top - m) * p.c > RESCALE;  // (m = -inf: the row has had no key yet)
+                        if (__any_sync(0xffffffffu, move)) {
+                            const float f = move ? exp2_approx((m - top) * p.c) : 1.0f;
+                            if (move) m = top;
+                            l *= f;
+#pragma unroll 1
+                            for (int i = 0; i < D / 32; ++i) {
+                                uint32_t o[32];
+                                tmem_ld32(o_tm + 32 * i, o);
+                                tmem_wait_ld();
+                                uint32_t lo[16], hi[16];
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) {
+                                    lo[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                    hi[j] = __float_as_uint(__uint_as_float(o[j + 16]) * f);
+                                }
+                                tmem_st16(o_tm + 32 * i, lo);
+                                tmem_st16(o_tm + 32 * i + 16, hi);
+                            }
+                        }
+                    }
+                    const float mc = m == -INFINITY ? 0.0f : m * p.c;
+                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const float x = exp2_approx(fmaf(__uint_as_float(r[i][2 * j]), p.c, -mc));
+                            const float y = exp2_approx(fmaf(__uint_as_float(r[i][2 * j + 1]), p.c, -mc));
+                            sum[(2 * j) & 3] += x;
+                            sum[(2 * j + 1) & 3] += y;
+                            w[j] = pack2(x, y);
+                        }
+                        tmem_st16(s_tm + 16 * i, w);
+                    }
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    tmem_wait_st();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full + 8 * stream);
+            }
+            if (!ok) break;
+            // ---- results
+            if (!(ok = warp_wait(o_full, n_seg & 1u))) break;
+            tc_fence_after();
+            float f0 = 1.0f, f1 = 0.0f;
+            const bool both = split && g.t1 - g.t0 > 1;  // stream 1 had a tile
+            if (both) {
+                if (stream == 1) {
+                    xch[wq * 32 + lane] = make_float2(m, l);
+                    mbar_arrive(xch_bar);
+                } else {
+                    if (!(ok = warp_wait(xch_bar, n_xch & 1u))) break;
+                    const float2 other = xch[wq * 32 + lane];
+                    const float top = fmaxf(m, other.x);
+                    f0 = m == -INFINITY ? 0.0f : exp2_approx((m - top) * p.c);
+                    f1 = other.x == -INFINITY ? 0.0f : exp2_approx((other.x - top) * p.c);
+                    l = l * f0 + other.y * f1;
+                    m = top;
+                }
+                ++n_xch;
+            }
+            if ((!split || stream == 0) && warp_on) {
+                const bool poisoned = sh.nonfinite[n_seg & 15u] == (int)n_seg + 1;
+                const float inv = g.whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
+                const long long out_row = ((long long)g.s * a.N + node) * a.Hq + g.h * p.G + gq;
+                const long long part = ((long long)blockIdx.x * 2 + g.slot) * p.rows_cap + tile_row;
+#pragma unroll 1
+                for (int i = 0; i < D / 32; ++i) {
+                    uint32_t o[32];
+                    float x[32];
+                    tmem_ld32(o_tm + 32 * i, o);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(o[j]) * f0;
+                    if (both) {
+                        tmem_ld32(o_tm + TILE + 32 * i, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) x[j] += __uint_as_float(o[j]) * f1;
+                    }
+                    if (poisoned && valid) {
+                        // values of the block that are not finite were taken as 0 in the products, where a weight of 0
+                        // would have made them NaN; rows that do attend to them get them here
+                        const int words = (a.N + 31) / 32;
+                        const int from = max(g.t0 - g.n_prefix, 0) * TILE, to = min((g.t1 - g.n_prefix) * TILE, g.live);
+                        for (int n = from; n < to; ++n) {
+                            if (!((a.mask[((long long)g.s * a.N + node) * words + (n >> 5)] >> (n & 31)) & 1)) continue;
+                            const __nv_bfloat16* v = (const __nv_bfloat16*)a.v + ((long long)g.s * a.N + n) * a.v_tok + (long long)g.h * a.v_head + 32 * i;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                const float y = __bfloat162float(v[j]);
+                                if (!isfinite(y)) x[j] += y;
+                            }
+                        }
+                    }
+                    if (valid) {
+                        if (g.whole) {
+                            uint4* dst = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + out_row * D + 32 * i);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                dst[j] = make_uint4(pack2(x[8 * j] * inv, x[8 * j + 1] * inv), pack2(x[8 * j + 2] * inv, x[8 * j + 3] * inv),
+                                                    pack2(x[8 * j + 4] * inv, x[8 * j + 5] * inv), pack2(x[8 * j + 6] * inv, x[8 * j + 7] * inv));
+                        } else {
+                            float4* dst = reinterpret_cast<float4*>(p.part_o + part * D + 32 * i);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) dst[j] = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+                        }
+                    }
+                }
+                if (valid) {
+                    if (!g.whole) p.part_ml[part] = make_float2(m, l);
+                    else if (a.lse) a.lse[out_row] = l == 0.0f ? -INFINITY : (m * p.c + log2f(l)) * LN2;
+                }
+            }
+            tc_fence_before();
+            ++n_seg;
+        }
+    } else if (warp < 12) {
+        // ------------------------------------------------------------------------------------ tiles written by threads
+        set_regs_down<REGS_LOADER>();
+        const int tid = threadIdx.x - 256;
+        constexpr int CH = D / 8;  // 16-byte chunks of a bf16 vector
+        uint32_t slot = 0, phase = 0, stg = 0, stg_phase = 0, n_seg = 0;
+        while (it.next(p, g)) {
+            const bool ok = for_each_tile(g, [&](bool is_v, int t) {
+                const bool block = t >= g.n_prefix;
+                const uint32_t dst = ring_at + slot * Geo::TILE_BYTES, bar_full = full + 8 * slot, bar_empty = empty + 8 * slot;
+                const uint32_t my_phase = phase;
+                if (++slot == Geo::SLOTS) {
+                    slot = 0;
+                    phase ^= 1u;
+                }
+                const int rows = block ? g.live - (t - g.n_prefix) * TILE : g.len - t * TILE;  // may exceed the tile
+                if (!Q8 && !block && rows >= TILE) return true;                                 // TMA's
+                if (Q8 && !block) {
+                    if (!wait(stg_full + 8 * stg, stg_phase)) return false;
+                    if (!wait(bar_empty, my_phase ^ 1u)) return false;
+                    const uint32_t src = stg_at + stg * Geo::STAGE_BYTES, ex = exp_at + stg * TILE;
+                    constexpr int LPR = D / 16;
+                    const bool swap = (tid & 4) != 0 && D == 128;  // so that the 8 lanes of a phase write to different banks
+#pragma unroll 4
+                    for (int i = 0; i < LPR; ++i) {
+                        const int r = i * (128 / LPR) + tid / LPR, c = tid % LPR;
+                        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+                        if (r < rows) {
+                            const uint4 v = ld_shared16(src + r * D + c * 16);
+                            uint32_t e;
+                            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e) : "r"(ex + r) : "memory");
+                            const uint32_t f = scale_bf16x2(e);
+                            lo = make_uint4(e4m3x2_bf16x2<0x1404>(v.x, f), e4m3x2_bf16x2<0x3424>(v.x, f), e4m3x2_bf16x2<0x1404>(v.y, f), e4m3x2_bf16x2<0x3424>(v.y, f));
+                            hi = make_uint4(e4m3x2_bf16x2<0x1404>(v.z, f), e4m3x2_bf16x2<0x3424>(v.z, f), e4m3x2_bf16x2<0x1404>(v.w, f), e4m3x2_bf16x2<0x3424>(v.w, f));
+                        }
+                        st_shared16(dst + tile_at(r, 2 * c + (swap ? 1 : 0)), swap ? hi : lo);
+                        st_shared16(dst + tile_at(r, 2 * c + (swap ? 0 : 1)), swap ? lo : hi);
+                    }
+                    mbar_arrive(stg_empty + 8 * stg);
+                    if (++stg == Geo::STAGES) {
+                        stg = 0;
+                        stg_phase ^= 1u;
+                    }
+                } else {
+                    if (!wait(bar_empty, my_phase ^ 1u)) return false;
+                    bool found = false;
+#pragma unroll 1
+                    for (int i0 = 0; i0 < CH; i0 += 8) {
+                        uint4 v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int r = (i0 + i) * (128 / CH) + tid / CH, c = tid % CH;
+                            v[i] = make_uint4(0, 0, 0, 0);
+                            if (r >= rows) continue;
+                            const __nv_bfloat16* src;
+                            if (block) {
+                                const long long tok = (long long)g.s * a.N + (t - g.n_prefix) * TILE + r;
+                                src = is_v ? (const __nv_bfloat16*)a.v + tok * a.v_tok + (long long)g.h * a.v_head
+                                           : (const __nv_bfloat16*)a.k + tok * a.k_tok + (long long)g.h * a.k_head;
+                            } else {
+                                const int pos = t * TILE + r;
+                                const int page = cache.table[(long long)g.s * cache.max_pages + (pos >> cache.page_shift)];
+                                if ((unsigned)page >= (unsigned)cache.n_pages) {
+                                    atomicOr(a.status, SPEC_STATUS_CAPACITY);
+                                    continue;
+                                }
+                                const long long at = (((long long)page * cache.heads + g.h) << cache.page_shift) + (pos & ((1 << cache.page_shift) - 1));
+                                src = (const __nv_bfloat16*)(is_v ? cache.v : cache.k) + at * D;
+                            }
+                            v[i] = *reinterpret_cast<const uint4*>(src + c * 8);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int r = (i0 + i) * (128 / CH) + tid / CH, c = tid % CH;
+                            if (block && is_v) {
+                                v[i].x = nonfinite_to_zero(v[i].x, found);
+                                v[i].y = nonfinite_to_zero(v[i].y, found);
+                                v[i].z = nonfinite_to_zero(v[i].z, found);
+                                v[i].w = nonfinite_to_zero(v[i].w, found);
+                            }
+                            st_shared16(dst + tile_at(r, c), v[i]);
+                        }
+                    }
+                    if (found) sh.nonfinite[n_seg & 15u] = (int)n_seg + 1;
+                }
+                fence_async_smem();
+                mbar_arrive(bar_full);
+                return true;
+            });
+            if (!ok) break;
+            ++n_seg;
+        }
+    } else {
+        set_regs_down<REGS_CONTROL>();
+        if (warp == 12) {
+            // -------------------------------------------------------------------------------- TMA
+            // A lane fetches one page's part of a tile; page numbers are read a tile ahead.
+            uint32_t slot = 0, phase = 0, issued = 0;
+            constexpr uint32_t RING = Q8 ? Geo::STAGES : Geo::SLOTS;
+            const int page = 1 << cache.page_shift, per_tile = TILE >> cache.page_shift;
+            const int all_rows = (cache.n_pages * cache.heads) << cache.page_shift;  // a coordinate beyond the cache: reads as 0
+            bool ok = true;
+            while (ok && it.next(p, g)) {
+                const int32_t* table = cache.table + (long long)g.s * cache.max_pages;
+                const int n_pages = (g.len + page - 1) >> cache.page_shift;
+                // (the pages of a tile's K serve its V one or two tiles later: kept in two registers, by the tile's parity)
+                auto fetch = [&](int t) {
+                    const int i = t * per_tile + lane;
+                    return lane < per_tile && i < n_pages && t < g.n_prefix ? table[i] : 0;
+                };
+                int pg[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pg[i] = fetch(g.t0 + i);  // pg[i]: tile t0 + i (mod 4)
+                ok = for_each_tile(g, [&](bool is_v, int t) {
+                    const bool block = t >= g.n_prefix;
+                    const int rows = block ? 0 : g.len - t * TILE;
+                    const bool mine = Q8 ? !block : rows >= TILE;
+                    const uint32_t bar_full = (Q8 ? stg_full : full) + 8 * slot, bar_empty = (Q8 ? stg_empty : empty) + 8 * slot;
+                    const uint32_t dst = Q8 ? stg_at + slot * Geo::STAGE_BYTES : ring_at + slot * Geo::TILE_BYTES;
+                    const uint32_t ex = exp_at + slot * TILE;
+                    const uint32_t my_phase = phase;
+                    if (mine || !Q8) {
+                        if (++slot == RING) {
+                            slot = 0;
+                            phase ^= 1u;
+                        }
+                    }
+                    const int k4 = (t - g.t0) & 3;
+                    const int pid = k4 == 0 ? pg[0] : (k4 == 1 ? pg[1] : (k4 == 2 ? pg[2] : pg[3]));
+                    if (is_v) {  // the tile's last use of its page numbers
+                        const int ahead = fetch(t + 4);
+                        if (k4 == 0) pg[0] = ahead;
+                        else if (k4 == 1) pg[1] = ahead;
+                        else if (k4 == 2) pg[2] = ahead;
+                        else pg[3] = ahead;
+                    }
+                    if (!mine) return true;
+                    const bool got = wait(bar_empty, my_phase ^ 1u);
+                    if (!__all_sync(0xffffffffu, got)) return false;
+                    const int pages = min((rows + page - 1) >> cache.page_shift, per_tile);
+                    if (lane == 0) {
+                        mbar_expect_tx(bar_full, (uint32_t)(pages * page) * (Q8 ? D + 1 : 2 * D));
+                        if (!Q8) mbar_arrive_n(bar_full, 127);
+                    }
+                    __syncwarp();
+                    if (lane < pages) {
+                        const bool good = (unsigned)pid < (unsigned)cache.n_pages;
+                        if (!good) atomicOr(a.status, SPEC_STATUS_CAPACITY);
+                        const int row = good ? (pid * cache.heads + g.h) << cache.page_shift : all_rows;
+                        const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
+                        if (Q8) {
+                            tma_load_2d(dst + lane * page * D, tm, 0, row, bar_full);
+                            bulk_load(ex + lane * page, (is_v ? cache.v_exp : cache.k_exp) + (good ? row : 0), page, bar_full);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < Geo::HALVES; ++i) tma_load_2d(dst + i * (TILE * 128) + lane * page * 128, tm, 64 * i, row, bar_full);
+                        }
+                    }
+                    ++issued;
+                    return true;
+                });
+            }
+            if (!ok && lane == 0) {  // give copies in flight a bounded chance to land before the CTA exits
+                const uint64_t until = global_timer_ns() + 1000000ull;
+                while (issued && global_timer_ns() < until) {}
+            }
+        } else if (warp == 13 && lane == 0) {
+            // -------------------------------------------------------------------------------- products
+            const uint32_t id_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
+            const uint32_t id_pv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
+            uint32_t slot = 0, phase = 0, n_seg = 0, n_p[2] = {0, 0};
+            bool ok = true;
+            auto take = [&](uint32_t& at, uint32_t& index) {  // the next tile of the ring, once it is there
+                index = slot;
+                at = ring_at + slot * Geo::TILE_BYTES;
+                const bool got = wait(full + 8 * slot, phase);
+                if (++slot == Geo::SLOTS) {
+                    slot = 0;
+                    phase ^= 1u;
+                }
+                tc_fence_after();
+                return got;
+            };
+            auto qk = [&](int stream, int q_tile, uint32_t k_at) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t o = (uint32_t)((k >> 2) * (TILE * 128) + (k & 3) * 32);
+                    tc_mma_bf16(tmem + stream * TILE, make_kmajor_sw128_desc(q_at + q_tile * Geo::TILE_BYTES + o), make_kmajor_sw128_desc(k_at + o), id_qk, k != 0);
+                }
+                tc_commit(s_full + 8 * stream);
+            };
+            auto pv = [&](int stream, uint32_t v_at, bool add) {
+#pragma unroll
+                for (int k = 0; k < TILE / 16; ++k)
+                    tc_mma_bf16_ts(tmem + 2 * TILE + stream * TILE, tmem + stream * TILE + 8 * k, make_mnmajor_sw128_desc(v_at + k * 2048, TILE * 128), id_pv,
+                                   (add || k != 0) ? 1u : 0u);
+            };
+            while (ok && it.next(p, g)) {
+                const int n = g.t1 - g.t0;
+                uint32_t k_at, v_at, ki, vi;
+                if (!(ok = wait(q_full, n_seg & 1u))) break;
+                tc_fence_after();
+                if (g.rows > TILE) {  // two row tiles, the same keys
+                    if (!(ok = take(k_at, ki))) break;
+                    qk(0, 0, k_at);
+                    qk(1, 1, k_at);
+                    tc_commit(empty + 8 * ki);
+                    for (int t = 0; t < n && ok; ++t) {
+                        if (!(ok = take(v_at, vi))) break;
+                        if (!(ok = wait(p_full, n_p[0]++ & 1u))) break;
+                        tc_fence_after();
+                        pv(0, v_at, t > 0);
+                        if (t + 1 < n) {
+                            if (!(ok = take(k_at, ki))) break;
+                            qk(0, 0, k_at);
+                        }
+                        if (!(ok = wait(p_full + 8, n_p[1]++ & 1u))) break;
+                        tc_fence_after();
+                        pv(1, v_at, t > 0);
+                        tc_commit(empty + 8 * vi);
+                        if (t + 1 < n) {
+                            qk(1, 1, k_at);
+                            tc_commit(empty + 8 * ki);
+                        }
+                    }
+                } else {  // one row tile, alternate keys
+                    for (int t = 0; t < 2 && t < n && ok; ++t) {
+                        if (!(ok = take(k_at, ki))) break;
+                        qk(t, 0, k_at);
+                        tc_commit(empty + 8 * ki);
+                    }
+                    for (int t = 0; t < n && ok; ++t) {
+                        const int i = t & 1;
+                        if (!(ok = take(v_at, vi))) break;
+                        if (!(ok = wait(p_full + 8 * i, n_p[i]++ & 1u))) break;
+                        tc_fence_after();
+                        pv(i, v_at, t > 1);
+                        tc_commit(empty + 8 * vi);
+                        if (t + 2 < n) {
+                            if (!(ok = take(k_at, ki))) break;
+                            qk(i, 0, k_at);
+                            tc_commit(empty + 8 * ki);
+                        }
+                    }
+                }
+                if (!ok) break;
+                tc_commit(o_full);
+                ++n_seg;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && *abort_flag) atomicOr(a.status, SPEC_STATUS_TIMEOUT);
+    if (warp == 13) tmem_dealloc(tmem, 512);
+}
+
+// Joins the partial rows of every (s, h, row-tile pair) whose key tiles were spread over several CTAs, in the CTAs'
+// order, and writes the rows that attend to nothing.  A warp per row; 32 rows per CTA.
+template <int D>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ AttParams p) {
+    constexpr int E = D / 32;
+    const TreeAttnArgs& a = p.a;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int s = (int)(blockIdx.x / a.cache.heads), h = (int)(blockIdx.x % a.cache.heads), qt = blockIdx.y;
+    int len, live, np;
+    const int tiles = sequence_tiles(a, s, len, live, np);
+    const long long per_pass = p.cum[a.S] * a.cache.heads, total = per_pass * p.passes;
+    const long long u0 = (qt / p.side) * per_pass + p.cum[s] * a.cache.heads + (long long)h * tiles, u1 = u0 + tiles;
+    const long long n_groups = groups_used(p, total);
+    auto group_of = [&](long long x) { return ((x + 1) * n_groups + total - 1) / total - 1; };  // the group whose range holds tile x
+    long long g0 = 0, g1 = 0;
+    if (tiles) {
+        g0 = group_of(u0);
+        g1 = group_of(u1 - 1);
+    }
+    const int rows = min(2 * TILE, a.N * p.G - qt * 2 * TILE), used = min(2 * TILE, live * p.G - qt * 2 * TILE);
+    if (g0 == g1 && used >= rows) return;
+    for (int r = blockIdx.z * 32 + warp; r < min(rows, (int)blockIdx.z * 32 + 32); r += 8) {
+        const int R = qt * 2 * TILE + r, node = R / p.G, gq = R - node * p.G;
+        const long long out_row = ((long long)s * a.N + node) * a.Hq + h * p.G + gq;
+        __nv_bfloat16* out = (__nv_bfloat16*)a.out + out_row * D + lane * E;
+        if (r >= used) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) out[j] = __float2bfloat16_rn(0.0f);
+            if (a.lse && lane == 0) a.lse[out_row] = -INFINITY;
+            continue;
+        }
+        if (g0 == g1) continue;
+        auto part_of = [&](long long gi) {
+            const int slot = u0 > gi * total / n_groups ? 1 : 0;
+            return (((gi * p.side + qt % p.side) * 2 + slot) * p.rows_cap) + r;
+        };
+        float m = -INFINITY;
+        for (long long gi = g0 + lane; gi <= g1; gi += 32) m = fmaxf(m, p.part_ml[part_of(gi)].x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        float l = 0.0f, x[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) x[j] = 0.0f;
+#pragma unroll 4
+        for (long long gi = g0; gi <= g1; ++gi) {
+            const long long at = part_of(gi);
+            const float2 ml = p.part_ml[at];
+            const float f = ml.x == -INFINITY ? 0.0f : exp2f((ml.x - m) * p.c);
+            const float* o = p.part_o + at * D + lane * E;
+            l += ml.y * f;
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[j] += o[j] * f;
+        }
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+        for (int j = 0; j < E; ++j) out[j] = __float2bfloat16_rn(x[j] * inv);
+        if (a.lse && lane == 0) a.lse[out_row] = l == 0.0f ? -INFINITY : (m * p.c + log2f(l)) * LN2;
+    }
+}
+
+// ------------------------------------------------------------------------------------------ host
+static void plan(int num_sms, int S, int N, int Hq, int heads, int head_dim, AttParams& p, size_t& bytes) {
+    p.G = Hq / heads;
+    const int rows = N * p.G;
+    p.n_qtiles = (rows + 2 * TILE - 1) / (2 * TILE);
+    p.side = std::min(p.n_qtiles, num_sms);
+    p.n_groups = num_sms / p.side;
+    p.passes = (p.n_qtiles + p.side - 1) / p.side;
+    p.rows_cap = std::min(2 * TILE, rows);
+    const size_t parts = (size_t)p.n_groups * p.side * 2 * p.rows_cap;
+    const size_t cum = ((size_t)S + 2) / 2 * 16;
+    p.cum = nullptr;
+    p.part_o = reinterpret_cast<float*>(cum);
+    p.part_ml = reinterpret_cast<float2*>(cum + parts * head_dim * 4);
+    bytes = cum + parts * (head_dim * 4 + 8);
+}
+
+size_t tree_attention_bytes(int num_sms, int S, int N, int Hq, int heads, int head_dim) {
+    AttParams p;
+    size_t bytes;
+    plan(num_sms, S, N, Hq, heads, head_dim, p, bytes);
+    return bytes;
+}
+
+// The cache as rows of one vector: [n_pages * heads * page, D], a page and 128 bytes (E4M3: a whole vector) at a time.
+static int cache_map(spec_ctx* ctx, CUtensorMap* tm, const void* base, const CacheArgs& c) {
+    const int elem = c.quantised ? 1 : 2;
+    cuuint64_t dims[2] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.n_pages * c.heads << c.page_shift};
+    cuuint64_t strides[1] = {(cuuint64_t)c.head_dim * elem};
+    cuuint32_t box[2] = {(cuuint32_t)(c.quantised ? c.head_dim : 64), 1u << c.page_shift};
+    cuuint32_t estr[2] = {1u, 1u};
+    CUresult r = ctx->encode(tm, c.quantised ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
+                             strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, c.quantised ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(ctx, SPEC_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+    return SPEC_OK;
+}
+
+template <int D, bool Q8>
+static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
+    auto kernel = tree_attention_kernel<D, Q8>;
+    {
+        static bool done[64] = {false};
+        std::lock_guard<std::mutex> lock(host_mutex());
+        bool& d = done[ctx->device & 63];
+        if (!d) {
+            cudaFuncAttributes attr;
+            int rc = check_cuda(ctx, cudaFuncGetAttributes(&attr, kernel), "spec_tree_attention: cudaFuncGetAttributes");
+            if (rc) return rc;
+            if (attr.numRegs * ATT_THREADS < 128 * (2 * REGS_SOFTMAX + REGS_LOADER + REGS_CONTROL))  // the warpgroups would wait for registers for ever
+                return fail(ctx, SPEC_ERR_UNSUPPORTED, "spec_tree_attention: built with %d registers per thread", attr.numRegs);
+            if ((rc = check_cuda(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Geometry<D, Q8>::SMEM),
+                                 "spec_tree_attention: cudaFuncSetAttribute")))
+                return rc;
+            d = true;
+        }
+    }
+    CUtensorMap tm_k, tm_v;
+    int rc = cache_map(ctx, &tm_k, p.a.cache.k, p.a.cache);
+    if (rc || (rc = cache_map(ctx, &tm_v, p.a.cache.v, p.a.cache))) return rc;
+    cudaError_t e = launch_pdl(kernel, dim3(p.n_groups * p.side), dim3(ATT_THREADS), (size_t)Geometry<D, Q8>::SMEM, st, tm_k, tm_v, p);
+    if ((rc = check_cuda(ctx, e, "spec_tree_attention launch"))) return rc;
+    e = launch_pdl(join_kernel<D>, dim3(p.a.S * p.a.cache.heads, p.n_qtiles, (p.rows_cap + 31) / 32), dim3(256), 0, st, p);
+    ctx->launches += 2;
+    return check_cuda(ctx, e, "spec_tree_attention join launch");
+}
 
 int launch_tree_attention(spec_ctx* ctx, const TreeAttnArgs& a, cudaStream_t st) {
-    const long long rows = (long long)a.S * a.N * a.Hq;
-    const dim3 grid((unsigned)((rows + 3) / 4));
-    auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(128), 0, st, a); };
-    cudaError_t e;
-    if (a.cache.quantised) e = a.cache.head_dim == 64 ? go(tree_attention_plain_kernel<64, true>) : go(tree_attention_plain_kernel<128, true>);
-    else e = a.cache.head_dim == 64 ? go(tree_attention_plain_kernel<64, false>) : go(tree_attention_plain_kernel<128, false>);
-    ctx->launches += 1;
-    return check_cuda(ctx, e, "spec_tree_attention launch");
+    AttParams p;
+    size_t bytes;
+    plan(ctx->num_sms, a.S, a.N, a.Hq, a.cache.heads, a.cache.head_dim, p, bytes);
+    p.a = a;
+    p.c = a.scale * LOG2E;
+    p.cum = reinterpret_cast<long long*>(a.work);
+    p.part_o = reinterpret_cast<float*>((char*)a.work + (size_t)p.part_o);
+    p.part_ml = reinterpret_cast<float2*>((char*)a.work + (size_t)p.part_ml);
+    p.wait_limit_ns = WAIT_LIMIT_NS;
+    if (a.cache.quantised) return a.cache.head_dim == 64 ? launch<64, true>(ctx, p, st) : launch<128, true>(ctx, p, st);
+    return a.cache.head_dim == 64 ? launch<64, false>(ctx, p, st) : launch<128, false>(ctx, p, st);
 }
 
 }  // namespace ngs
