@@ -64,7 +64,7 @@ struct Geometry {
 };
 
 struct AttShared {  // after the 1024 bytes of the (m, l) exchange
-    uint64_t full[8], empty[8], stg_full[6], stg_empty[6], s_full[2], p_full[2], o_full, q_full, xch;
+    uint64_t full[8], empty[8], go[8], stg_full[6], stg_empty[6], s_full[2], p_full[2], o_full, q_full, xch;
     long long lo, hi, total;
     int s, h, t, pass;
     int nonfinite[16];
@@ -216,6 +216,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         for (int i = 0; i < Geo::SLOTS; ++i) {
             mbar_init(smem_u32(&sh.full[i]), 128);
             mbar_init(smem_u32(&sh.empty[i]), 1);
+            mbar_init(smem_u32(&sh.go[i]), 1);
         }
         for (int i = 0; i < Geo::STAGES; ++i) {
             mbar_init(smem_u32(&sh.stg_full[i]), 1);
@@ -290,7 +291,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     tc_fence_after();
     if (threadIdx.x == 0) grid_launch_dependents();
     const uint32_t tmem = sh.tmem;
-    const uint32_t full = smem_u32(&sh.full[0]), empty = smem_u32(&sh.empty[0]), stg_full = smem_u32(&sh.stg_full[0]), stg_empty = smem_u32(&sh.stg_empty[0]);
+    const uint32_t full = smem_u32(&sh.full[0]), empty = smem_u32(&sh.empty[0]), go = smem_u32(&sh.go[0]), stg_full = smem_u32(&sh.stg_full[0]), stg_empty = smem_u32(&sh.stg_empty[0]);
     const uint32_t s_full = smem_u32(&sh.s_full[0]), p_full = smem_u32(&sh.p_full[0]), o_full = smem_u32(&sh.o_full), q_full = smem_u32(&sh.q_full);
     const uint32_t xch_bar = smem_u32(&sh.xch);
     auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, p.wait_limit_ns); };
@@ -496,11 +497,12 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         const int tid = threadIdx.x - 256;
         constexpr int CH = D / 8;  // 16-byte chunks of a bf16 vector
         uint32_t slot = 0, phase = 0, stg = 0, stg_phase = 0, n_seg = 0;
+        uint32_t go_phase = 0;  // bit per slot
         while (it.next(p, g)) {
             const bool ok = for_each_tile(g, [&](bool is_v, int t) {
                 const bool block = t >= g.n_prefix;
                 const uint32_t dst = ring_at + slot * Geo::TILE_BYTES, bar_full = full + 8 * slot, bar_empty = empty + 8 * slot;
-                const uint32_t my_phase = phase;
+                const uint32_t my_phase = phase, my_slot = slot;
                 if (++slot == Geo::SLOTS) {
                     slot = 0;
                     phase ^= 1u;
@@ -534,7 +536,15 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                         stg_phase ^= 1u;
                     }
                 } else {
-                    if (!wait(bar_empty, my_phase ^ 1u)) return false;
+                    // A barrier's parity tells one use of a slot from the next, not from the one after.  E4M3: these
+                    // threads fill every slot and so wait for each.  bfloat16: they skip TMA's, which would let them get
+                    // more than one use ahead or behind; the TMA warp waits for every slot and hands this one over.
+                    if (Q8) {
+                        if (!wait(bar_empty, my_phase ^ 1u)) return false;
+                    } else {
+                        if (!wait(go + 8 * my_slot, (go_phase >> my_slot) & 1u)) return false;
+                        go_phase ^= 1u << my_slot;
+                    }
                     bool found = false;
 #pragma unroll 1
                     for (int i0 = 0; i0 < CH; i0 += 8) {
@@ -609,7 +619,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     const bool mine = Q8 ? !block : rows >= TILE;
                     const uint32_t bar_full = (Q8 ? stg_full : full) + 8 * slot, bar_empty = (Q8 ? stg_empty : empty) + 8 * slot;
                     const uint32_t dst = Q8 ? stg_at + slot * Geo::STAGE_BYTES : ring_at + slot * Geo::TILE_BYTES;
-                    const uint32_t ex = exp_at + slot * TILE;
+                    const uint32_t ex = exp_at + slot * TILE, bar_go = go + 8 * slot;
                     const uint32_t my_phase = phase;
                     if (mine || !Q8) {
                         if (++slot == RING) {
@@ -626,9 +636,13 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                         else if (k4 == 2) pg[2] = ahead;
                         else pg[3] = ahead;
                     }
-                    if (!mine) return true;
+                    if (Q8 && !mine) return true;
                     const bool got = wait(bar_empty, my_phase ^ 1u);
                     if (!__all_sync(0xffffffffu, got)) return false;
+                    if (!mine) {
+                        if (lane == 0) mbar_arrive(bar_go);
+                        return true;
+                    }
                     const int pages = min((rows + page - 1) >> cache.page_shift, per_tile);
                     if (lane == 0) {
                         mbar_expect_tx(bar_full, (uint32_t)(pages * page) * (Q8 ? D + 1 : 2 * D));

@@ -102,10 +102,12 @@ def pack(mask):
 
 def attention(q, k, v, held_k, held_v, mask, lens, scale, live=None):
     """out, lse and sum p |v| in 64 bits.  What a row does not attend to is left out, not multiplied by zero."""
+    held_k, held_v, mask = held_k.cuda(), held_v.cuda(), mask.cuda()
     S, N, Hq, D = q.shape
     G = Hq // k.shape[2]
     out, lse, mag = torch.zeros(S, N, Hq, D, dtype=torch.float64), torch.full((S, N, Hq), -math.inf, dtype=torch.float64), torch.zeros(S, N, Hq, D, dtype=torch.float64)
-    q, k, v = (x.double().cpu() for x in (q, k, v))
+    q, k, v = (x.double().cuda() for x in (q, k, v))
+    out, lse, mag = out.cuda(), lse.cuda(), mag.cuda()
     for s in range(S):
         n = int(lens[s])
         for i in range(N if live is None else int(live[s])):
@@ -121,7 +123,7 @@ def attention(q, k, v, held_k, held_v, mask, lens, scale, live=None):
             p = torch.exp(z - lse[s, i][:, None])
             out[s, i] = torch.einsum("hk,khd->hd", p, vv)
             mag[s, i] = torch.einsum("hk,khd->hd", p, vv.abs())
-    return out, lse, mag
+    return out.cpu(), lse.cpu(), mag.cpu()
 
 
 def check_attention(got, ref, score_bound):

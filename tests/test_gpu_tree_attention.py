@@ -94,6 +94,19 @@ def test_long_context_is_split_and_joined(ctx, quantised, N, Hq, Hkv):
     run(ctx, 1, N, Hq, Hkv, 128, [6000 + N], 128, quantised, seed=N)
 
 
+@pytest.mark.parametrize("quantised", [False, True])
+@pytest.mark.parametrize("D,N,Hq,Hkv", [(128, 2, 16, 8), (64, 3, 8, 8), (128, 150, 8, 4)])
+def test_many_tiles_per_cta(ctx, quantised, D, N, Hq, Hkv):
+    """Some thousand key tiles: every CTA walks several heads and sequences, rings wrap around, contexts end on and off
+    tile borders."""
+    g = torch.Generator().manual_seed(N)
+    S = 40 if N < 100 else 12
+    lens = torch.randint(0, 2500, (S,), generator=g)
+    lens[::3] = lens[::3] // 128 * 128
+    lens[1::7] = lens[1::7] % 300
+    run(ctx, S, N, Hq, Hkv, D, lens.tolist(), 64, quantised, seed=N, kind="rows")
+
+
 def test_strided_projections(ctx):
     run(ctx, 2, 20, 6, 3, 64, [40, 140], 16, False, strided=True)
 
