@@ -7,8 +7,9 @@
 // and o = O / l at the end.  Both products run on the tensor cores (tcgen05, bf16 x bf16 -> fp32): S and O live in tensor
 // memory, P goes back into tensor memory as bfloat16 (over S, which has been read by then) and is the A operand of
 // P V from there, so that no intermediate touches shared memory.  P is at most 2^8 and keeps 8 bits; its row sum is
-// taken before the rounding.  The running maximum only moves when it is exceeded by more than 2^8, so the
-// read-modify-write of O that a new maximum costs happens in the first tiles and hardly ever after.
+// taken before the rounding.  m need not be the maximum itself: it is a score of the row
+// that stays the reference until weights grow beyond 2^8, so that the read-modify-write of O that a new reference costs
+// happens in the first tiles and hardly ever after.
 //
 // Two streams per CTA hide the softmax of one tile behind the products of another.  With more than 128 rows they are
 // two row tiles against the same keys; with at most 128 they are the even and the odd tiles of keys against the same
@@ -19,25 +20,28 @@
 // an (s, h) leaves fp32 partial rows and their (m, l), which a second kernel joins in a fixed order.  Any mixture of
 // lengths thus occupies all SMs to within a tile, and nothing about the lengths is needed on the host.
 //
-// Warps (512 threads): 0-3 and 4-7 softmax of stream 0 and 1 (a thread owns a row); 8-11 write key and value tiles that
-// TMA cannot (the last tile of a context, zero-padded; the block's own; an E4M3 cache's, as bfloat16 code * scale, which
-// is exact); 12 TMA; 13 issues the products.
+// Warps (640 threads, which share the registers unevenly): 0-3 and 4-7 softmax of stream 0 and 1 (a thread owns a row); 8-15 write key
+// and value tiles that TMA cannot (the last tile of a context, zero-padded; the block's own; an E4M3 cache's, as bfloat16
+// code * scale, which is exact); 16 TMA; 17 issues the products.
 #include <cuda_bf16.h>
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.cuh"
 #include "tc100.cuh"
 
 namespace ngs {
 
-constexpr int ATT_THREADS = 512;
+constexpr int SOFTMAX_WARPS = 8, LOADER_WARPS = 8, LOADERS = 32 * LOADER_WARPS, TMA_WARP = 16, MMA_WARP = 17;
+constexpr int ATT_THREADS = 640;  // whole warpgroups, which is what registers are moved between
+constexpr int LAUNCH_REGS = 96;   // per thread at launch: 65536 / 640, rounded down to a multiple of 8
+constexpr int REGS_SOFTMAX = 112, REGS_LOADER = 80, REGS_CONTROL = 96;
+static_assert(128 * (2 * REGS_SOFTMAX + 2 * REGS_LOADER + REGS_CONTROL) <= ATT_THREADS * LAUNCH_REGS, "the warpgroups' shares exceed the launch's registers");
 constexpr int TILE = 128;  // keys of a tile and rows of a row tile
 constexpr int ATT_SMEM = 227 * 1024;
-constexpr int REGS_SOFTMAX = 176, REGS_LOADER = 80, REGS_CONTROL = 80;
-static_assert(128 * (2 * REGS_SOFTMAX + REGS_LOADER + REGS_CONTROL) <= ATT_THREADS * 128, "the warpgroups' shares exceed the launch's registers");
-constexpr float RESCALE = 8.0f;  // log2 of how far a row's weights may exceed 1 before the maximum is moved
+constexpr float RESCALE = 256.0f;  // what 32 weights may add up to before their reference is moved
 
 struct AttParams {
     TreeAttnArgs a;
@@ -50,6 +54,26 @@ struct AttParams {
     unsigned long long wait_limit_ns;
 };
 
+// A run of key tiles [t0, t1) of one (s, h) against one row-tile pair, and where the walk goes on.  Every warp keeps its
+// own in shared memory (it is read now and then, and would take some twenty registers from the softmax).
+struct Walk {
+    int s, h, qt, t0, t1, n_prefix, len, live, rows;
+    int whole;  // all key tiles of the (s, h)
+    int slot;   // partial result: 0 = the CTA's range starts here, 1 = it ends here
+    int more;   // result of the last advance()
+    int next_s, next_h, next_t, next_pass;
+    long long pos, hi;
+};
+struct AttShared {
+    uint64_t full[8], empty[8], go[8], stg_full[6], stg_empty[6], s_full[2], p_full[2], o_full, q_full, xch;
+    long long lo, hi, total;
+    int s, h, t, pass;
+    int nonfinite[16];
+    uint32_t tmem;
+    int abort_flag;
+    Walk walk[MMA_WARP + 1];
+};
+
 template <int D, bool Q8>
 struct Geometry {
     static constexpr int HALVES = D / 64;  // 128-byte swizzle rows per vector
@@ -59,19 +83,10 @@ struct Geometry {
     static constexpr int STAGE_BYTES = TILE * D;
     static constexpr int EXP_AT = 2 * TILE_BYTES + SLOTS * TILE_BYTES + STAGES * STAGE_BYTES;
     static constexpr int MISC_AT = EXP_AT + STAGES * TILE;
-    static constexpr int SMEM = MISC_AT + 1024 + 512 + 1024;
+    static constexpr int SMEM = MISC_AT + (int)sizeof(AttShared);
     static_assert(SMEM <= ATT_SMEM, "shared memory");
 };
 
-struct AttShared {  // after the 1024 bytes of the (m, l) exchange
-    uint64_t full[8], empty[8], go[8], stg_full[6], stg_empty[6], s_full[2], p_full[2], o_full, q_full, xch;
-    long long lo, hi, total;
-    int s, h, t, pass;
-    int nonfinite[16];
-    uint32_t tmem;
-    int abort_flag;
-};
-static_assert(sizeof(AttShared) <= 512, "shared control block");
 
 // Key tiles of sequence s; 0 if it has no live node (or a length that its pages cannot hold).
 __device__ __forceinline__ int sequence_tiles(const TreeAttnArgs& a, int s, int& len, int& live, int& n_prefix) {
@@ -88,67 +103,71 @@ __device__ __forceinline__ int sequence_tiles(const TreeAttnArgs& a, int s, int&
 // Groups that get a range: with fewer tiles than groups, one tile each.
 __device__ __forceinline__ long long groups_used(const AttParams& p, long long total) { return min((long long)p.n_groups, total); }
 
-// A run of key tiles [t0, t1) of one (s, h) against one row-tile pair.
-struct Segment {
-    int s, h, qt, t0, t1, n_tiles, n_prefix, len, live, rows;
-    bool whole;  // all key tiles of the (s, h)
-    int slot;    // partial result: 0 = the CTA's range starts here, 1 = it ends here
-};
-struct SegmentIter {
-    long long pos, hi;
-    int pass, s, h, t;
-    bool first;
-    __device__ __forceinline__ explicit SegmentIter(const AttShared& sh) : pos(sh.lo), hi(sh.hi), pass(sh.pass), s(sh.s), h(sh.h), t(sh.t), first(true) {}
-    __device__ __forceinline__ bool next(const AttParams& p, Segment& g) {
-        while (pos < hi) {
-            g.n_tiles = sequence_tiles(p.a, s, g.len, g.live, g.n_prefix);
-            if (t >= g.n_tiles) {  // (only a sequence without tiles)
-                t = 0;
+__device__ __forceinline__ void start_walk(Walk& w, const AttShared& sh) {
+    w.pos = sh.lo;
+    w.hi = sh.hi;
+    w.next_pass = sh.pass;
+    w.next_s = sh.s;
+    w.next_h = sh.h;
+    w.next_t = sh.t;
+    w.slot = -1;
+}
+__device__ __forceinline__ void advance(const AttParams& p, Walk& w) {
+    long long pos = w.pos;
+    const long long hi = w.hi;
+    int s = w.next_s, h = w.next_h, t = w.next_t, pass = w.next_pass, rows = 0, slot = w.slot;
+    while (pos < hi && rows <= 0) {
+        int len, live, n_prefix;
+        const int n_tiles = sequence_tiles(p.a, s, len, live, n_prefix);
+        if (t < n_tiles) {
+            const int take = (int)min((long long)(n_tiles - t), hi - pos), qt = pass * p.side + (int)(blockIdx.x % p.side);
+            slot = min(slot + 1, 1);
+            rows = qt < p.n_qtiles ? min(2 * TILE, live * p.G - qt * 2 * TILE) : 0;
+            w.s = s;
+            w.h = h;
+            w.qt = qt;
+            w.t0 = t;
+            w.t1 = t + take;
+            w.n_prefix = n_prefix;
+            w.len = len;
+            w.live = live;
+            w.whole = take == n_tiles;
+            pos += take;
+            t += take;
+        }
+        if (t >= n_tiles) {  // on to the next key head
+            t = 0;
+            if (n_tiles == 0 || ++h == p.a.cache.heads) {
                 h = 0;
                 if (++s == p.a.S) {
                     s = 0;
                     ++pass;
                 }
-                continue;
             }
-            const int take = (int)min((long long)(g.n_tiles - t), hi - pos);
-            g.s = s;
-            g.h = h;
-            g.t0 = t;
-            g.t1 = t + take;
-            g.whole = take == g.n_tiles;
-            g.slot = first ? 0 : 1;
-            first = false;
-            g.qt = pass * p.side + (int)(blockIdx.x % p.side);
-            g.rows = min(2 * TILE, g.live * p.G - g.qt * 2 * TILE);
-            pos += take;
-            t += take;
-            if (t == g.n_tiles) {
-                t = 0;
-                if (++h == p.a.cache.heads) {
-                    h = 0;
-                    if (++s == p.a.S) {
-                        s = 0;
-                        ++pass;
-                    }
-                }
-            }
-            if (g.rows > 0 && g.qt < p.n_qtiles) return true;
         }
-        return false;
     }
-};
+    w.rows = rows;
+    w.slot = slot;
+    w.more = rows > 0;
+    w.pos = pos;
+    w.next_s = s;
+    w.next_h = h;
+    w.next_t = t;
+    w.next_pass = pass;
+}
 
 // Calls f(is_v, tile) for the key and value tiles of a segment in the order in which the products consume them;
 // `lead`: streams that start side by side on different tiles (2 if they split the keys).
 template <typename F>
-__device__ __forceinline__ bool for_each_tile(const Segment& g, F&& f) {
+__device__ __forceinline__ bool for_each_tile(const Walk& g, F&& f) {
     const int lead = g.rows > TILE ? 1 : 2;
-    for (int j = g.t0; j < min(g.t1, g.t0 + lead); ++j)
-        if (!f(false, j)) return false;
-    for (int j = g.t0; j < g.t1; ++j) {
-        if (!f(true, j)) return false;
-        if (j + lead < g.t1 && !f(false, j + lead)) return false;
+    const int t1 = g.t1;
+    int k = g.t0, v = k;
+    while (v < t1) {  // (one call of f: it is inlined)
+        const bool is_v = k == t1 || k >= v + lead;
+        if (!f(is_v, is_v ? v : k)) return false;
+        if (is_v) ++v;
+        else ++k;
     }
     return true;
 }
@@ -184,6 +203,34 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// Weights 2^(c s - mc) of 32 scores, as bfloat16, and their sum.
+__device__ __forceinline__ float weights32(const uint32_t (&s)[32], float c, float mc, uint32_t (&w)[16]) {
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const float x = exp2_approx(fmaf(__uint_as_float(s[2 * j]), c, -mc)), y = exp2_approx(fmaf(__uint_as_float(s[2 * j + 1]), c, -mc));
+        sum[(2 * j) & 3] += x;
+        sum[(2 * j + 1) & 3] += y;
+        w[j] = pack2(x, y);
+    }
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+__device__ __forceinline__ float max32(const uint32_t (&s)[32]) {
+    float m[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        m[j] = fmaxf(__uint_as_float(s[j]), __uint_as_float(s[j + 4]));
+#pragma unroll
+        for (int i = j + 8; i < 32; i += 8) m[j] = fmaxf(m[j], fmaxf(__uint_as_float(s[i]), __uint_as_float(s[i + 4])));
+    }
+    return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+}
+__device__ __forceinline__ void hide(uint32_t (&s)[32], uint32_t seen) {  // scores without their bit become -inf
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (!((seen >> j) & 1u)) s[j] = 0xFF800000u;
+}
+
 __device__ __forceinline__ uint32_t nonfinite_to_zero(uint32_t v, bool& found) {
     if ((v & 0x7F80u) == 0x7F80u) {
         v &= 0xFFFF0000u;
@@ -200,13 +247,15 @@ template <int D, bool Q8>
 __global__ void __launch_bounds__(ATT_THREADS, 1)
 tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttParams p) {
     using Geo = Geometry<D, Q8>;
-    extern __shared__ unsigned char smem_raw[];
-    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-    unsigned char* smem = smem_raw + (base - raw);
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const uint32_t base = smem_u32(smem);
+    if (base & 1023u) {  // (never: the swizzled tiles need it)
+        if (threadIdx.x == 0) atomicOr(p.a.status, SPEC_STATUS_TIMEOUT);
+        return;
+    }
     const uint32_t q_at = base, ring_at = base + 2 * Geo::TILE_BYTES, stg_at = ring_at + Geo::SLOTS * Geo::TILE_BYTES;
     const uint32_t exp_at = base + Geo::EXP_AT;
-    float2* xch = reinterpret_cast<float2*>(smem + Geo::MISC_AT);
-    AttShared& sh = *reinterpret_cast<AttShared*>(smem + Geo::MISC_AT + 1024);
+    AttShared& sh = *reinterpret_cast<AttShared*>(smem + Geo::MISC_AT);
     volatile int* abort_flag = &sh.abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const TreeAttnArgs& a = p.a;
@@ -214,13 +263,13 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < Geo::SLOTS; ++i) {
-            mbar_init(smem_u32(&sh.full[i]), 128);
+            mbar_init(smem_u32(&sh.full[i]), LOADERS);
             mbar_init(smem_u32(&sh.empty[i]), 1);
             mbar_init(smem_u32(&sh.go[i]), 1);
         }
         for (int i = 0; i < Geo::STAGES; ++i) {
             mbar_init(smem_u32(&sh.stg_full[i]), 1);
-            mbar_init(smem_u32(&sh.stg_empty[i]), 128);
+            mbar_init(smem_u32(&sh.stg_empty[i]), LOADERS);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sh.s_full[i]), 1);
@@ -233,17 +282,18 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 13) {
+    if (warp == MMA_WARP) {
         tmem_alloc(smem_u32(&sh.tmem), 512);
         tmem_relinquish();
     }
-    if (warp == 12 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? &tm_v : &tm_k)) : "memory");
+    if (warp == TMA_WARP && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? &tm_v : &tm_k)) : "memory");
     grid_dependency_wait();
     // ---------------------------------------------------------------- this CTA's range of key tiles
     if (warp == 0) {
-        long long sum = 0;
         int len, live, np;
-        for (int s = lane; s < a.S; s += 32) sum += sequence_tiles(a, s, len, live, np);
+        const int n_first = lane < a.S ? sequence_tiles(a, lane, len, live, np) : 0;
+        long long sum = n_first;
+        for (int s = lane + 32; s < a.S; s += 32) sum += sequence_tiles(a, s, len, live, np);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         const long long per_pass = sum * cache.heads, total = per_pass * p.passes;
@@ -263,7 +313,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         long long before = 0;
         for (int s0 = 0; s0 < a.S; s0 += 32) {
             const int s = s0 + lane;
-            const int n = s < a.S ? sequence_tiles(a, s, len, live, np) : 0;
+            const int n = s0 == 0 ? n_first : (s < a.S ? sequence_tiles(a, s, len, live, np) : 0);
             long long upto = n;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -295,28 +345,34 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     const uint32_t s_full = smem_u32(&sh.s_full[0]), p_full = smem_u32(&sh.p_full[0]), o_full = smem_u32(&sh.o_full), q_full = smem_u32(&sh.q_full);
     const uint32_t xch_bar = smem_u32(&sh.xch);
     auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, p.wait_limit_ns); };
-    Segment g;
-    SegmentIter it(sh);
+    Walk& g = sh.walk[min(warp, MMA_WARP)];
+    auto next = [&]() {  // the warp's next segment
+        __syncwarp();
+        if (lane == 0) advance(p, g);
+        __syncwarp();
+        return g.more != 0;
+    };
+    if (lane == 0 && warp <= MMA_WARP) start_walk(g, sh);
 
-    if (warp < 8) {
+    if (warp < SOFTMAX_WARPS) {
         // ------------------------------------------------------------------------------------ softmax
+        set_regs_up<REGS_SOFTMAX>();
         // (a warp gives up as a whole: what follows a wait is collective)
         auto warp_wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
-        set_regs_up<REGS_SOFTMAX>();
         const int stream = warp >> 2, wq = warp & 3;
         const uint32_t lanes = tmem + ((uint32_t)(wq * 32) << 16);
         const uint32_t s_tm = lanes + stream * TILE, o_tm = lanes + 2 * TILE + stream * TILE;
         uint32_t n_s = 0, n_seg = 0, n_xch = 0;  // tiles of this stream, segments, exchanges so far
         bool ok = true;
-        while (ok && it.next(p, g)) {
+        while (ok && next()) {
             const bool split = g.rows <= TILE;  // the streams split the keys
             const int tile_row = (split ? 0 : stream * TILE) + wq * 32 + lane;
             const bool valid = tile_row < g.rows;
-            const int R = g.qt * 2 * TILE + tile_row, node = R / p.G, gq = R - node * p.G;
             const bool warp_on = (split ? 0 : stream * TILE) + wq * 32 < g.rows;
             // ---- queries into shared memory (once: by stream 0 if both read the same rows)
             if (!split || stream == 0) {
                 constexpr int LPR = D / 8, RPI = 32 / LPR;  // lanes per row, rows per instruction
+                const int R = g.qt * 2 * TILE + tile_row, node = R / p.G, gq = R - node * p.G;
                 const long long off = valid ? ((long long)g.s * a.N + node) * a.q_tok + (long long)(g.h * p.G + gq) * a.q_head : -1;
                 const uint32_t dst = q_at + stream * Geo::TILE_BYTES;
                 const int c = lane % LPR;
@@ -340,74 +396,70 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 ++n_s;
                 tc_fence_after();
                 if (warp_on) {
-                    uint32_t r[4][32];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) tmem_ld32(s_tm + 32 * i, r[i]);
-                    tmem_wait_ld();
                     const int valid_keys = t < g.n_prefix ? g.len - t * TILE : g.live - (t - g.n_prefix) * TILE;
-                    if (t >= g.n_prefix || valid_keys < TILE) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int left = valid_keys - 32 * i;
-                            w[i] = left >= 32 ? 0xFFFFFFFFu : (left <= 0 ? 0u : (1u << left) - 1u);
-                            if (t >= g.n_prefix) {
-                                const int words = (a.N + 31) / 32, at = (t - g.n_prefix) * 4 + i;
-                                w[i] &= (valid && at < words) ? (uint32_t)a.mask[((long long)g.s * a.N + node) * words + at] : 0u;
-                            }
+                    const bool masked = t >= g.n_prefix || valid_keys < TILE;
+                    auto seen = [&](int i) {  // which of scores [32 i, 32 i + 32) this row has
+                        const int left = valid_keys - 32 * i;
+                        uint32_t w = left >= 32 ? 0xFFFFFFFFu : (left <= 0 ? 0u : (1u << left) - 1u);
+                        if (t >= g.n_prefix) {
+                            const int words = (a.N + 31) / 32, at = (t - g.n_prefix) * 4 + i, node = (g.qt * 2 * TILE + tile_row) / p.G;
+                            w &= (valid && at < words) ? (uint32_t)a.mask[((long long)g.s * a.N + node) * words + at] : 0u;
                         }
+                        return w;
+                    };
+                    // 32 scores at a time, the next 32 on their way, in a loop that stays in the instruction cache (with all 128
+                    // unrolled, fetching instructions cost more than the exponentials).  The reference m is a score of the row
+                    // that was the largest of its 32 when it was taken; it stays until 32 weights add up to more than
+                    // RESCALE (or to no number, as for a row without a reference), which is when their maximum is looked for.
+                    auto scale_sums = [&](float f) {  // O, of this warp's rows
+#pragma unroll 1
+                        for (int i = 0; i < D; i += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(o_tm + i, o);
+                            tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (!((w[i] >> j) & 1u)) r[i][j] = 0xFF800000u;
-                    }
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int j = 0; j < 32; j += 2) top = fmaxf(top, fmaxf(__uint_as_float(r[i][j]), __uint_as_float(r[i][j + 1])));
-                    const bool first = t < g.t0 + step;
-                    if (first) {
-                        m = top;
-                    } else {
-                        const bool move = (top - m) * p.c > RESCALE;  // (m = -inf: the row has had no key yet)
+                            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                            tmem_st16(o_tm + i, o);
+                        }
+                    };
+                    auto chunk = [&](int i, uint32_t(&x)[32]) {
+                        if (masked) hide(x, seen(i));
+                        uint32_t w[16];
+                        float sum = weights32(x, p.c, m * p.c, w);
+                        const bool move = !(sum <= RESCALE);
                         if (__any_sync(0xffffffffu, move)) {
-                            const float f = move ? exp2_approx((m - top) * p.c) : 1.0f;
+                            const float top = fmaxf(m, max32(x));
+                            const float f = move && top > m ? exp2_approx((m - top) * p.c) : 1.0f;
                             if (move) m = top;
                             l *= f;
+                            if (t >= g.t0 + step) scale_sums(f);
 #pragma unroll 1
-                            for (int i = 0; i < D / 32; ++i) {
-                                uint32_t o[32];
-                                tmem_ld32(o_tm + 32 * i, o);
+                            for (int k = 0; k < i; ++k) {  // this tile's weights so far
+                                uint32_t v[16];
+                                tmem_ld16(s_tm + 16 * k, v);
                                 tmem_wait_ld();
-                                uint32_t lo[16], hi[16];
+                                const uint32_t f2 = pack2(f, f);  // (1, or below 2^-3: its rounding counts for little)
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) {
-                                    lo[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                                    hi[j] = __float_as_uint(__uint_as_float(o[j + 16]) * f);
-                                }
-                                tmem_st16(o_tm + 32 * i, lo);
-                                tmem_st16(o_tm + 32 * i + 16, hi);
+                                for (int j = 0; j < 16; ++j) v[j] = mul_bf16x2(v[j], f2);
+                                tmem_st16(s_tm + 16 * k, v);
                             }
+                            sum = weights32(x, p.c, m == -INFINITY ? 0.0f : m * p.c, w);
                         }
-                    }
-                    const float mc = m == -INFINITY ? 0.0f : m * p.c;
-                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t w[16];
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const float x = exp2_approx(fmaf(__uint_as_float(r[i][2 * j]), p.c, -mc));
-                            const float y = exp2_approx(fmaf(__uint_as_float(r[i][2 * j + 1]), p.c, -mc));
-                            sum[(2 * j) & 3] += x;
-                            sum[(2 * j + 1) & 3] += y;
-                            w[j] = pack2(x, y);
-                        }
+                        l += sum;
                         tmem_st16(s_tm + 16 * i, w);
+                    };
+                    uint32_t x[32], y[32];
+                    tmem_ld32(s_tm, x);
+                    tmem_wait_ld();
+#pragma unroll 1
+                    for (int i = 0; i < 4; i += 2) {
+                        tmem_ld32(s_tm + 32 * (i + 1), y);
+                        chunk(i, x);
+                        tmem_wait_ld();
+                        if (i == 0) tmem_ld32(s_tm + 64, x);
+                        chunk(i + 1, y);
+                        tmem_wait_ld();
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                     tmem_wait_st();
                 }
                 tc_fence_before();
@@ -422,20 +474,27 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             const bool both = split && g.t1 - g.t0 > 1;  // stream 1 had a tile
             if (both) {
                 if (stream == 1) {
-                    xch[wq * 32 + lane] = make_float2(m, l);
+                    // through the lanes' own columns of stream 1's scores, which are done with
+                    tmem_st1(s_tm, __float_as_uint(m));
+                    tmem_st1(s_tm + 1, __float_as_uint(l));
+                    tmem_wait_st();
+                    tc_fence_before();
                     mbar_arrive(xch_bar);
                 } else {
                     if (!(ok = warp_wait(xch_bar, n_xch & 1u))) break;
-                    const float2 other = xch[wq * 32 + lane];
-                    const float top = fmaxf(m, other.x);
+                    tc_fence_after();
+                    const uint32_t m1 = tmem_ld1(s_tm + TILE), l1 = tmem_ld1(s_tm + TILE + 1);
+                    tmem_wait_ld();
+                    const float other = __uint_as_float(m1), top = fmaxf(m, other);
                     f0 = m == -INFINITY ? 0.0f : exp2_approx((m - top) * p.c);
-                    f1 = other.x == -INFINITY ? 0.0f : exp2_approx((other.x - top) * p.c);
-                    l = l * f0 + other.y * f1;
+                    f1 = other == -INFINITY ? 0.0f : exp2_approx((other - top) * p.c);
+                    l = l * f0 + __uint_as_float(l1) * f1;
                     m = top;
                 }
                 ++n_xch;
             }
             if ((!split || stream == 0) && warp_on) {
+                const int R = g.qt * 2 * TILE + tile_row, node = R / p.G, gq = R - node * p.G;
                 const bool poisoned = sh.nonfinite[n_seg & 15u] == (int)n_seg + 1;
                 const float inv = g.whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
                 const long long out_row = ((long long)g.s * a.N + node) * a.Hq + g.h * p.G + gq;
@@ -491,14 +550,14 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             tc_fence_before();
             ++n_seg;
         }
-    } else if (warp < 12) {
+    } else if (warp < SOFTMAX_WARPS + LOADER_WARPS) {
         // ------------------------------------------------------------------------------------ tiles written by threads
         set_regs_down<REGS_LOADER>();
         const int tid = threadIdx.x - 256;
         constexpr int CH = D / 8;  // 16-byte chunks of a bf16 vector
         uint32_t slot = 0, phase = 0, stg = 0, stg_phase = 0, n_seg = 0;
         uint32_t go_phase = 0;  // bit per slot
-        while (it.next(p, g)) {
+        while (next()) {
             const bool ok = for_each_tile(g, [&](bool is_v, int t) {
                 const bool block = t >= g.n_prefix;
                 const uint32_t dst = ring_at + slot * Geo::TILE_BYTES, bar_full = full + 8 * slot, bar_empty = empty + 8 * slot;
@@ -515,9 +574,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     const uint32_t src = stg_at + stg * Geo::STAGE_BYTES, ex = exp_at + stg * TILE;
                     constexpr int LPR = D / 16;
                     const bool swap = (tid & 4) != 0 && D == 128;  // so that the 8 lanes of a phase write to different banks
-#pragma unroll 4
-                    for (int i = 0; i < LPR; ++i) {
-                        const int r = i * (128 / LPR) + tid / LPR, c = tid % LPR;
+#pragma unroll
+                    for (int i = 0; i < TILE * LPR / LOADERS; ++i) {
+                        const int r = i * (LOADERS / LPR) + tid / LPR, c = tid % LPR;
                         uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
                         if (r < rows) {
                             const uint4 v = ld_shared16(src + r * D + c * 16);
@@ -546,12 +605,12 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                         go_phase ^= 1u << my_slot;
                     }
                     bool found = false;
-#pragma unroll 1
-                    for (int i0 = 0; i0 < CH; i0 += 8) {
-                        uint4 v[8];
+                    constexpr int PER = TILE * CH / LOADERS;
+                    {
+                        uint4 v[PER];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int r = (i0 + i) * (128 / CH) + tid / CH, c = tid % CH;
+                        for (int i = 0; i < PER; ++i) {
+                            const int r = i * (LOADERS / CH) + tid / CH, c = tid % CH;
                             v[i] = make_uint4(0, 0, 0, 0);
                             if (r >= rows) continue;
                             const __nv_bfloat16* src;
@@ -572,8 +631,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                             v[i] = *reinterpret_cast<const uint4*>(src + c * 8);
                         }
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int r = (i0 + i) * (128 / CH) + tid / CH, c = tid % CH;
+                        for (int i = 0; i < PER; ++i) {
+                            const int r = i * (LOADERS / CH) + tid / CH, c = tid % CH;
                             if (block && is_v) {
                                 v[i].x = nonfinite_to_zero(v[i].x, found);
                                 v[i].y = nonfinite_to_zero(v[i].y, found);
@@ -594,7 +653,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         }
     } else {
         set_regs_down<REGS_CONTROL>();
-        if (warp == 12) {
+        if (warp == TMA_WARP) {
             // -------------------------------------------------------------------------------- TMA
             // A lane fetches one page's part of a tile; page numbers are read a tile ahead.
             uint32_t slot = 0, phase = 0, issued = 0;
@@ -602,7 +661,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             const int page = 1 << cache.page_shift, per_tile = TILE >> cache.page_shift;
             const int all_rows = (cache.n_pages * cache.heads) << cache.page_shift;  // a coordinate beyond the cache: reads as 0
             bool ok = true;
-            while (ok && it.next(p, g)) {
+            while (ok && next()) {
                 const int32_t* table = cache.table + (long long)g.s * cache.max_pages;
                 const int n_pages = (g.len + page - 1) >> cache.page_shift;
                 // (the pages of a tile's K serve its V one or two tiles later: kept in two registers, by the tile's parity)
@@ -646,7 +705,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     const int pages = min((rows + page - 1) >> cache.page_shift, per_tile);
                     if (lane == 0) {
                         mbar_expect_tx(bar_full, (uint32_t)(pages * page) * (Q8 ? D + 1 : 2 * D));
-                        if (!Q8) mbar_arrive_n(bar_full, 127);
+                        if (!Q8) mbar_arrive_n(bar_full, LOADERS - 1);
                     }
                     __syncwarp();
                     if (lane < pages) {
@@ -670,7 +729,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 const uint64_t until = global_timer_ns() + 1000000ull;
                 while (issued && global_timer_ns() < until) {}
             }
-        } else if (warp == 13 && lane == 0) {
+        } else if (warp == MMA_WARP && lane == 0) {
             // -------------------------------------------------------------------------------- products
             const uint32_t id_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
             const uint32_t id_pv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
@@ -687,21 +746,27 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 tc_fence_after();
                 return got;
             };
+            // (descriptors of the first k-slice; the others are a constant further in their address field)
+            const uint64_t q_desc = make_kmajor_sw128_desc(q_at), k_desc = make_kmajor_sw128_desc(0), v_desc = make_mnmajor_sw128_desc(0, TILE * 128);
             auto qk = [&](int stream, int q_tile, uint32_t k_at) {
+                const uint64_t qd = q_desc + (uint64_t)(q_tile * (Geo::TILE_BYTES >> 4)), kd = k_desc + (k_at >> 4);
+                const uint32_t d = tmem + stream * TILE;
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t o = (uint32_t)((k >> 2) * (TILE * 128) + (k & 3) * 32);
-                    tc_mma_bf16(tmem + stream * TILE, make_kmajor_sw128_desc(q_at + q_tile * Geo::TILE_BYTES + o), make_kmajor_sw128_desc(k_at + o), id_qk, k != 0);
+                    constexpr uint32_t half = TILE * 128 >> 4;
+                    tc_mma_bf16(d, qd + ((k >> 2) * half + (k & 3) * 2), kd + ((k >> 2) * half + (k & 3) * 2), id_qk, k != 0);
                 }
                 tc_commit(s_full + 8 * stream);
             };
             auto pv = [&](int stream, uint32_t v_at, bool add) {
+                const uint64_t vd = v_desc + (v_at >> 4);
+                const uint32_t w = tmem + stream * TILE, d = tmem + 2 * TILE + stream * TILE;
 #pragma unroll
-                for (int k = 0; k < TILE / 16; ++k)
-                    tc_mma_bf16_ts(tmem + 2 * TILE + stream * TILE, tmem + stream * TILE + 8 * k, make_mnmajor_sw128_desc(v_at + k * 2048, TILE * 128), id_pv,
-                                   (add || k != 0) ? 1u : 0u);
+                for (int k = 0; k < TILE / 16; ++k) tc_mma_bf16_ts(d, w + 8 * k, vd + k * (2048 >> 4), id_pv, (add || k != 0) ? 1u : 0u);
             };
-            while (ok && it.next(p, g)) {
+            while (ok) {
+                advance(p, g);
+                if (!g.more) break;
                 const int n = g.t1 - g.t0;
                 uint32_t k_at, v_at, ki, vi;
                 if (!(ok = wait(q_full, n_seg & 1u))) break;
@@ -758,69 +823,74 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && *abort_flag) atomicOr(a.status, SPEC_STATUS_TIMEOUT);
-    if (warp == 13) tmem_dealloc(tmem, 512);
+    if (warp == MMA_WARP) tmem_dealloc(tmem, 512);
 }
 
 // Joins the partial rows of every (s, h, row-tile pair) whose key tiles were spread over several CTAs, in the CTAs'
-// order, and writes the rows that attend to nothing.  A warp per row; 32 rows per CTA.
+// order, and writes the rows that attend to nothing.  A warp per row.
+constexpr int JOIN_ROWS = 8;
 template <int D>
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ AttParams p) {
+__global__ void __launch_bounds__(32 * JOIN_ROWS) join_kernel(const __grid_constant__ AttParams p) {
     constexpr int E = D / 32;
     const TreeAttnArgs& a = p.a;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    grid_dependency_wait();
+    const int lane = threadIdx.x & 31;
     grid_launch_dependents();
+    grid_dependency_wait();
     const int s = (int)(blockIdx.x / a.cache.heads), h = (int)(blockIdx.x % a.cache.heads), qt = blockIdx.y;
+    const int r = blockIdx.z * JOIN_ROWS + (threadIdx.x >> 5);
+    if (r >= min(2 * TILE, a.N * p.G - qt * 2 * TILE)) return;
     int len, live, np;
     const int tiles = sequence_tiles(a, s, len, live, np);
-    const long long per_pass = p.cum[a.S] * a.cache.heads, total = per_pass * p.passes;
+    const int R = qt * 2 * TILE + r, node = R / p.G, gq = R - node * p.G;
+    const long long out_row = ((long long)s * a.N + node) * a.Hq + h * p.G + gq;
+    __nv_bfloat16* out = (__nv_bfloat16*)a.out + out_row * D + lane * E;
+    if (node >= live) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) out[j] = __float2bfloat16_rn(0.0f);
+        if (a.lse && lane == 0) a.lse[out_row] = -INFINITY;
+        return;
+    }
+    const long long per_pass = p.cum[a.S] * a.cache.heads, total = per_pass * p.passes, n_groups = groups_used(p, total);
     const long long u0 = (qt / p.side) * per_pass + p.cum[s] * a.cache.heads + (long long)h * tiles, u1 = u0 + tiles;
-    const long long n_groups = groups_used(p, total);
-    auto group_of = [&](long long x) { return ((x + 1) * n_groups + total - 1) / total - 1; };  // the group whose range holds tile x
-    long long g0 = 0, g1 = 0;
-    if (tiles) {
-        g0 = group_of(u0);
-        g1 = group_of(u1 - 1);
-    }
-    const int rows = min(2 * TILE, a.N * p.G - qt * 2 * TILE), used = min(2 * TILE, live * p.G - qt * 2 * TILE);
-    if (g0 == g1 && used >= rows) return;
-    for (int r = blockIdx.z * 32 + warp; r < min(rows, (int)blockIdx.z * 32 + 32); r += 8) {
-        const int R = qt * 2 * TILE + r, node = R / p.G, gq = R - node * p.G;
-        const long long out_row = ((long long)s * a.N + node) * a.Hq + h * p.G + gq;
-        __nv_bfloat16* out = (__nv_bfloat16*)a.out + out_row * D + lane * E;
-        if (r >= used) {
+    // the groups whose ranges [g total / n, (g + 1) total / n) hold the first and the last tile
+    const int g0 = (int)(((u0 + 1) * n_groups + total - 1) / total) - 1, g1 = (int)((u1 * n_groups + total - 1) / total) - 1;
+    if (g0 == g1) return;
+    // the first group's range may begin before u0: then its part is the one at the range's end
+    const long long at0 = (((long long)g0 * p.side + qt % p.side) * 2 + (u0 > g0 * total / n_groups ? 1 : 0)) * p.rows_cap + r;
+    const long long at1 = (((long long)(g0 + 1) * p.side + qt % p.side) * 2) * p.rows_cap + r, stride = (long long)p.side * 2 * p.rows_cap;
+    auto part = [&](int i) { return i == 0 ? at0 : at1 + (i - 1) * stride; };
+    const int n = g1 - g0 + 1;
+    float m = -INFINITY;
+    for (int i = lane; i < n; i += 32) m = fmaxf(m, p.part_ml[part(i)].x);
 #pragma unroll
-            for (int j = 0; j < E; ++j) out[j] = __float2bfloat16_rn(0.0f);
-            if (a.lse && lane == 0) a.lse[out_row] = -INFINITY;
-            continue;
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float l = 0.0f, x[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) x[j] = 0.0f;
+    for (int i0 = 0; i0 < n; i0 += 8) {  // eight parts' loads in flight
+        float2 ml[8];
+        float o[8][E];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (i0 + i >= n) continue;
+            const long long at = part(i0 + i);
+            ml[i] = p.part_ml[at];
+#pragma unroll
+            for (int j = 0; j < E; ++j) o[i][j] = p.part_o[at * D + lane * E + j];
         }
-        if (g0 == g1) continue;
-        auto part_of = [&](long long gi) {
-            const int slot = u0 > gi * total / n_groups ? 1 : 0;
-            return (((gi * p.side + qt % p.side) * 2 + slot) * p.rows_cap) + r;
-        };
-        float m = -INFINITY;
-        for (long long gi = g0 + lane; gi <= g1; gi += 32) m = fmaxf(m, p.part_ml[part_of(gi)].x);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        float l = 0.0f, x[E];
+        for (int i = 0; i < 8; ++i) {
+            if (i0 + i >= n) continue;
+            const float f = ml[i].x == -INFINITY ? 0.0f : exp2f((ml[i].x - m) * p.c);
+            l += ml[i].y * f;
 #pragma unroll
-        for (int j = 0; j < E; ++j) x[j] = 0.0f;
-#pragma unroll 4
-        for (long long gi = g0; gi <= g1; ++gi) {
-            const long long at = part_of(gi);
-            const float2 ml = p.part_ml[at];
-            const float f = ml.x == -INFINITY ? 0.0f : exp2f((ml.x - m) * p.c);
-            const float* o = p.part_o + at * D + lane * E;
-            l += ml.y * f;
-#pragma unroll
-            for (int j = 0; j < E; ++j) x[j] += o[j] * f;
+            for (int j = 0; j < E; ++j) x[j] += o[i][j] * f;
         }
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-#pragma unroll
-        for (int j = 0; j < E; ++j) out[j] = __float2bfloat16_rn(x[j] * inv);
-        if (a.lse && lane == 0) a.lse[out_row] = l == 0.0f ? -INFINITY : (m * p.c + log2f(l)) * LN2;
     }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int j = 0; j < E; ++j) out[j] = __float2bfloat16_rn(x[j] * inv);
+    if (a.lse && lane == 0) a.lse[out_row] = l == 0.0f ? -INFINITY : (m * p.c + log2f(l)) * LN2;
 }
 
 // ------------------------------------------------------------------------------------------ host
@@ -872,7 +942,7 @@ static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
             cudaFuncAttributes attr;
             int rc = check_cuda(ctx, cudaFuncGetAttributes(&attr, kernel), "spec_tree_attention: cudaFuncGetAttributes");
             if (rc) return rc;
-            if (attr.numRegs * ATT_THREADS < 128 * (2 * REGS_SOFTMAX + REGS_LOADER + REGS_CONTROL))  // the warpgroups would wait for registers for ever
+            if (attr.numRegs < LAUNCH_REGS)  // the warpgroups would wait for registers for ever
                 return fail(ctx, SPEC_ERR_UNSUPPORTED, "spec_tree_attention: built with %d registers per thread", attr.numRegs);
             if ((rc = check_cuda(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Geometry<D, Q8>::SMEM),
                                  "spec_tree_attention: cudaFuncSetAttribute")))
@@ -885,7 +955,7 @@ static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
     if (rc || (rc = cache_map(ctx, &tm_v, p.a.cache.v, p.a.cache))) return rc;
     cudaError_t e = launch_pdl(kernel, dim3(p.n_groups * p.side), dim3(ATT_THREADS), (size_t)Geometry<D, Q8>::SMEM, st, tm_k, tm_v, p);
     if ((rc = check_cuda(ctx, e, "spec_tree_attention launch"))) return rc;
-    e = launch_pdl(join_kernel<D>, dim3(p.a.S * p.a.cache.heads, p.n_qtiles, (p.rows_cap + 31) / 32), dim3(256), 0, st, p);
+    e = launch_pdl(join_kernel<D>, dim3(p.a.S * p.a.cache.heads, p.n_qtiles, (p.rows_cap + JOIN_ROWS - 1) / JOIN_ROWS), dim3(32 * JOIN_ROWS), 0, st, p);
     ctx->launches += 2;
     return check_cuda(ctx, e, "spec_tree_attention join launch");
 }
