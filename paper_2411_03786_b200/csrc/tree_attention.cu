@@ -13,16 +13,19 @@
 //
 // Two streams per CTA hide the softmax of one tile behind the products of another.  With more than 128 rows they are
 // two row tiles against the same keys; with at most 128 they are the even and the odd tiles of keys against the same
-// rows, joined at the end (O of both streams lies in the same lanes).
+// rows, joined at the end (O of both streams lies in the same lanes).  One warp issues the products of both in turn,
+// which keeps them out of step: in step, both would wait for the exponentials and then both for the products.
 //
 // Work: the tiles of all (s, h) in a row are cut into equal consecutive ranges, one per CTA (with several row-tile pairs:
 // per group of CTAs, one for each, which walk the same keys in step and so share them in L2).  A range that ends inside
 // an (s, h) leaves fp32 partial rows and their (m, l), which a second kernel joins in a fixed order.  Any mixture of
 // lengths thus occupies all SMs to within a tile, and nothing about the lengths is needed on the host.
 //
-// Warps (640 threads, which share the registers unevenly): 0-3 and 4-7 softmax of stream 0 and 1 (a thread owns a row); 8-15 write key
-// and value tiles that TMA cannot (the last tile of a context, zero-padded; the block's own; an E4M3 cache's, as bfloat16
-// code * scale, which is exact); 16 TMA; 17 issues the products.
+// Warps (896 threads, which share the registers unevenly): 0-7 and 8-15 softmax of stream 0 and 1 (a row's 128 scores
+// belong to two threads, of warps w and w + 4: a single warp per scheduler leaves the special function unit waiting);
+// 16-23 write key and value tiles that TMA cannot (the last tile of a context, zero-padded; the block's own; an E4M3
+// cache's, as bfloat16 code * scale, which is exact); 24 TMA; 25 issues the products; 26 walks the CTA's range and tells
+// the others.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -34,13 +37,14 @@
 
 namespace ngs {
 
-constexpr int SOFTMAX_WARPS = 8, LOADER_WARPS = 8, LOADERS = 32 * LOADER_WARPS, TMA_WARP = 16, MMA_WARP = 17;
-constexpr int ATT_THREADS = 640;  // whole warpgroups, which is what registers are moved between
-constexpr int LAUNCH_REGS = 96;   // per thread at launch: 65536 / 640, rounded down to a multiple of 8
-constexpr int REGS_SOFTMAX = 112, REGS_LOADER = 80, REGS_CONTROL = 96;
-static_assert(128 * (2 * REGS_SOFTMAX + 2 * REGS_LOADER + REGS_CONTROL) <= ATT_THREADS * LAUNCH_REGS, "the warpgroups' shares exceed the launch's registers");
+constexpr int SOFTMAX_WARPS = 16, LOADER_WARPS = 8, LOADERS = 32 * LOADER_WARPS, TMA_WARP = 24, MMA_WARP = 25, PLAN_WARP = 26;
 constexpr int TILE = 128;  // keys of a tile and rows of a row tile
 constexpr int ATT_SMEM = 227 * 1024;
+constexpr int ATT_THREADS = 896;  // whole warpgroups, which is what registers are moved between
+constexpr int LAUNCH_REGS = 72;   // per thread at launch: 65536 / 896, rounded down to a multiple of 8
+constexpr int REGS_SOFTMAX = 88, REGS_LOADER = 40, REGS_CONTROL = 72;
+constexpr int SEGMENTS = 4;  // segments that the planning warp is ahead
+static_assert(128 * (4 * REGS_SOFTMAX + 2 * REGS_LOADER + REGS_CONTROL) <= ATT_THREADS * LAUNCH_REGS, "the warpgroups' shares exceed the launch's registers");
 constexpr float RESCALE = 256.0f;  // what 32 weights may add up to before their reference is moved
 
 struct AttParams {
@@ -54,24 +58,19 @@ struct AttParams {
     unsigned long long wait_limit_ns;
 };
 
-// A run of key tiles [t0, t1) of one (s, h) against one row-tile pair, and where the walk goes on.  Every warp keeps its
-// own in shared memory (it is read now and then, and would take some twenty registers from the softmax).
-struct Walk {
+// A run of key tiles [t0, t1) of one (s, h) against one row-tile pair.
+struct Segment {
     int s, h, qt, t0, t1, n_prefix, len, live, rows;
     int whole;  // all key tiles of the (s, h)
     int slot;   // partial result: 0 = the CTA's range starts here, 1 = it ends here
-    int more;   // result of the last advance()
-    int next_s, next_h, next_t, next_pass;
-    long long pos, hi;
+    int more;   // 0: there was none left
 };
 struct AttShared {
-    uint64_t full[8], empty[8], go[8], stg_full[6], stg_empty[6], s_full[2], p_full[2], o_full, q_full, xch;
-    long long lo, hi, total;
-    int s, h, t, pass;
+    uint64_t full[8], empty[8], go[8], stg_full[6], stg_empty[6], s_full[2], p_full[2], o_full, q_full, xch, seg_full[SEGMENTS], seg_empty[SEGMENTS];
+    Segment segment[SEGMENTS];
     int nonfinite[16];
     uint32_t tmem;
     int abort_flag;
-    Walk walk[MMA_WARP + 1];
 };
 
 template <int D, bool Q8>
@@ -103,63 +102,52 @@ __device__ __forceinline__ int sequence_tiles(const TreeAttnArgs& a, int s, int&
 // Groups that get a range: with fewer tiles than groups, one tile each.
 __device__ __forceinline__ long long groups_used(const AttParams& p, long long total) { return min((long long)p.n_groups, total); }
 
-__device__ __forceinline__ void start_walk(Walk& w, const AttShared& sh) {
-    w.pos = sh.lo;
-    w.hi = sh.hi;
-    w.next_pass = sh.pass;
-    w.next_s = sh.s;
-    w.next_h = sh.h;
-    w.next_t = sh.t;
-    w.slot = -1;
-}
-__device__ __forceinline__ void advance(const AttParams& p, Walk& w) {
-    long long pos = w.pos;
-    const long long hi = w.hi;
-    int s = w.next_s, h = w.next_h, t = w.next_t, pass = w.next_pass, rows = 0, slot = w.slot;
-    while (pos < hi && rows <= 0) {
+// The planning warp's place in the CTA's range.
+struct Walk {
+    int s, h, t, pass, slot;
+    long long pos, hi;
+};
+__device__ __forceinline__ void advance(const AttParams& p, Walk& w, Segment& g) {
+    int rows = 0;
+    while (w.pos < w.hi && rows <= 0) {
         int len, live, n_prefix;
-        const int n_tiles = sequence_tiles(p.a, s, len, live, n_prefix);
-        if (t < n_tiles) {
-            const int take = (int)min((long long)(n_tiles - t), hi - pos), qt = pass * p.side + (int)(blockIdx.x % p.side);
-            slot = min(slot + 1, 1);
+        const int n_tiles = sequence_tiles(p.a, w.s, len, live, n_prefix);
+        if (w.t < n_tiles) {
+            const int take = (int)min((long long)(n_tiles - w.t), w.hi - w.pos), qt = w.pass * p.side + (int)(blockIdx.x % p.side);
             rows = qt < p.n_qtiles ? min(2 * TILE, live * p.G - qt * 2 * TILE) : 0;
-            w.s = s;
-            w.h = h;
-            w.qt = qt;
-            w.t0 = t;
-            w.t1 = t + take;
-            w.n_prefix = n_prefix;
-            w.len = len;
-            w.live = live;
-            w.whole = take == n_tiles;
-            pos += take;
-            t += take;
+            g.s = w.s;
+            g.h = w.h;
+            g.qt = qt;
+            g.t0 = w.t;
+            g.t1 = w.t + take;
+            g.n_prefix = n_prefix;
+            g.len = len;
+            g.live = live;
+            g.whole = take == n_tiles;
+            g.slot = w.slot;
+            w.slot = 1;
+            w.pos += take;
+            w.t += take;
         }
-        if (t >= n_tiles) {  // on to the next key head
-            t = 0;
-            if (n_tiles == 0 || ++h == p.a.cache.heads) {
-                h = 0;
-                if (++s == p.a.S) {
-                    s = 0;
-                    ++pass;
+        if (w.t >= n_tiles) {  // on to the next key head
+            w.t = 0;
+            if (n_tiles == 0 || ++w.h == p.a.cache.heads) {
+                w.h = 0;
+                if (++w.s == p.a.S) {
+                    w.s = 0;
+                    ++w.pass;
                 }
             }
         }
     }
-    w.rows = rows;
-    w.slot = slot;
-    w.more = rows > 0;
-    w.pos = pos;
-    w.next_s = s;
-    w.next_h = h;
-    w.next_t = t;
-    w.next_pass = pass;
+    g.rows = rows;
+    g.more = rows > 0;
 }
 
 // Calls f(is_v, tile) for the key and value tiles of a segment in the order in which the products consume them;
 // `lead`: streams that start side by side on different tiles (2 if they split the keys).
 template <typename F>
-__device__ __forceinline__ bool for_each_tile(const Walk& g, F&& f) {
+__device__ __forceinline__ bool for_each_tile(const Segment& g, F&& f) {
     const int lead = g.rows > TILE ? 1 : 2;
     const int t1 = g.t1;
     int k = g.t0, v = k;
@@ -273,11 +261,15 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sh.s_full[i]), 1);
-            mbar_init(smem_u32(&sh.p_full[i]), 4);
+            mbar_init(smem_u32(&sh.p_full[i]), 8);
         }
         mbar_init(smem_u32(&sh.o_full), 1);
-        mbar_init(smem_u32(&sh.q_full), 8);
-        mbar_init(smem_u32(&sh.xch), 128);
+        mbar_init(smem_u32(&sh.q_full), SOFTMAX_WARPS);
+        mbar_init(smem_u32(&sh.xch), SOFTMAX_WARPS / 2);
+        for (int i = 0; i < SEGMENTS; ++i) {
+            mbar_init(smem_u32(&sh.seg_full[i]), 1);
+            mbar_init(smem_u32(&sh.seg_empty[i]), SOFTMAX_WARPS + LOADER_WARPS + 2);
+        }
         for (int i = 0; i < 16; ++i) sh.nonfinite[i] = 0;
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -287,98 +279,60 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         tmem_relinquish();
     }
     if (warp == TMA_WARP && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? &tm_v : &tm_k)) : "memory");
-    grid_dependency_wait();
-    // ---------------------------------------------------------------- this CTA's range of key tiles
-    if (warp == 0) {
-        int len, live, np;
-        const int n_first = lane < a.S ? sequence_tiles(a, lane, len, live, np) : 0;
-        long long sum = n_first;
-        for (int s = lane + 32; s < a.S; s += 32) sum += sequence_tiles(a, s, len, live, np);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        const long long per_pass = sum * cache.heads, total = per_pass * p.passes;
-        const long long n_groups = groups_used(p, total), group = min((long long)(blockIdx.x / p.side), n_groups);
-        const long long lo = total ? group * total / n_groups : 0, hi = group < n_groups ? (group + 1) * total / n_groups : lo;
-        const int pass = per_pass ? (int)(lo / per_pass) : 0;
-        const long long x = lo - pass * per_pass;  // < per_pass
-        if (lane == 0) {
-            sh.lo = lo;
-            sh.hi = hi;
-            sh.pass = pass;
-            sh.s = 0;
-            sh.h = 0;
-            sh.t = 0;
-        }
-        __syncwarp();
-        long long before = 0;
-        for (int s0 = 0; s0 < a.S; s0 += 32) {
-            const int s = s0 + lane;
-            const int n = s0 == 0 ? n_first : (s < a.S ? sequence_tiles(a, s, len, live, np) : 0);
-            long long upto = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long other = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += other;
-            }
-            upto += before;
-            if (blockIdx.x == 0 && s < a.S) {
-                p.cum[s + 1] = upto;
-                if (s == 0) p.cum[0] = 0;
-                if (a.len[s] < 0 || (long long)a.len[s] > ((long long)cache.max_pages << cache.page_shift)) atomicOr(a.status, SPEC_STATUS_CAPACITY);
-            }
-            const long long from = (upto - n) * cache.heads;
-            if (n > 0 && lo < hi && x >= from && x < upto * cache.heads) {
-                sh.s = s;
-                sh.h = (int)((x - from) / n);
-                sh.t = (int)((x - from) % n);
-            }
-            before = __shfl_sync(0xffffffffu, upto, 31);
-            if (blockIdx.x != 0 && before * cache.heads > x) break;
-        }
-    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (threadIdx.x == 0) grid_launch_dependents();
+    grid_dependency_wait();
     const uint32_t tmem = sh.tmem;
     const uint32_t full = smem_u32(&sh.full[0]), empty = smem_u32(&sh.empty[0]), go = smem_u32(&sh.go[0]), stg_full = smem_u32(&sh.stg_full[0]), stg_empty = smem_u32(&sh.stg_empty[0]);
     const uint32_t s_full = smem_u32(&sh.s_full[0]), p_full = smem_u32(&sh.p_full[0]), o_full = smem_u32(&sh.o_full), q_full = smem_u32(&sh.q_full);
-    const uint32_t xch_bar = smem_u32(&sh.xch);
-    auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, p.wait_limit_ns); };
-    Walk& g = sh.walk[min(warp, MMA_WARP)];
-    auto next = [&]() {  // the warp's next segment
-        __syncwarp();
-        if (lane == 0) advance(p, g);
-        __syncwarp();
-        return g.more != 0;
+    const uint32_t xch_bar = smem_u32(&sh.xch), seg_full = smem_u32(&sh.seg_full[0]), seg_empty = smem_u32(&sh.seg_empty[0]);
+    // Bounded.  Once a wait has expired, every other gives up at once.
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*abort_flag) return false;
+        return mbar_wait(bar, parity, abort_flag, p.wait_limit_ns);
     };
-    if (lane == 0 && warp <= MMA_WARP) start_walk(g, sh);
+    uint32_t n_seg = 0;  // segments that this warp has been through
+    auto segment = [&]() -> const Segment& { return sh.segment[n_seg % SEGMENTS]; };
+    auto segment_there = [&]() { return wait(seg_full + 8 * (n_seg % SEGMENTS), (n_seg / SEGMENTS) & 1u); };
+    auto segment_done = [&]() {  // by one lane, after the warp's last look at it
+        mbar_arrive(seg_empty + 8 * (n_seg % SEGMENTS));
+    };
 
     if (warp < SOFTMAX_WARPS) {
         // ------------------------------------------------------------------------------------ softmax
         set_regs_up<REGS_SOFTMAX>();
-        // (a warp gives up as a whole: what follows a wait is collective)
-        auto warp_wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
-        const int stream = warp >> 2, wq = warp & 3;
+        const int stream = warp >> 3, half = (warp >> 2) & 1, wq = warp & 3;
         const uint32_t lanes = tmem + ((uint32_t)(wq * 32) << 16);
         const uint32_t s_tm = lanes + stream * TILE, o_tm = lanes + 2 * TILE + stream * TILE;
-        uint32_t n_s = 0, n_seg = 0, n_xch = 0;  // tiles of this stream, segments, exchanges so far
-        bool ok = true;
-        while (ok && next()) {
+        // The two warps of the same rows meet at a barrier of their own, with a vote.  They go through the same number of
+        // meetings whatever happens: a wait that has expired is passed over, and the end is decided together.
+        auto meet = [&](bool vote) {
+            int r;
+            asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %2, 0;\n bar.red.or.pred q, %1, 64, p;\n selp.b32 %0, 1, 0, q;\n}\n" : "=r"(r) : "r"(1 + stream * 4 + wq), "r"((int)vote) : "memory");
+            return r != 0;
+        };
+        uint32_t n_s = 0, n_xch = 0;  // tiles of this stream, exchanges so far
+        for (;; ++n_seg) {
+            const bool there = __all_sync(0xffffffffu, segment_there());
+            const Segment& g = segment();
+            if (meet(!there || !g.more)) break;
             const bool split = g.rows <= TILE;  // the streams split the keys
             const int tile_row = (split ? 0 : stream * TILE) + wq * 32 + lane;
             const bool valid = tile_row < g.rows;
             const bool warp_on = (split ? 0 : stream * TILE) + wq * 32 < g.rows;
-            // ---- queries into shared memory (once: by stream 0 if both read the same rows)
+            // ---- queries into shared memory (once: by stream 0 if both read the same rows), 16 rows by each warp
             if (!split || stream == 0) {
                 constexpr int LPR = D / 8, RPI = 32 / LPR;  // lanes per row, rows per instruction
                 const int R = g.qt * 2 * TILE + tile_row, node = R / p.G, gq = R - node * p.G;
                 const long long off = valid ? ((long long)g.s * a.N + node) * a.q_tok + (long long)(g.h * p.G + gq) * a.q_head : -1;
                 const uint32_t dst = q_at + stream * Geo::TILE_BYTES;
                 const int c = lane % LPR;
-#pragma unroll 8
-                for (int i = 0; i < LPR; ++i) {
-                    const int r = i * RPI + lane / LPR;
+#pragma unroll
+                for (int i = 0; i < 16 / RPI; ++i) {
+                    const int r = half * 16 + i * RPI + lane / LPR;
                     const long long o = __shfl_sync(0xffffffffu, off, r);
                     uint4 v = make_uint4(0, 0, 0, 0);
                     if (o >= 0) v = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + c * 8);
@@ -389,107 +343,114 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full);
             // ---- key tiles
-            float m = -INFINITY, l = 0.0f;
+            float m = -INFINITY, l = 0.0f;  // m: the same in both threads of a row; l: this thread's columns
             const int step = split ? 2 : 1;
             for (int t = g.t0 + (split ? stream : 0); t < g.t1; t += step) {
-                if (!(ok = warp_wait(s_full + 8 * stream, n_s & 1u))) break;
+                wait(s_full + 8 * stream, n_s & 1u);
                 ++n_s;
+                __syncwarp();
                 tc_fence_after();
                 if (warp_on) {
                     const int valid_keys = t < g.n_prefix ? g.len - t * TILE : g.live - (t - g.n_prefix) * TILE;
                     const bool masked = t >= g.n_prefix || valid_keys < TILE;
-                    auto seen = [&](int i) {  // which of scores [32 i, 32 i + 32) this row has
-                        const int left = valid_keys - 32 * i;
-                        uint32_t w = left >= 32 ? 0xFFFFFFFFu : (left <= 0 ? 0u : (1u << left) - 1u);
-                        if (t >= g.n_prefix) {
-                            const int words = (a.N + 31) / 32, at = (t - g.n_prefix) * 4 + i, node = (g.qt * 2 * TILE + tile_row) / p.G;
-                            w &= (valid && at < words) ? (uint32_t)a.mask[((long long)g.s * a.N + node) * words + at] : 0u;
-                        }
-                        return w;
-                    };
-                    // 32 scores at a time, the next 32 on their way, in a loop that stays in the instruction cache (with all 128
-                    // unrolled, fetching instructions cost more than the exponentials).  The reference m is a score of the row
-                    // that was the largest of its 32 when it was taken; it stays until 32 weights add up to more than
-                    // RESCALE (or to no number, as for a row without a reference), which is when their maximum is looked for.
-                    auto scale_sums = [&](float f) {  // O, of this warp's rows
-#pragma unroll 1
-                        for (int i = 0; i < D; i += 16) {
-                            uint32_t o[16];
-                            tmem_ld16(o_tm + i, o);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                            tmem_st16(o_tm + i, o);
-                        }
-                    };
-                    auto chunk = [&](int i, uint32_t(&x)[32]) {
-                        if (masked) hide(x, seen(i));
-                        uint32_t w[16];
-                        float sum = weights32(x, p.c, m * p.c, w);
-                        const bool move = !(sum <= RESCALE);
-                        if (__any_sync(0xffffffffu, move)) {
-                            const float top = fmaxf(m, max32(x));
-                            const float f = move && top > m ? exp2_approx((m - top) * p.c) : 1.0f;
-                            if (move) m = top;
-                            l *= f;
-                            if (t >= g.t0 + step) scale_sums(f);
-#pragma unroll 1
-                            for (int k = 0; k < i; ++k) {  // this tile's weights so far
-                                uint32_t v[16];
-                                tmem_ld16(s_tm + 16 * k, v);
-                                tmem_wait_ld();
-                                const uint32_t f2 = pack2(f, f);  // (1, or below 2^-3: its rounding counts for little)
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) v[j] = mul_bf16x2(v[j], f2);
-                                tmem_st16(s_tm + 16 * k, v);
+                    auto load = [&](int i, uint32_t(&x)[32]) {  // scores [32 i, 32 i + 32) of the row, -inf where it has none
+                        tmem_ld32(s_tm + 32 * i, x);
+                        tmem_wait_ld();
+                        if (masked) {
+                            const int left = valid_keys - 32 * i;
+                            uint32_t seen = left >= 32 ? 0xFFFFFFFFu : (left <= 0 ? 0u : (1u << left) - 1u);
+                            if (t >= g.n_prefix) {
+                                const int words = (a.N + 31) / 32, at = (t - g.n_prefix) * 4 + i, node = (g.qt * 2 * TILE + tile_row) / p.G;
+                                seen &= (valid && at < words) ? (uint32_t)a.mask[((long long)g.s * a.N + node) * words + at] : 0u;
                             }
-                            sum = weights32(x, p.c, m == -INFINITY ? 0.0f : m * p.c, w);
+                            hide(x, seen);
                         }
-                        l += sum;
-                        tmem_st16(s_tm + 16 * i, w);
                     };
-                    uint32_t x[32], y[32];
-                    tmem_ld32(s_tm, x);
-                    tmem_wait_ld();
+                    uint32_t w[2][16];
+                    float sum[2];
+                    auto weigh = [&](float mc) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            uint32_t x[32];
+                            load(2 * half + i, x);
+                            sum[i] = weights32(x, p.c, mc, w[i]);
+                        }
+                    };
+                    // The reference m is a score of the row that was the largest when it was taken.  It stays until some 32
+                    // weights add up to more than RESCALE (or to no number, as for a row without a reference): only then is
+                    // the maximum looked for, by both threads over the whole row.
+                    weigh(m * p.c);
+                    if (meet(!(sum[0] <= RESCALE && sum[1] <= RESCALE))) {
+                        float top = -INFINITY;
 #pragma unroll 1
-                    for (int i = 0; i < 4; i += 2) {
-                        tmem_ld32(s_tm + 32 * (i + 1), y);
-                        chunk(i, x);
-                        tmem_wait_ld();
-                        if (i == 0) tmem_ld32(s_tm + 64, x);
-                        chunk(i + 1, y);
-                        tmem_wait_ld();
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t x[32];
+                            load(i, x);
+                            top = fmaxf(top, max32(x));
+                        }
+                        const bool move = top > m && !((top - m) * p.c <= 1.0f);
+                        const float f = move ? exp2_approx((m - top) * p.c) : 1.0f;
+                        if (move) m = top;
+                        l *= f;
+                        if (t >= g.t0 + step && __any_sync(0xffffffffu, move)) {  // this warp's half of O's columns
+#pragma unroll 1
+                            for (int i = half * (D / 2); i < (half + 1) * (D / 2); i += 16) {
+                                uint32_t o[16];
+                                tmem_ld16(o_tm + i, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                tmem_st16(o_tm + i, o);
+                            }
+                        }
+                        weigh(m == -INFINITY ? 0.0f : m * p.c);
+                        meet(false);
                     }
+                    // (the other warp has read its scores, which these weights overwrite in part)
+                    l += sum[0] + sum[1];
+                    tmem_st16(s_tm + 32 * half, w[0]);
+                    tmem_st16(s_tm + 32 * half + 16, w[1]);
                     tmem_wait_st();
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full + 8 * stream);
             }
-            if (!ok) break;
             // ---- results
-            if (!(ok = warp_wait(o_full, n_seg & 1u))) break;
+            wait(o_full, n_seg & 1u);
+            __syncwarp();
             tc_fence_after();
+            // sums and references change hands through the lanes' own columns of the scores, which are done with
             float f0 = 1.0f, f1 = 0.0f;
             const bool both = split && g.t1 - g.t0 > 1;  // stream 1 had a tile
+            if (warp_on && (stream == 0 || !split || both)) {
+                tmem_st1(s_tm + half, __float_as_uint(l));
+                tmem_st1(s_tm + 2, __float_as_uint(m));
+                tmem_wait_st();
+                tc_fence_before();
+                meet(false);
+                tc_fence_after();
+                const uint32_t other = tmem_ld1(s_tm + 1 - half);
+                tmem_wait_ld();
+                l += __uint_as_float(other);
+            }
             if (both) {
                 if (stream == 1) {
-                    // through the lanes' own columns of stream 1's scores, which are done with
-                    tmem_st1(s_tm, __float_as_uint(m));
-                    tmem_st1(s_tm + 1, __float_as_uint(l));
-                    tmem_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(xch_bar);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(xch_bar);
                 } else {
-                    if (!(ok = warp_wait(xch_bar, n_xch & 1u))) break;
+                    wait(xch_bar, n_xch & 1u);
+                    __syncwarp();
                     tc_fence_after();
-                    const uint32_t m1 = tmem_ld1(s_tm + TILE), l1 = tmem_ld1(s_tm + TILE + 1);
-                    tmem_wait_ld();
-                    const float other = __uint_as_float(m1), top = fmaxf(m, other);
-                    f0 = m == -INFINITY ? 0.0f : exp2_approx((m - top) * p.c);
-                    f1 = other == -INFINITY ? 0.0f : exp2_approx((other - top) * p.c);
-                    l = l * f0 + __uint_as_float(l1) * f1;
-                    m = top;
+                    if (warp_on) {
+                        const uint32_t la = tmem_ld1(s_tm + TILE), lb = tmem_ld1(s_tm + TILE + 1), m1 = tmem_ld1(s_tm + TILE + 2);
+                        tmem_wait_ld();
+                        const float other = __uint_as_float(m1), top = fmaxf(m, other);
+                        f0 = m == -INFINITY ? 0.0f : exp2_approx((m - top) * p.c);
+                        f1 = other == -INFINITY ? 0.0f : exp2_approx((other - top) * p.c);
+                        l = l * f0 + (__uint_as_float(la) + __uint_as_float(lb)) * f1;
+                        m = top;
+                    }
                 }
                 ++n_xch;
             }
@@ -500,7 +461,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 const long long out_row = ((long long)g.s * a.N + node) * a.Hq + g.h * p.G + gq;
                 const long long part = ((long long)blockIdx.x * 2 + g.slot) * p.rows_cap + tile_row;
 #pragma unroll 1
-                for (int i = 0; i < D / 32; ++i) {
+                for (int i = half * (D / 64); i < (half + 1) * (D / 64); ++i) {  // this warp's half of the columns
                     uint32_t o[32];
                     float x[32];
                     tmem_ld32(o_tm + 32 * i, o);
@@ -542,22 +503,26 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                         }
                     }
                 }
-                if (valid) {
+                if (valid && half == 0) {
                     if (!g.whole) p.part_ml[part] = make_float2(m, l);
                     else if (a.lse) a.lse[out_row] = l == 0.0f ? -INFINITY : (m * p.c + log2f(l)) * LN2;
                 }
             }
             tc_fence_before();
-            ++n_seg;
+            __syncwarp();
+            if (lane == 0) segment_done();
         }
     } else if (warp < SOFTMAX_WARPS + LOADER_WARPS) {
         // ------------------------------------------------------------------------------------ tiles written by threads
         set_regs_down<REGS_LOADER>();
-        const int tid = threadIdx.x - 256;
+        const int tid = threadIdx.x - 32 * SOFTMAX_WARPS;
         constexpr int CH = D / 8;  // 16-byte chunks of a bf16 vector
-        uint32_t slot = 0, phase = 0, stg = 0, stg_phase = 0, n_seg = 0;
+        uint32_t slot = 0, phase = 0, stg = 0, stg_phase = 0;
         uint32_t go_phase = 0;  // bit per slot
-        while (next()) {
+        for (;; ++n_seg) {
+            if (!segment_there()) break;
+            const Segment& g = segment();
+            if (!g.more) break;
             const bool ok = for_each_tile(g, [&](bool is_v, int t) {
                 const bool block = t >= g.n_prefix;
                 const uint32_t dst = ring_at + slot * Geo::TILE_BYTES, bar_full = full + 8 * slot, bar_empty = empty + 8 * slot;
@@ -649,7 +614,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 return true;
             });
             if (!ok) break;
-            ++n_seg;
+            __syncwarp();
+            if (lane == 0) segment_done();
         }
     } else {
         set_regs_down<REGS_CONTROL>();
@@ -661,7 +627,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             const int page = 1 << cache.page_shift, per_tile = TILE >> cache.page_shift;
             const int all_rows = (cache.n_pages * cache.heads) << cache.page_shift;  // a coordinate beyond the cache: reads as 0
             bool ok = true;
-            while (ok && next()) {
+            for (;; ++n_seg) {
+                ok = __all_sync(0xffffffffu, segment_there());
+                const Segment& g = segment();
+                if (!ok || !g.more) break;
                 const int32_t* table = cache.table + (long long)g.s * cache.max_pages;
                 const int n_pages = (g.len + page - 1) >> cache.page_shift;
                 // (the pages of a tile's K serve its V one or two tiles later: kept in two registers, by the tile's parity)
@@ -724,6 +693,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     ++issued;
                     return true;
                 });
+                if (!ok) break;
+                __syncwarp();
+                if (lane == 0) segment_done();
             }
             if (!ok && lane == 0) {  // give copies in flight a bounded chance to land before the CTA exits
                 const uint64_t until = global_timer_ns() + 1000000ull;
@@ -733,7 +705,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             // -------------------------------------------------------------------------------- products
             const uint32_t id_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
             const uint32_t id_pv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
-            uint32_t slot = 0, phase = 0, n_seg = 0, n_p[2] = {0, 0};
+            uint32_t slot = 0, phase = 0, n_p[2] = {0, 0};
             bool ok = true;
             auto take = [&](uint32_t& at, uint32_t& index) {  // the next tile of the ring, once it is there
                 index = slot;
@@ -764,8 +736,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
 #pragma unroll
                 for (int k = 0; k < TILE / 16; ++k) tc_mma_bf16_ts(d, w + 8 * k, vd + k * (2048 >> 4), id_pv, (add || k != 0) ? 1u : 0u);
             };
-            while (ok) {
-                advance(p, g);
+            for (;; ++n_seg) {
+                if (!segment_there()) break;
+                const Segment& g = segment();
                 if (!g.more) break;
                 const int n = g.t1 - g.t0;
                 uint32_t k_at, v_at, ki, vi;
@@ -816,7 +789,65 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 }
                 if (!ok) break;
                 tc_commit(o_full);
-                ++n_seg;
+                segment_done();
+            }
+        } else if (warp == PLAN_WARP) {
+            // -------------------------------------------------------------------------------- this CTA's range of key tiles
+            int len, live, np;
+            const int n_first = lane < a.S ? sequence_tiles(a, lane, len, live, np) : 0;
+            long long sum = n_first;
+            for (int s = lane + 32; s < a.S; s += 32) sum += sequence_tiles(a, s, len, live, np);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            const long long per_pass = sum * cache.heads, total = per_pass * p.passes;
+            const long long n_groups = groups_used(p, total), group = min((long long)(blockIdx.x / p.side), n_groups);
+            Walk w;
+            w.pos = total ? group * total / n_groups : 0;
+            w.hi = group < n_groups ? (group + 1) * total / n_groups : w.pos;
+            w.pass = per_pass ? (int)(w.pos / per_pass) : 0;
+            w.slot = 0;
+            const long long x = w.pos - w.pass * per_pass;  // < per_pass
+            int mine = 0;  // the lane whose sequence the range starts in has its place
+            long long before = 0;
+            for (int s0 = 0; s0 < a.S; s0 += 32) {
+                const int s = s0 + lane;
+                const int n = s0 == 0 ? n_first : (s < a.S ? sequence_tiles(a, s, len, live, np) : 0);
+                long long upto = n;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const long long other = __shfl_up_sync(0xffffffffu, upto, o);
+                    if (lane >= o) upto += other;
+                }
+                upto += before;
+                if (blockIdx.x == 0 && s < a.S) {
+                    p.cum[s + 1] = upto;
+                    if (s == 0) p.cum[0] = 0;
+                    if (a.len[s] < 0 || (long long)a.len[s] > ((long long)cache.max_pages << cache.page_shift)) atomicOr(a.status, SPEC_STATUS_CAPACITY);
+                }
+                const long long from = (upto - n) * cache.heads;
+                if (n > 0 && x >= from && x < upto * cache.heads) {
+                    mine = 1;
+                    w.s = s;
+                    w.h = (int)((x - from) / n);
+                    w.t = (int)((x - from) % n);
+                }
+                before = __shfl_sync(0xffffffffu, upto, 31);
+                if (blockIdx.x != 0 && before * cache.heads > x) break;
+            }
+            const unsigned who = __ballot_sync(0xffffffffu, mine);
+            const int src = who ? __ffs(who) - 1 : 0;
+            w.s = __shfl_sync(0xffffffffu, w.s, src);
+            w.h = __shfl_sync(0xffffffffu, w.h, src);
+            w.t = __shfl_sync(0xffffffffu, w.t, src);
+            if (lane == 0) {
+                for (uint32_t k = 0;; ++k) {
+                    if (!wait(seg_empty + 8 * (k % SEGMENTS), ((k / SEGMENTS) & 1u) ^ 1u)) break;
+                    Segment& g = sh.segment[k % SEGMENTS];
+                    advance(p, w, g);
+                    const int more = g.more;
+                    mbar_arrive(seg_full + 8 * (k % SEGMENTS));
+                    if (!more) break;
+                }
             }
         }
     }
