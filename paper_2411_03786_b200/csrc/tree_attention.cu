@@ -539,18 +539,23 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     const uint32_t src = stg_at + stg * Geo::STAGE_BYTES, ex = exp_at + stg * TILE;
                     constexpr int LPR = D / 16;
                     const bool swap = (tid & 4) != 0 && D == 128;  // so that the 8 lanes of a phase write to different banks
+                    constexpr int PER = TILE * LPR / LOADERS;
+                    const int c = tid % LPR;
+                    uint4 v[PER];
+                    uint32_t e[PER];
 #pragma unroll
-                    for (int i = 0; i < TILE * LPR / LOADERS; ++i) {
-                        const int r = i * (LOADERS / LPR) + tid / LPR, c = tid % LPR;
-                        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-                        if (r < rows) {
-                            const uint4 v = ld_shared16(src + r * D + c * 16);
-                            uint32_t e;
-                            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e) : "r"(ex + r) : "memory");
-                            const uint32_t f = scale_bf16x2(e);
-                            lo = make_uint4(e4m3x2_bf16x2<0x1404>(v.x, f), e4m3x2_bf16x2<0x3424>(v.x, f), e4m3x2_bf16x2<0x1404>(v.y, f), e4m3x2_bf16x2<0x3424>(v.y, f));
-                            hi = make_uint4(e4m3x2_bf16x2<0x1404>(v.z, f), e4m3x2_bf16x2<0x3424>(v.z, f), e4m3x2_bf16x2<0x1404>(v.w, f), e4m3x2_bf16x2<0x3424>(v.w, f));
-                        }
+                    for (int i = 0; i < PER; ++i) {
+                        const int r = i * (LOADERS / LPR) + tid / LPR;
+                        v[i] = ld_shared16(src + r * D + c * 16);
+                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e[i]) : "r"(ex + r) : "memory");
+                    }
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) {
+                        const int r = i * (LOADERS / LPR) + tid / LPR;
+                        const uint32_t f = scale_bf16x2(e[i]);
+                        uint4 lo = make_uint4(e4m3x2_bf16x2<0x1404>(v[i].x, f), e4m3x2_bf16x2<0x3424>(v[i].x, f), e4m3x2_bf16x2<0x1404>(v[i].y, f), e4m3x2_bf16x2<0x3424>(v[i].y, f));
+                        uint4 hi = make_uint4(e4m3x2_bf16x2<0x1404>(v[i].z, f), e4m3x2_bf16x2<0x3424>(v[i].z, f), e4m3x2_bf16x2<0x1404>(v[i].w, f), e4m3x2_bf16x2<0x3424>(v[i].w, f));
+                        if (r >= rows) lo = hi = make_uint4(0, 0, 0, 0);  // (whatever the staging tile held)
                         st_shared16(dst + tile_at(r, 2 * c + (swap ? 1 : 0)), swap ? hi : lo);
                         st_shared16(dst + tile_at(r, 2 * c + (swap ? 0 : 1)), swap ? lo : hi);
                     }
@@ -621,7 +626,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         set_regs_down<REGS_CONTROL>();
         if (warp == TMA_WARP) {
             // -------------------------------------------------------------------------------- TMA
-            // A lane fetches one page's part of a tile; page numbers are read a tile ahead.
+            // A lane fetches one page's part of a tile.  Page numbers are read 32 at a time, a window ahead of their use (two
+            // registers, by the window's parity: a load is never waited for where it is issued).
             uint32_t slot = 0, phase = 0, issued = 0;
             constexpr uint32_t RING = Q8 ? Geo::STAGES : Geo::SLOTS;
             const int page = 1 << cache.page_shift, per_tile = TILE >> cache.page_shift;
@@ -633,14 +639,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 if (!ok || !g.more) break;
                 const int32_t* table = cache.table + (long long)g.s * cache.max_pages;
                 const int n_pages = (g.len + page - 1) >> cache.page_shift;
-                // (the pages of a tile's K serve its V one or two tiles later: kept in two registers, by the tile's parity)
-                auto fetch = [&](int t) {
-                    const int i = t * per_tile + lane;
-                    return lane < per_tile && i < n_pages && t < g.n_prefix ? table[i] : 0;
-                };
-                int pg[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) pg[i] = fetch(g.t0 + i);  // pg[i]: tile t0 + i (mod 4)
+                const int wsh = cache.page_shift - 2, in_window = (1 << wsh) - 1;  // tiles of a window: 4 to 32
+                auto fetch = [&](int window) { return window * 32 + lane < n_pages ? table[window * 32 + lane] : 0; };
+                const int w0 = g.t0 >> wsh;
+                int even = fetch(w0 + (w0 & 1)), odd = fetch(w0 + 1 - (w0 & 1));
                 ok = for_each_tile(g, [&](bool is_v, int t) {
                     const bool block = t >= g.n_prefix;
                     const int rows = block ? 0 : g.len - t * TILE;
@@ -655,14 +657,11 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                             phase ^= 1u;
                         }
                     }
-                    const int k4 = (t - g.t0) & 3;
-                    const int pid = k4 == 0 ? pg[0] : (k4 == 1 ? pg[1] : (k4 == 2 ? pg[2] : pg[3]));
-                    if (is_v) {  // the tile's last use of its page numbers
-                        const int ahead = fetch(t + 4);
-                        if (k4 == 0) pg[0] = ahead;
-                        else if (k4 == 1) pg[1] = ahead;
-                        else if (k4 == 2) pg[2] = ahead;
-                        else pg[3] = ahead;
+                    const int window = t >> wsh;
+                    const int pid = __shfl_sync(0xffffffffu, (window & 1) ? odd : even, ((t & in_window) << (7 - cache.page_shift)) + (lane & (per_tile - 1)));
+                    if (is_v && t > g.t0 && (t & in_window) == 0) {  // values, which come last, have left the window before
+                        if (window & 1) even = fetch(window + 1);
+                        else odd = fetch(window + 1);
                     }
                     if (Q8 && !mine) return true;
                     const bool got = wait(bar_empty, my_phase ^ 1u);
