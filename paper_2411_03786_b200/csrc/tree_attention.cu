@@ -54,7 +54,7 @@ struct AttParams {
     float c;                                  // scale * log2(e)
     long long* cum;                           // [S + 1] key tiles of the sequences before
     float2* part_ml;                          // [grid * 2, rows_cap]
-    float* part_o;                            // [grid * 2, rows_cap, D]
+    float* part_o;                            // [grid * 2, D / 4, rows_cap, 4]
     unsigned long long wait_limit_ns;
 };
 
@@ -330,14 +330,15 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 const long long off = valid ? ((long long)g.s * a.N + node) * a.q_tok + (long long)(g.h * p.G + gq) * a.q_head : -1;
                 const uint32_t dst = q_at + stream * Geo::TILE_BYTES;
                 const int c = lane % LPR;
+                uint4 v[16 / RPI];
 #pragma unroll
                 for (int i = 0; i < 16 / RPI; ++i) {
-                    const int r = half * 16 + i * RPI + lane / LPR;
-                    const long long o = __shfl_sync(0xffffffffu, off, r);
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (o >= 0) v = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + c * 8);
-                    st_shared16(dst + tile_at(wq * 32 + r, c), v);
+                    const long long o = __shfl_sync(0xffffffffu, off, half * 16 + i * RPI + lane / LPR);
+                    v[i] = make_uint4(0, 0, 0, 0);
+                    if (o >= 0) v[i] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + c * 8);
                 }
+#pragma unroll
+                for (int i = 0; i < 16 / RPI; ++i) st_shared16(dst + tile_at(wq * 32 + half * 16 + i * RPI + lane / LPR, c), v[i]);
                 fence_async_smem();
             }
             __syncwarp();
@@ -459,7 +460,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 const bool poisoned = sh.nonfinite[n_seg & 15u] == (int)n_seg + 1;
                 const float inv = g.whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
                 const long long out_row = ((long long)g.s * a.N + node) * a.Hq + g.h * p.G + gq;
-                const long long part = ((long long)blockIdx.x * 2 + g.slot) * p.rows_cap + tile_row;
+                const long long part = (long long)blockIdx.x * 2 + g.slot;
 #pragma unroll 1
                 for (int i = half * (D / 64); i < (half + 1) * (D / 64); ++i) {  // this warp's half of the columns
                     uint32_t o[32];
@@ -489,22 +490,35 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                             }
                         }
                     }
-                    if (valid) {
-                        if (g.whole) {
-                            uint4* dst = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + out_row * D + 32 * i);
+                    if (g.whole) {  // into the row's place in the query tile, which is done with
+                        const uint32_t dst = q_at + stream * Geo::TILE_BYTES;
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                dst[j] = make_uint4(pack2(x[8 * j] * inv, x[8 * j + 1] * inv), pack2(x[8 * j + 2] * inv, x[8 * j + 3] * inv),
-                                                    pack2(x[8 * j + 4] * inv, x[8 * j + 5] * inv), pack2(x[8 * j + 6] * inv, x[8 * j + 7] * inv));
-                        } else {
-                            float4* dst = reinterpret_cast<float4*>(p.part_o + part * D + 32 * i);
+                        for (int j = 0; j < 4; ++j)
+                            st_shared16(dst + tile_at(wq * 32 + lane, 4 * i + j),
+                                        make_uint4(pack2(x[8 * j] * inv, x[8 * j + 1] * inv), pack2(x[8 * j + 2] * inv, x[8 * j + 3] * inv),
+                                                   pack2(x[8 * j + 4] * inv, x[8 * j + 5] * inv), pack2(x[8 * j + 6] * inv, x[8 * j + 7] * inv)));
+                    } else if (valid) {  // four columns of neighbouring rows side by side
+                        float4* dst = reinterpret_cast<float4*>(p.part_o) + (part * (D / 4) + 8 * i) * p.rows_cap + tile_row;
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) dst[j] = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
-                        }
+                        for (int j = 0; j < 8; ++j) dst[(long long)j * p.rows_cap] = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+                    }
+                }
+                if (g.whole) {  // rows of the output from there, a 128-byte line (D = 64: half of one) by neighbouring lanes
+                    constexpr int LPR = D / 16, RPI = 32 / LPR;  // lanes that share a row of this warp's columns, rows per instruction
+                    const long long off = valid ? out_row * D : -1;
+                    const uint32_t src = q_at + stream * Geo::TILE_BYTES;
+                    const int c = half * LPR + lane % LPR;
+                    __syncwarp();
+#pragma unroll
+                    for (int r0 = 0; r0 < 32; r0 += RPI) {
+                        const int r = r0 + lane / LPR;
+                        const long long o = __shfl_sync(0xffffffffu, off, r);
+                        const uint4 v = ld_shared16(src + tile_at(wq * 32 + r, c));
+                        if (o >= 0) *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + o + c * 8) = v;
                     }
                 }
                 if (valid && half == 0) {
-                    if (!g.whole) p.part_ml[part] = make_float2(m, l);
+                    if (!g.whole) p.part_ml[part * p.rows_cap + tile_row] = make_float2(m, l);
                     else if (a.lse) a.lse[out_row] = l == 0.0f ? -INFINITY : (m * p.c + log2f(l)) * LN2;
                 }
             }
@@ -857,70 +871,70 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
 }
 
 // Joins the partial rows of every (s, h, row-tile pair) whose key tiles were spread over several CTAs, in the CTAs'
-// order, and writes the rows that attend to nothing.  A warp per row.
-constexpr int JOIN_ROWS = 8;
+// order, and writes the rows that attend to nothing.  A lane per row, 16 columns per warp.
 template <int D>
-__global__ void __launch_bounds__(32 * JOIN_ROWS) join_kernel(const __grid_constant__ AttParams p) {
-    constexpr int E = D / 32;
+__global__ void __launch_bounds__(2 * D) join_kernel(const __grid_constant__ AttParams p) {
     const TreeAttnArgs& a = p.a;
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, cols = threadIdx.x >> 5;  // columns [16 cols, 16 cols + 16)
     grid_launch_dependents();
     grid_dependency_wait();
     const int s = (int)(blockIdx.x / a.cache.heads), h = (int)(blockIdx.x % a.cache.heads), qt = blockIdx.y;
-    const int r = blockIdx.z * JOIN_ROWS + (threadIdx.x >> 5);
-    if (r >= min(2 * TILE, a.N * p.G - qt * 2 * TILE)) return;
+    const int r = blockIdx.z * 32 + lane;
     int len, live, np;
     const int tiles = sequence_tiles(a, s, len, live, np);
+    const long long per_pass = p.cum[a.S] * a.cache.heads, total = per_pass * p.passes, n_groups = groups_used(p, total);
+    if (r >= min(2 * TILE, a.N * p.G - qt * 2 * TILE)) return;
     const int R = qt * 2 * TILE + r, node = R / p.G, gq = R - node * p.G;
     const long long out_row = ((long long)s * a.N + node) * a.Hq + h * p.G + gq;
-    __nv_bfloat16* out = (__nv_bfloat16*)a.out + out_row * D + lane * E;
+    uint4* out = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + out_row * D + 16 * cols);
     if (node >= live) {
-#pragma unroll
-        for (int j = 0; j < E; ++j) out[j] = __float2bfloat16_rn(0.0f);
-        if (a.lse && lane == 0) a.lse[out_row] = -INFINITY;
+        out[0] = out[1] = make_uint4(0, 0, 0, 0);
+        if (a.lse && cols == 0) a.lse[out_row] = -INFINITY;
         return;
     }
-    const long long per_pass = p.cum[a.S] * a.cache.heads, total = per_pass * p.passes, n_groups = groups_used(p, total);
     const long long u0 = (qt / p.side) * per_pass + p.cum[s] * a.cache.heads + (long long)h * tiles, u1 = u0 + tiles;
     // the groups whose ranges [g total / n, (g + 1) total / n) hold the first and the last tile
     const int g0 = (int)(((u0 + 1) * n_groups + total - 1) / total) - 1, g1 = (int)((u1 * n_groups + total - 1) / total) - 1;
     if (g0 == g1) return;
     // the first group's range may begin before u0: then its part is the one at the range's end
-    const long long at0 = (((long long)g0 * p.side + qt % p.side) * 2 + (u0 > g0 * total / n_groups ? 1 : 0)) * p.rows_cap + r;
-    const long long at1 = (((long long)(g0 + 1) * p.side + qt % p.side) * 2) * p.rows_cap + r, stride = (long long)p.side * 2 * p.rows_cap;
-    auto part = [&](int i) { return i == 0 ? at0 : at1 + (i - 1) * stride; };
+    const long long at0 = ((long long)g0 * p.side + qt % p.side) * 2 + (u0 > g0 * total / n_groups ? 1 : 0), at1 = ((long long)(g0 + 1) * p.side + qt % p.side) * 2;
+    auto part = [&](int i) { return i == 0 ? at0 : at1 + (long long)(i - 1) * p.side * 2; };
     const int n = g1 - g0 + 1;
-    float m = -INFINITY;
-    for (int i = lane; i < n; i += 32) m = fmaxf(m, p.part_ml[part(i)].x);
+    float m = -INFINITY, l = 0.0f, x[16];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    float l = 0.0f, x[E];
+    for (int j = 0; j < 16; ++j) x[j] = 0.0f;
+    for (int i0 = 0; i0 < n; i0 += 4) {  // four parts' loads in flight
+        float2 ml[4];
+        float4 o[4][4];
 #pragma unroll
-    for (int j = 0; j < E; ++j) x[j] = 0.0f;
-    for (int i0 = 0; i0 < n; i0 += 8) {  // eight parts' loads in flight
-        float2 ml[8];
-        float o[8][E];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             if (i0 + i >= n) continue;
             const long long at = part(i0 + i);
-            ml[i] = p.part_ml[at];
+            ml[i] = p.part_ml[at * p.rows_cap + r];
 #pragma unroll
-            for (int j = 0; j < E; ++j) o[i][j] = p.part_o[at * D + lane * E + j];
+            for (int j = 0; j < 4; ++j) o[i][j] = reinterpret_cast<const float4*>(p.part_o)[(at * (D / 4) + 4 * cols + j) * p.rows_cap + r];
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             if (i0 + i >= n) continue;
-            const float f = ml[i].x == -INFINITY ? 0.0f : exp2f((ml[i].x - m) * p.c);
-            l += ml[i].y * f;
+            const float top = fmaxf(m, ml[i].x), f0 = m == -INFINITY ? 0.0f : exp2f((m - top) * p.c), f = ml[i].x == -INFINITY ? 0.0f : exp2f((ml[i].x - top) * p.c);
+            m = top;
+            l = l * f0 + ml[i].y * f;
 #pragma unroll
-            for (int j = 0; j < E; ++j) x[j] += o[i][j] * f;
+            for (int j = 0; j < 4; ++j) {
+                x[4 * j] = x[4 * j] * f0 + o[i][j].x * f;
+                x[4 * j + 1] = x[4 * j + 1] * f0 + o[i][j].y * f;
+                x[4 * j + 2] = x[4 * j + 2] * f0 + o[i][j].z * f;
+                x[4 * j + 3] = x[4 * j + 3] * f0 + o[i][j].w * f;
+            }
         }
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-    for (int j = 0; j < E; ++j) out[j] = __float2bfloat16_rn(x[j] * inv);
-    if (a.lse && lane == 0) a.lse[out_row] = l == 0.0f ? -INFINITY : (m * p.c + log2f(l)) * LN2;
+    for (int j = 0; j < 2; ++j)
+        out[j] = make_uint4(pack2(x[8 * j] * inv, x[8 * j + 1] * inv), pack2(x[8 * j + 2] * inv, x[8 * j + 3] * inv),
+                            pack2(x[8 * j + 4] * inv, x[8 * j + 5] * inv), pack2(x[8 * j + 6] * inv, x[8 * j + 7] * inv));
+    if (a.lse && cols == 0) a.lse[out_row] = l == 0.0f ? -INFINITY : (m * p.c + log2f(l)) * LN2;
 }
 
 // ------------------------------------------------------------------------------------------ host
@@ -985,7 +999,7 @@ static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
     if (rc || (rc = cache_map(ctx, &tm_v, p.a.cache.v, p.a.cache))) return rc;
     cudaError_t e = launch_pdl(kernel, dim3(p.n_groups * p.side), dim3(ATT_THREADS), (size_t)Geometry<D, Q8>::SMEM, st, tm_k, tm_v, p);
     if ((rc = check_cuda(ctx, e, "spec_tree_attention launch"))) return rc;
-    e = launch_pdl(join_kernel<D>, dim3(p.a.S * p.a.cache.heads, p.n_qtiles, (p.rows_cap + JOIN_ROWS - 1) / JOIN_ROWS), dim3(32 * JOIN_ROWS), 0, st, p);
+    e = launch_pdl(join_kernel<D>, dim3(p.a.S * p.a.cache.heads, p.n_qtiles, (p.rows_cap + 31) / 32), dim3(2 * D), 0, st, p);
     ctx->launches += 2;
     return check_cuda(ctx, e, "spec_tree_attention join launch");
 }
