@@ -99,8 +99,25 @@ __device__ __forceinline__ int sequence_tiles(const TreeAttnArgs& a, int s, int&
     return live == 0 ? 0 : n_prefix + (live + TILE - 1) / TILE;
 }
 
-// Groups that get a range: with fewer tiles than groups, one tile each.
-__device__ __forceinline__ long long groups_used(const AttParams& p, long long total) { return min((long long)p.n_groups, total); }
+// Quotient of numbers that nearly always fit in 32 bits (a 64-bit division is a long subroutine).
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+// The tiles [0, total) in equal consecutive ranges: the first `rem` groups have base + 1, the others base.  With fewer
+// tiles than groups, as many groups as tiles have one.
+struct Ranges {
+    long long total, n, base, rem;
+    __device__ __forceinline__ Ranges(const AttParams& p, long long total_) : total(total_), n(min((long long)p.n_groups, total_)), base(0), rem(0) {
+        if (n) {
+            base = quotient(total, n);
+            rem = total - base * n;
+        }
+    }
+    __device__ __forceinline__ long long begin(long long g) const { return g * base + min(g, rem); }
+    __device__ __forceinline__ long long group_of(long long x) const {
+        return x < rem * (base + 1) ? quotient(x, base + 1) : rem + quotient(x - rem * (base + 1), base);
+    }
+};
 
 // The planning warp's place in the CTA's range.
 struct Walk {
@@ -367,45 +384,48 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                             hide(x, seen);
                         }
                     };
+                    // The reference m is a score of the row that was the largest when it was taken: in the first tile, and
+                    // again whenever some 32 weights add up to more than RESCALE (or to no number).  Only then is the
+                    // maximum looked for, by both threads over the whole row.
                     uint32_t w[2][16];
                     float sum[2];
-                    auto weigh = [&](float mc) {
+                    bool look = t < g.t0 + step;
+#pragma unroll 1
+                    for (;;) {
+                        if (look) {
+                            float top = -INFINITY;
+#pragma unroll 1
+                            for (int i = 0; i < 4; ++i) {
+                                uint32_t x[32];
+                                load(i, x);
+                                top = fmaxf(top, max32(x));
+                            }
+                            const bool move = top > m && !((top - m) * p.c <= 1.0f);
+                            const float f = move ? exp2_approx((m - top) * p.c) : 1.0f;
+                            if (move) m = top;
+                            l *= f;
+                            if (t >= g.t0 + step && __any_sync(0xffffffffu, move)) {  // this warp's half of O's columns
+#pragma unroll 1
+                                for (int i = half * (D / 2); i < (half + 1) * (D / 2); i += 16) {
+                                    uint32_t o[16];
+                                    tmem_ld16(o_tm + i, o);
+                                    tmem_wait_ld();
+#pragma unroll
+                                    for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                    tmem_st16(o_tm + i, o);
+                                }
+                            }
+                        }
+                        // (no reference: all of the row's keys so far are hidden, and any number will do for their weights, 0)
+                        const float mc = m == -INFINITY ? 0.0f : m * p.c;
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             uint32_t x[32];
                             load(2 * half + i, x);
                             sum[i] = weights32(x, p.c, mc, w[i]);
                         }
-                    };
-                    // The reference m is a score of the row that was the largest when it was taken.  It stays until some 32
-                    // weights add up to more than RESCALE (or to no number, as for a row without a reference): only then is
-                    // the maximum looked for, by both threads over the whole row.
-                    weigh(m * p.c);
-                    if (meet(!(sum[0] <= RESCALE && sum[1] <= RESCALE))) {
-                        float top = -INFINITY;
-#pragma unroll 1
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t x[32];
-                            load(i, x);
-                            top = fmaxf(top, max32(x));
-                        }
-                        const bool move = top > m && !((top - m) * p.c <= 1.0f);
-                        const float f = move ? exp2_approx((m - top) * p.c) : 1.0f;
-                        if (move) m = top;
-                        l *= f;
-                        if (t >= g.t0 + step && __any_sync(0xffffffffu, move)) {  // this warp's half of O's columns
-#pragma unroll 1
-                            for (int i = half * (D / 2); i < (half + 1) * (D / 2); i += 16) {
-                                uint32_t o[16];
-                                tmem_ld16(o_tm + i, o);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                                tmem_st16(o_tm + i, o);
-                            }
-                        }
-                        weigh(m == -INFINITY ? 0.0f : m * p.c);
-                        meet(false);
+                        if (!meet(!look && (m == -INFINITY || !(sum[0] <= RESCALE && sum[1] <= RESCALE)))) break;
+                        look = true;
                     }
                     // (the other warp has read its scores, which these weights overwrite in part)
                     l += sum[0] + sum[1];
@@ -813,11 +833,12 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             const long long per_pass = sum * cache.heads, total = per_pass * p.passes;
-            const long long n_groups = groups_used(p, total), group = min((long long)(blockIdx.x / p.side), n_groups);
+            const Ranges ranges(p, total);
+            const long long group = min((long long)(blockIdx.x / p.side), ranges.n);
             Walk w;
-            w.pos = total ? group * total / n_groups : 0;
-            w.hi = group < n_groups ? (group + 1) * total / n_groups : w.pos;
-            w.pass = per_pass ? (int)(w.pos / per_pass) : 0;
+            w.pos = ranges.begin(group);
+            w.hi = group < ranges.n ? ranges.begin(group + 1) : w.pos;
+            w.pass = p.passes > 1 && per_pass ? (int)quotient(w.pos, per_pass) : 0;
             w.slot = 0;
             const long long x = w.pos - w.pass * per_pass;  // < per_pass
             int mine = 0;  // the lane whose sequence the range starts in has its place
@@ -841,8 +862,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 if (n > 0 && x >= from && x < upto * cache.heads) {
                     mine = 1;
                     w.s = s;
-                    w.h = (int)((x - from) / n);
-                    w.t = (int)((x - from) % n);
+                    w.h = (int)quotient(x - from, n);
+                    w.t = (int)(x - from - (long long)w.h * n);
                 }
                 before = __shfl_sync(0xffffffffu, upto, 31);
                 if (blockIdx.x != 0 && before * cache.heads > x) break;
@@ -882,7 +903,8 @@ __global__ void __launch_bounds__(2 * D) join_kernel(const __grid_constant__ Att
     const int r = blockIdx.z * 32 + lane;
     int len, live, np;
     const int tiles = sequence_tiles(a, s, len, live, np);
-    const long long per_pass = p.cum[a.S] * a.cache.heads, total = per_pass * p.passes, n_groups = groups_used(p, total);
+    const long long per_pass = p.cum[a.S] * a.cache.heads;
+    const Ranges ranges(p, per_pass * p.passes);
     if (r >= min(2 * TILE, a.N * p.G - qt * 2 * TILE)) return;
     const int R = qt * 2 * TILE + r, node = R / p.G, gq = R - node * p.G;
     const long long out_row = ((long long)s * a.N + node) * a.Hq + h * p.G + gq;
@@ -893,11 +915,10 @@ __global__ void __launch_bounds__(2 * D) join_kernel(const __grid_constant__ Att
         return;
     }
     const long long u0 = (qt / p.side) * per_pass + p.cum[s] * a.cache.heads + (long long)h * tiles, u1 = u0 + tiles;
-    // the groups whose ranges [g total / n, (g + 1) total / n) hold the first and the last tile
-    const int g0 = (int)(((u0 + 1) * n_groups + total - 1) / total) - 1, g1 = (int)((u1 * n_groups + total - 1) / total) - 1;
+    const int g0 = (int)ranges.group_of(u0), g1 = (int)ranges.group_of(u1 - 1);  // of the first and the last tile
     if (g0 == g1) return;
     // the first group's range may begin before u0: then its part is the one at the range's end
-    const long long at0 = ((long long)g0 * p.side + qt % p.side) * 2 + (u0 > g0 * total / n_groups ? 1 : 0), at1 = ((long long)(g0 + 1) * p.side + qt % p.side) * 2;
+    const long long at0 = ((long long)g0 * p.side + qt % p.side) * 2 + (u0 > ranges.begin(g0) ? 1 : 0), at1 = ((long long)(g0 + 1) * p.side + qt % p.side) * 2;
     auto part = [&](int i) { return i == 0 ? at0 : at1 + (long long)(i - 1) * p.side * 2; };
     const int n = g1 - g0 + 1;
     float m = -INFINITY, l = 0.0f, x[16];
