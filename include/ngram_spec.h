@@ -377,7 +377,8 @@ int spec_tree_mask(spec_ctx* ctx, const int32_t* d_parent, int S, int N, const i
  *   out = sum_j softmax_j(scale <q, k_j>) v_j,   lse = log sum_j exp(scale <q, k_j>).
  * Rows that attend to nothing, and nodes from d_nnodes[s] on, give out = 0 and lse = -inf; what a row does not attend to
  * does not reach it, NaN and infinities included.  N = 1 is plain decoding of one token.
- *   d_q [S*N, Hq, head_dim], d_k / d_v [S*N, heads, head_dim] strided, bfloat16 (keys already rotated).
+ *   d_q [S*N, Hq, head_dim], d_k / d_v [S*N, heads, head_dim] strided, bfloat16 (keys already rotated); strides of d_k and
+ *   d_v are positive.
  *   d_out [S, N, Hq, head_dim] bfloat16, d_lse [S, N, Hq] float32 or NULL, contiguous.
  *   d_work: spec_tree_attention_bytes() of scratch, 16-byte aligned, for this call alone; needs no initial value.
  * Products are bf16 x bf16 with fp32 accumulation; statistics are fp32; the weights exp(s - max) are rounded to

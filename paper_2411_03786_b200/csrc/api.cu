@@ -614,6 +614,9 @@ int spec_tree_attention(spec_ctx* ctx, const spec_kv_cache* cache, const void* d
         (rc = check_rows(ctx, d_work, 0, 0, who, "work")))
         return rc;
     if (!d_mask || !d_len) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
+    if ((a.cache.heads > 1 && (k_head <= 0 || v_head <= 0)) || ((long long)S * N > 1 && (k_tok <= 0 || v_tok <= 0)) || k_head >= (1ll << 38) ||
+        v_head >= (1ll << 38) || k_tok >= (1ll << 38) || v_tok >= (1ll << 38))
+        return fail(ctx, SPEC_ERR_ARG, "%s: strides of k and v must be positive and below 2^38", who);
     if (!(scale > 0.0f) || scale > 3e38f) return fail(ctx, SPEC_ERR_ARG, "%s: scale must be positive and finite", who);
     const size_t need = tree_attention_bytes(ctx->num_sms, S, N, Hq, a.cache.heads, a.cache.head_dim);
     if (work_bytes < need) return fail(ctx, SPEC_ERR_ARG, "%s: %zu bytes of scratch given, %zu needed", who, work_bytes, need);

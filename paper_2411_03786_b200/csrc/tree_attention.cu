@@ -23,8 +23,8 @@
 //
 // Warps (896 threads, which share the registers unevenly): 0-7 and 8-15 softmax of stream 0 and 1 (a row's 128 scores
 // belong to two threads, of warps w and w + 4: a single warp per scheduler leaves the special function unit waiting);
-// 16-23 write key and value tiles that TMA cannot (the last tile of a context, zero-padded; the block's own; an E4M3
-// cache's, as bfloat16 code * scale, which is exact); 24 TMA; 25 issues the products; 26 walks the CTA's range and tells
+// 16-23 turn an E4M3 cache's tiles into bfloat16 (code * scale, which is exact) and mend value tiles (zeros after the
+// end of a context, and in place of what is not finite in the block); 24 TMA; 25 issues the products; 26 walks the CTA's range and tells
 // the others.
 #include <cuda_bf16.h>
 #include <math.h>
@@ -250,7 +250,8 @@ __device__ __forceinline__ uint32_t nonfinite_to_zero(uint32_t v, bool& found) {
 
 template <int D, bool Q8>
 __global__ void __launch_bounds__(ATT_THREADS, 1)
-tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttParams p) {
+tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_bk,
+                      const __grid_constant__ CUtensorMap tm_bv, const __grid_constant__ AttParams p) {
     using Geo = Geometry<D, Q8>;
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = smem_u32(smem);
@@ -295,7 +296,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         tmem_alloc(smem_u32(&sh.tmem), 512);
         tmem_relinquish();
     }
-    if (warp == TMA_WARP && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? &tm_v : &tm_k)) : "memory");
+    if (warp == TMA_WARP && lane < (Q8 ? 2 : 4))
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane == 0 ? &tm_k : (lane == 1 ? &tm_v : (lane == 2 ? &tm_bk : &tm_bv)))) : "memory");
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -566,7 +568,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     phase ^= 1u;
                 }
                 const int rows = block ? g.live - (t - g.n_prefix) * TILE : g.len - t * TILE;  // may exceed the tile
-                if (!Q8 && !block && rows >= TILE) return true;                                 // TMA's
+                if (!Q8 && !(is_v && (block || rows < TILE))) return true;  // all TMA's
                 if (Q8 && !block) {
                     if (!wait(stg_full + 8 * stg, stg_phase)) return false;
                     if (!wait(bar_empty, my_phase ^ 1u)) return false;
@@ -599,16 +601,36 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                         stg_phase ^= 1u;
                     }
                 } else {
-                    // A barrier's parity tells one use of a slot from the next, not from the one after.  E4M3: these
-                    // threads fill every slot and so wait for each.  bfloat16: they skip TMA's, which would let them get
-                    // more than one use ahead or behind; the TMA warp waits for every slot and hands this one over.
-                    if (Q8) {
-                        if (!wait(bar_empty, my_phase ^ 1u)) return false;
-                    } else {
+                    if (!Q8) {
+                        // TMA's as well, but what lies beyond the end must be 0 (a weight of 0 would not keep a NaN out of the
+                        // products), and so must values of the block that are not finite.  (A barrier's parity tells one use
+                        // of a slot from the next, not from the one after, so these threads, which skip slots, do not wait for
+                        // empty ones: the TMA warp waits for every slot, and a barrier of the slot's own says it has landed.)
                         if (!wait(go + 8 * my_slot, (go_phase >> my_slot) & 1u)) return false;
                         go_phase ^= 1u << my_slot;
+                        bool found = false;
+#pragma unroll 2
+                        for (int i = 0; i < TILE * CH / LOADERS; ++i) {
+                            const int r = i * (LOADERS / CH) + tid / CH, c = tid % CH;
+                            if (r >= rows) {
+                                st_shared16(dst + tile_at(r, c), make_uint4(0, 0, 0, 0));
+                            } else if (block) {
+                                uint4 v = ld_shared16(dst + tile_at(r, c));
+                                bool bad = false;
+                                v.x = nonfinite_to_zero(v.x, bad);
+                                v.y = nonfinite_to_zero(v.y, bad);
+                                v.z = nonfinite_to_zero(v.z, bad);
+                                v.w = nonfinite_to_zero(v.w, bad);
+                                if (bad) st_shared16(dst + tile_at(r, c), v);
+                                found |= bad;
+                            }
+                        }
+                        if (found) sh.nonfinite[n_seg & 15u] = (int)n_seg + 1;
+                        fence_async_smem();
+                        mbar_arrive(bar_full);
+                        return true;
                     }
-                    bool found = false;
+                    bool found = false;  // a tile of the block
                     constexpr int PER = TILE * CH / LOADERS;
                     {
                         uint4 v[PER];
@@ -617,27 +639,16 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                             const int r = i * (LOADERS / CH) + tid / CH, c = tid % CH;
                             v[i] = make_uint4(0, 0, 0, 0);
                             if (r >= rows) continue;
-                            const __nv_bfloat16* src;
-                            if (block) {
-                                const long long tok = (long long)g.s * a.N + (t - g.n_prefix) * TILE + r;
-                                src = is_v ? (const __nv_bfloat16*)a.v + tok * a.v_tok + (long long)g.h * a.v_head
-                                           : (const __nv_bfloat16*)a.k + tok * a.k_tok + (long long)g.h * a.k_head;
-                            } else {
-                                const int pos = t * TILE + r;
-                                const int page = cache.table[(long long)g.s * cache.max_pages + (pos >> cache.page_shift)];
-                                if ((unsigned)page >= (unsigned)cache.n_pages) {
-                                    atomicOr(a.status, SPEC_STATUS_CAPACITY);
-                                    continue;
-                                }
-                                const long long at = (((long long)page * cache.heads + g.h) << cache.page_shift) + (pos & ((1 << cache.page_shift) - 1));
-                                src = (const __nv_bfloat16*)(is_v ? cache.v : cache.k) + at * D;
-                            }
+                            const long long tok = (long long)g.s * a.N + (t - g.n_prefix) * TILE + r;
+                            const __nv_bfloat16* src = is_v ? (const __nv_bfloat16*)a.v + tok * a.v_tok + (long long)g.h * a.v_head
+                                                            : (const __nv_bfloat16*)a.k + tok * a.k_tok + (long long)g.h * a.k_head;
                             v[i] = *reinterpret_cast<const uint4*>(src + c * 8);
                         }
+                        if (!wait(bar_empty, my_phase ^ 1u)) return false;
 #pragma unroll
                         for (int i = 0; i < PER; ++i) {
                             const int r = i * (LOADERS / CH) + tid / CH, c = tid % CH;
-                            if (block && is_v) {
+                            if (is_v) {
                                 v[i].x = nonfinite_to_zero(v[i].x, found);
                                 v[i].y = nonfinite_to_zero(v[i].y, found);
                                 v[i].z = nonfinite_to_zero(v[i].z, found);
@@ -679,13 +690,13 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 int even = fetch(w0 + (w0 & 1)), odd = fetch(w0 + 1 - (w0 & 1));
                 ok = for_each_tile(g, [&](bool is_v, int t) {
                     const bool block = t >= g.n_prefix;
-                    const int rows = block ? 0 : g.len - t * TILE;
-                    const bool mine = Q8 ? !block : rows >= TILE;
+                    const int rows = block ? TILE : min(g.len - t * TILE, TILE);
+                    const bool mended = !Q8 && is_v && (block || rows < TILE);  // goes through the other threads' hands
                     const uint32_t bar_full = (Q8 ? stg_full : full) + 8 * slot, bar_empty = (Q8 ? stg_empty : empty) + 8 * slot;
                     const uint32_t dst = Q8 ? stg_at + slot * Geo::STAGE_BYTES : ring_at + slot * Geo::TILE_BYTES;
                     const uint32_t ex = exp_at + slot * TILE, bar_go = go + 8 * slot;
                     const uint32_t my_phase = phase;
-                    if (mine || !Q8) {
+                    if (!Q8 || !block) {
                         if (++slot == RING) {
                             slot = 0;
                             phase ^= 1u;
@@ -697,30 +708,29 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                         if (window & 1) even = fetch(window + 1);
                         else odd = fetch(window + 1);
                     }
-                    if (Q8 && !mine) return true;
+                    if (Q8 && block) return true;
                     const bool got = wait(bar_empty, my_phase ^ 1u);
                     if (!__all_sync(0xffffffffu, got)) return false;
-                    if (!mine) {
-                        if (lane == 0) mbar_arrive(bar_go);
-                        return true;
-                    }
-                    const int pages = min((rows + page - 1) >> cache.page_shift, per_tile);
+                    const int pages = block ? 0 : (rows + page - 1) >> cache.page_shift;
+                    const uint32_t bar = mended ? bar_go : bar_full;
                     if (lane == 0) {
-                        mbar_expect_tx(bar_full, (uint32_t)(pages * page) * (Q8 ? D + 1 : 2 * D));
-                        if (!Q8) mbar_arrive_n(bar_full, LOADERS - 1);
+                        mbar_expect_tx(bar, (uint32_t)(block ? TILE : pages * page) * (Q8 ? D + 1 : 2 * D));
+                        if (!Q8 && !mended) mbar_arrive_n(bar_full, LOADERS - 1);
                     }
                     __syncwarp();
-                    if (lane < pages) {
+                    if (block) {
+                        if (lane < Geo::HALVES) tma_load_3d(dst + lane * (TILE * 128), is_v ? &tm_bv : &tm_bk, 64 * lane, g.h, g.s * a.N + (t - g.n_prefix) * TILE, bar);
+                    } else if (lane < pages) {
                         const bool good = (unsigned)pid < (unsigned)cache.n_pages;
                         if (!good) atomicOr(a.status, SPEC_STATUS_CAPACITY);
                         const int row = good ? (pid * cache.heads + g.h) << cache.page_shift : all_rows;
                         const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
                         if (Q8) {
-                            tma_load_2d(dst + lane * page * D, tm, 0, row, bar_full);
-                            bulk_load(ex + lane * page, (is_v ? cache.v_exp : cache.k_exp) + (good ? row : 0), page, bar_full);
+                            tma_load_2d(dst + lane * page * D, tm, 0, row, bar);
+                            bulk_load(ex + lane * page, (is_v ? cache.v_exp : cache.k_exp) + (good ? row : 0), page, bar);
                         } else {
 #pragma unroll
-                            for (int i = 0; i < Geo::HALVES; ++i) tma_load_2d(dst + i * (TILE * 128) + lane * page * 128, tm, 64 * i, row, bar_full);
+                            for (int i = 0; i < Geo::HALVES; ++i) tma_load_2d(dst + i * (TILE * 128) + lane * page * 128, tm, 64 * i, row, bar);
                         }
                     }
                     ++issued;
@@ -828,11 +838,23 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             // -------------------------------------------------------------------------------- this CTA's range of key tiles
             int len, live, np;
             const int n_first = lane < a.S ? sequence_tiles(a, lane, len, live, np) : 0;
-            long long sum = n_first;
-            for (int s = lane + 32; s < a.S; s += 32) sum += sequence_tiles(a, s, len, live, np);
+            auto scan = [&](int n) {  // inclusive
+                long long upto = n;
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            const long long per_pass = sum * cache.heads, total = per_pass * p.passes;
+                for (int o = 1; o < 32; o <<= 1) {
+                    const long long other = __shfl_up_sync(0xffffffffu, upto, o);
+                    if (lane >= o) upto += other;
+                }
+                return upto;
+            };
+            const long long first_upto = scan(n_first);
+            long long sum = 0;
+            if (a.S > 32) {
+                for (int s = lane + 32; s < a.S; s += 32) sum += sequence_tiles(a, s, len, live, np);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            }
+            const long long per_pass = (sum + __shfl_sync(0xffffffffu, first_upto, 31)) * cache.heads, total = per_pass * p.passes;
             const Ranges ranges(p, total);
             const long long group = min((long long)(blockIdx.x / p.side), ranges.n);
             Walk w;
@@ -846,13 +868,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             for (int s0 = 0; s0 < a.S; s0 += 32) {
                 const int s = s0 + lane;
                 const int n = s0 == 0 ? n_first : (s < a.S ? sequence_tiles(a, s, len, live, np) : 0);
-                long long upto = n;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const long long other = __shfl_up_sync(0xffffffffu, upto, o);
-                    if (lane >= o) upto += other;
-                }
-                upto += before;
+                const long long upto = before + (s0 == 0 ? first_upto : scan(n));
                 if (blockIdx.x == 0 && s < a.S) {
                     p.cum[s + 1] = upto;
                     if (s == 0) p.cum[0] = 0;
@@ -996,6 +1012,20 @@ static int cache_map(spec_ctx* ctx, CUtensorMap* tm, const void* base, const Cac
     return SPEC_OK;
 }
 
+// Keys or values of the block, [S * N, heads, D] strided, 128 nodes of a head and 128 bytes at a time.
+static int block_map(spec_ctx* ctx, CUtensorMap* tm, const void* base, long long tok, long long head, const TreeAttnArgs& a) {
+    const CacheArgs& c = a.cache;
+    cuuint64_t dims[3] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.heads, (cuuint64_t)a.S * a.N};
+    // (the stride of a dimension of one is never used, but has to be a valid one)
+    cuuint64_t strides[2] = {(cuuint64_t)(c.heads > 1 ? head : c.head_dim) * 2, (cuuint64_t)((long long)a.S * a.N > 1 ? tok : (long long)c.heads * c.head_dim) * 2};
+    cuuint32_t box[3] = {64u, 1u, (cuuint32_t)TILE};
+    cuuint32_t estr[3] = {1u, 1u, 1u};
+    CUresult r = ctx->encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(ctx, SPEC_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+    return SPEC_OK;
+}
+
 template <int D, bool Q8>
 static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
     auto kernel = tree_attention_kernel<D, Q8>;
@@ -1015,10 +1045,12 @@ static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
             d = true;
         }
     }
-    CUtensorMap tm_k, tm_v;
+    CUtensorMap tm_k, tm_v, tm_bk, tm_bv;
     int rc = cache_map(ctx, &tm_k, p.a.cache.k, p.a.cache);
-    if (rc || (rc = cache_map(ctx, &tm_v, p.a.cache.v, p.a.cache))) return rc;
-    cudaError_t e = launch_pdl(kernel, dim3(p.n_groups * p.side), dim3(ATT_THREADS), (size_t)Geometry<D, Q8>::SMEM, st, tm_k, tm_v, p);
+    if (rc || (rc = cache_map(ctx, &tm_v, p.a.cache.v, p.a.cache)) || (rc = block_map(ctx, &tm_bk, p.a.k, p.a.k_tok, p.a.k_head, p.a)) ||
+        (rc = block_map(ctx, &tm_bv, p.a.v, p.a.v_tok, p.a.v_head, p.a)))
+        return rc;
+    cudaError_t e = launch_pdl(kernel, dim3(p.n_groups * p.side), dim3(ATT_THREADS), (size_t)Geometry<D, Q8>::SMEM, st, tm_k, tm_v, tm_bk, tm_bv, p);
     if ((rc = check_cuda(ctx, e, "spec_tree_attention launch"))) return rc;
     e = launch_pdl(join_kernel<D>, dim3(p.a.S * p.a.cache.heads, p.n_qtiles, (p.rows_cap + 31) / 32), dim3(2 * D), 0, st, p);
     ctx->launches += 2;
