@@ -45,6 +45,7 @@ constexpr int LAUNCH_REGS = 72;   // per thread at launch: 65536 / 896, rounded 
 constexpr int REGS_SOFTMAX = 88, REGS_LOADER = 40, REGS_CONTROL = 72;
 constexpr int SEGMENTS = 4;  // segments that the planning warp is ahead
 static_assert(128 * (4 * REGS_SOFTMAX + 2 * REGS_LOADER + REGS_CONTROL) <= ATT_THREADS * LAUNCH_REGS, "the warpgroups' shares exceed the launch's registers");
+constexpr int START = 4;  // tiles that the beginning and end of a segment take as long as (6 us where a tile takes 1.4)
 constexpr float RESCALE = 256.0f;  // what 32 weights may add up to before their reference is moved
 
 struct AttParams {
@@ -52,7 +53,7 @@ struct AttParams {
     int G, n_qtiles, side, n_groups, passes;  // side: row-tile pairs that run side by side
     int rows_cap;                             // rows of a partial result
     float c;                                  // scale * log2(e)
-    long long* cum;                           // [S + 1] key tiles of the sequences before
+    long long* cum;                           // [S + 1] places (see Ranges) of a key head of the sequences before
     float2* part_ml;                          // [grid * 2, rows_cap]
     float* part_o;                            // [grid * 2, D / 4, rows_cap, 4]
     unsigned long long wait_limit_ns;
@@ -99,12 +100,15 @@ __device__ __forceinline__ int sequence_tiles(const TreeAttnArgs& a, int s, int&
     return live == 0 ? 0 : n_prefix + (live + TILE - 1) / TILE;
 }
 
+__device__ __forceinline__ int places(int n_tiles) { return n_tiles ? n_tiles + START : 0; }
+
 // Quotient of numbers that nearly always fit in 32 bits (a 64-bit division is a long subroutine).
 __device__ __forceinline__ long long quotient(long long a, long long b) {
     return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
 }
-// The tiles [0, total) in equal consecutive ranges: the first `rem` groups have base + 1, the others base.  With fewer
-// tiles than groups, as many groups as tiles have one.
+// The work is cut where it costs the same: every (s, h) counts as START places more than it has tiles, for what it takes to
+// begin and end a segment (its places first), and the places [0, total) are cut into equal consecutive ranges: the first
+// `rem` groups have base + 1 places, the others base.  With fewer places than groups, as many groups as places have one.
 struct Ranges {
     long long total, n, base, rem;
     __device__ __forceinline__ Ranges(const AttParams& p, long long total_) : total(total_), n(min((long long)p.n_groups, total_)), base(0), rem(0) {
@@ -128,25 +132,27 @@ __device__ __forceinline__ void advance(const AttParams& p, Walk& w, Segment& g)
     int rows = 0;
     while (w.pos < w.hi && rows <= 0) {
         int len, live, n_prefix;
-        const int n_tiles = sequence_tiles(p.a, w.s, len, live, n_prefix);
-        if (w.t < n_tiles) {
-            const int take = (int)min((long long)(n_tiles - w.t), w.hi - w.pos), qt = w.pass * p.side + (int)(blockIdx.x % p.side);
-            rows = qt < p.n_qtiles ? min(2 * TILE, live * p.G - qt * 2 * TILE) : 0;
-            g.s = w.s;
-            g.h = w.h;
-            g.qt = qt;
-            g.t0 = w.t;
-            g.t1 = w.t + take;
-            g.n_prefix = n_prefix;
-            g.len = len;
-            g.live = live;
-            g.whole = take == n_tiles;
-            g.slot = w.slot;
-            w.slot = 1;
+        const int n_tiles = sequence_tiles(p.a, w.s, len, live, n_prefix), n = places(n_tiles);
+        if (w.t < n) {
+            const int take = (int)min((long long)(n - w.t), w.hi - w.pos), qt = w.pass * p.side + (int)(blockIdx.x % p.side);
+            g.t0 = max(w.t - START, 0);
+            g.t1 = w.t + take - START;
+            if (g.t1 > g.t0) {
+                rows = qt < p.n_qtiles ? min(2 * TILE, live * p.G - qt * 2 * TILE) : 0;
+                g.s = w.s;
+                g.h = w.h;
+                g.qt = qt;
+                g.n_prefix = n_prefix;
+                g.len = len;
+                g.live = live;
+                g.whole = g.t1 - g.t0 == n_tiles;
+                g.slot = w.slot;
+                w.slot = 1;
+            }
             w.pos += take;
             w.t += take;
         }
-        if (w.t >= n_tiles) {  // on to the next key head
+        if (w.t >= n) {  // on to the next key head
             w.t = 0;
             if (n_tiles == 0 || ++w.h == p.a.cache.heads) {
                 w.h = 0;
@@ -837,7 +843,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         } else if (warp == PLAN_WARP) {
             // -------------------------------------------------------------------------------- this CTA's range of key tiles
             int len, live, np;
-            const int n_first = lane < a.S ? sequence_tiles(a, lane, len, live, np) : 0;
+            const int n_first = lane < a.S ? places(sequence_tiles(a, lane, len, live, np)) : 0;
             auto scan = [&](int n) {  // inclusive
                 long long upto = n;
 #pragma unroll
@@ -850,7 +856,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             const long long first_upto = scan(n_first);
             long long sum = 0;
             if (a.S > 32) {
-                for (int s = lane + 32; s < a.S; s += 32) sum += sequence_tiles(a, s, len, live, np);
+                for (int s = lane + 32; s < a.S; s += 32) sum += places(sequence_tiles(a, s, len, live, np));
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             }
@@ -867,7 +873,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             long long before = 0;
             for (int s0 = 0; s0 < a.S; s0 += 32) {
                 const int s = s0 + lane;
-                const int n = s0 == 0 ? n_first : (s < a.S ? sequence_tiles(a, s, len, live, np) : 0);
+                const int n = s0 == 0 ? n_first : (s < a.S ? places(sequence_tiles(a, s, len, live, np)) : 0);
                 const long long upto = before + (s0 == 0 ? first_upto : scan(n));
                 if (blockIdx.x == 0 && s < a.S) {
                     p.cum[s + 1] = upto;
@@ -930,10 +936,10 @@ __global__ void __launch_bounds__(2 * D) join_kernel(const __grid_constant__ Att
         if (a.lse && cols == 0) a.lse[out_row] = -INFINITY;
         return;
     }
-    const long long u0 = (qt / p.side) * per_pass + p.cum[s] * a.cache.heads + (long long)h * tiles, u1 = u0 + tiles;
-    const int g0 = (int)ranges.group_of(u0), g1 = (int)ranges.group_of(u1 - 1);  // of the first and the last tile
+    const long long u0 = (qt / p.side) * per_pass + p.cum[s] * a.cache.heads + (long long)h * (tiles + START), u1 = u0 + START + tiles;
+    const int g0 = (int)ranges.group_of(u0 + START), g1 = (int)ranges.group_of(u1 - 1);  // of the first and the last tile
     if (g0 == g1) return;
-    // the first group's range may begin before u0: then its part is the one at the range's end
+    // the first group's range may begin with another (s, h): then its part is the one at the range's end
     const long long at0 = ((long long)g0 * p.side + qt % p.side) * 2 + (u0 > ranges.begin(g0) ? 1 : 0), at1 = ((long long)(g0 + 1) * p.side + qt % p.side) * 2;
     auto part = [&](int i) { return i == 0 ? at0 : at1 + (long long)(i - 1) * p.side * 2; };
     const int n = g1 - g0 + 1;
