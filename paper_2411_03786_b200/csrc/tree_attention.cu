@@ -187,12 +187,12 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
     const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
-// Two E4M3 codes (bytes SEL of w) times a power of two as bfloat16: the code's sign, exponent and mantissa moved into
-// a bfloat16's fields read as its value times 2^-120 (subnormals as subnormals), and `f` holds scale * 2^120.
-template <uint32_t SEL>
-__device__ __forceinline__ uint32_t e4m3x2_bf16x2(uint32_t w, uint32_t f) {
-    const uint32_t x = __byte_perm(w, 0u, SEL);
-    return mul_bf16x2((x & 0x80008000u) | ((x >> 4) & 0x07F007F0u), f);
+// Four E4M3 codes times a power of two as bfloat16, two to a word: a code's sign, exponent and mantissa moved into a
+// bfloat16's fields read as its value times 2^-120 (subnormals as subnormals), and `f` holds scale * 2^120.
+__device__ __forceinline__ void e4m3x4_bf16x4(uint32_t w, uint32_t f, uint32_t& lo, uint32_t& hi) {
+    const uint32_t low = (w << 4) & 0xF0F0F0F0u, high = ((w >> 4) & 0x07070707u) | (w & 0x80808080u);  // the bytes of the results
+    lo = mul_bf16x2(__byte_perm(low, high, 0x5140), f);
+    hi = mul_bf16x2(__byte_perm(low, high, 0x7362), f);
 }
 __device__ __forceinline__ uint32_t scale_bf16x2(uint32_t exp) {
     const uint32_t b = exp > 127u + E8_MAX ? 0x7FC0u : (exp + 120u) << 7;  // beyond the largest: NaN
@@ -595,8 +595,11 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     for (int i = 0; i < PER; ++i) {
                         const int r = i * (LOADERS / LPR) + tid / LPR;
                         const uint32_t f = scale_bf16x2(e[i]);
-                        uint4 lo = make_uint4(e4m3x2_bf16x2<0x1404>(v[i].x, f), e4m3x2_bf16x2<0x3424>(v[i].x, f), e4m3x2_bf16x2<0x1404>(v[i].y, f), e4m3x2_bf16x2<0x3424>(v[i].y, f));
-                        uint4 hi = make_uint4(e4m3x2_bf16x2<0x1404>(v[i].z, f), e4m3x2_bf16x2<0x3424>(v[i].z, f), e4m3x2_bf16x2<0x1404>(v[i].w, f), e4m3x2_bf16x2<0x3424>(v[i].w, f));
+                        uint4 lo, hi;
+                        e4m3x4_bf16x4(v[i].x, f, lo.x, lo.y);
+                        e4m3x4_bf16x4(v[i].y, f, lo.z, lo.w);
+                        e4m3x4_bf16x4(v[i].z, f, hi.x, hi.y);
+                        e4m3x4_bf16x4(v[i].w, f, hi.z, hi.w);
                         if (r >= rows) lo = hi = make_uint4(0, 0, 0, 0);  // (whatever the staging tile held)
                         st_shared16(dst + tile_at(r, 2 * c + (swap ? 1 : 0)), swap ? hi : lo);
                         st_shared16(dst + tile_at(r, 2 * c + (swap ? 0 : 1)), swap ? lo : hi);
