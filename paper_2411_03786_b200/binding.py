@@ -120,6 +120,10 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _new(like: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(like, memory_format=torch.contiguous_format)
+
+
 def _need(ok: bool, what: str):
     if not ok:
         raise SpecError(what)
@@ -128,18 +132,19 @@ def _need(ok: bool, what: str):
 def _rows(t: torch.Tensor, name: str):
     """Pointer, token stride and head stride of ``t[S, N, heads, D]`` or ``t[T, heads, D]`` whose head vectors are
     contiguous and whose sequences follow one another at N token strides."""
-    _need(t.is_cuda and t.dtype == torch.bfloat16, f"{name}: expected a bfloat16 CUDA tensor")
+    if not t.is_cuda or t.dtype is not torch.bfloat16:
+        raise SpecError(f"{name}: expected a bfloat16 CUDA tensor")
     st = t.stride()
-    _need(st[-1] == 1 and (t.dim() == 3 or t.shape[0] <= 1 or st[0] == st[1] * t.shape[1]),
-          f"{name}: head vectors must be contiguous, and sequences N tokens apart")
+    if st[-1] != 1 or (len(st) == 4 and t.shape[0] > 1 and st[0] != st[1] * t.shape[1]):
+        raise SpecError(f"{name}: head vectors must be contiguous, and sequences N tokens apart")
     return t.data_ptr(), st[-3], st[-2]
 
 
 def _i32(t: torch.Tensor | None, name: str, shape):
     if t is None:
         return None
-    _need(t.is_cuda and t.dtype == torch.int32 and t.shape == shape and t.is_contiguous(),
-          f"{name}: expected a contiguous int32 CUDA tensor of shape {tuple(shape)}")
+    if not t.is_cuda or t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
+        raise SpecError(f"{name}: expected a contiguous int32 CUDA tensor of shape {tuple(shape)}")
     return t.data_ptr()
 
 
@@ -161,6 +166,7 @@ class KVCache:
             _need(t is None or (t.is_cuda and t.is_contiguous()), "KVCache: tensors must be contiguous CUDA tensors")
         self.k, self.v, self.table, self.k_exp, self.v_exp = k, v, table, k_exp, v_exp
         self.n_pages, self.heads, self.page, self.head_dim = (int(x) for x in k.shape)
+        self.sequences = int(table.shape[0])
         ptr = lambda t: None if t is None else t.data_ptr()
         self._struct = _KVCacheStruct(ptr(k), ptr(v), ptr(k_exp), ptr(v_exp), ptr(table), SPEC_BF16 if k.dtype == torch.bfloat16 else SPEC_E4M3,
                                       self.n_pages, int(table.shape[1]), self.page, self.heads, self.head_dim)
@@ -196,6 +202,8 @@ class SpecContext:
         dtype = {torch.float32: SPEC_F32, torch.bfloat16: SPEC_BF16}[embed.dtype]
         self.V, self.d = int(embed.shape[0]), int(embed.shape[1])
         self._keep = [embed, unembed]
+        self._device = embed.device.index or 0
+        self._work_bytes = {}  # scratch of a tree_attention call, by its sizes
         rc = self._lib.spec_init(C.byref(self._h), _ptr(embed), _ptr(unembed), dtype, self.V, self.d,
                                  embed.device.index or 0, _stream())
         if rc != 0:
@@ -204,6 +212,10 @@ class SpecContext:
     def _check(self, rc: int, what: str):
         if rc != 0:
             raise SpecError(f"{what} failed ({rc}): {self._lib.spec_last_error(self._h).decode()}")
+
+    def _raw_stream(self) -> int:
+        """torch's current stream on the context's device (torch.cuda.current_stream() makes an object of it: 3 us)."""
+        return torch._C._cuda_getCurrentRawStream(self._device)
 
     def close(self):
         if self._h:
@@ -433,17 +445,22 @@ class SpecContext:
 
         Returns ``(logp[M], entropy[M], alt_ids[M, n_alt] or None, alt_logp[M, n_alt] or None)``.
         """
-        M, dev = hidden.shape[0], hidden.device
-        _need(hidden.dim() == 2 and hidden.shape[1] == self.d, "score_tokens: hidden must be [M, d]")
+        M = hidden.shape[0]
+        _need(hidden.dim() == 2 and hidden.shape[1] == self.d and hidden.dtype == torch.bfloat16 and hidden.is_cuda and hidden.is_contiguous(),
+              "score_tokens: hidden must be contiguous bfloat16 [M, d]")
         if out is None:
-            out = (torch.empty(M, dtype=torch.float32, device=dev), torch.empty(M, dtype=torch.float32, device=dev),
-                   torch.empty((M, n_alt), dtype=torch.int32, device=dev) if n_alt else None,
-                   torch.empty((M, n_alt), dtype=torch.float32, device=dev) if n_alt else None)
+            logp = torch.empty_like(tokens, dtype=torch.float32)
+            idx = tokens.new_empty((M, n_alt)) if n_alt > 0 else None
+            out = (logp, torch.empty_like(logp), idx, None if idx is None else torch.empty_like(idx, dtype=torch.float32))
+        else:
+            for y, shape, dtype in zip(out, ((M,), (M,), (M, n_alt), (M, n_alt)), (torch.float32, torch.float32, torch.int32, torch.float32)):
+                _need((y is None and n_alt == 0) or (y is not None and y.shape == shape and y.dtype == dtype and y.is_cuda and y.is_contiguous()),
+                      "score_tokens: outputs must be contiguous float32 [M], float32 [M], int32 [M, n_alt], float32 [M, n_alt]")
         if work is None:
-            work = torch.empty(max(16, self._lib.spec_score_bytes(self._h, M, n_alt)), dtype=torch.uint8, device=dev)
-        self._check(self._lib.score_tokens(self._h, _ptr(hidden, torch.bfloat16), M, _i32(tokens, "tokens", (M,)), n_alt, _ptr(out[0], torch.float32),
-                                           _ptr(out[1], torch.float32), _ptr(out[2], torch.int32), _ptr(out[3], torch.float32), work.data_ptr(),
-                                           work.numel(), _stream()), "score_tokens")
+            work = hidden.new_empty(max(16, self._lib.spec_score_bytes(self._h, M, n_alt)), dtype=torch.uint8)
+        ptr = lambda y: None if y is None else y.data_ptr()
+        self._check(self._lib.score_tokens(self._h, hidden.data_ptr(), M, _i32(tokens, "tokens", (M,)), n_alt, ptr(out[0]), ptr(out[1]), ptr(out[2]),
+                                           ptr(out[3]), work.data_ptr(), work.numel(), self._raw_stream()), "score_tokens")
         return out
 
     def rope_rows(self, rope: Rope, q: torch.Tensor, k: torch.Tensor | None, pos: torch.Tensor, out=None):
@@ -451,39 +468,43 @@ class SpecContext:
 
         Returns contiguous ``(q_out, k_out)``, or writes to ``out``, whose tensors may be ``q`` and ``k`` themselves.
         """
+        shape = q.shape
+        _need(k is None or (k.shape[-1] == shape[-1] and k.shape[:-2] == shape[:-2]), "rope_rows: q and k must have the same tokens and head size")
         if out is None:
-            out = (torch.empty(q.shape, dtype=q.dtype, device=q.device), None if k is None else torch.empty(k.shape, dtype=k.dtype, device=k.device))
-        D, T = q.shape[-1], q.shape[:-2].numel()
-        _need(k is None or (k.shape[-1] == D and k.shape[:-2] == q.shape[:-2]), "rope_rows: q and k must have the same tokens and head size")
-        for x, y in zip((q, k), out):
-            _need(x is None or (y.shape == x.shape and y.dtype == x.dtype and y.is_contiguous()), "rope_rows: outputs must be contiguous, of the inputs' shapes")
+            out = (_new(q), None if k is None else _new(k))
+        else:
+            for x, y in zip((q, k), out):
+                _need(x is None or (y.shape == x.shape and y.dtype == x.dtype and y.is_contiguous()), "rope_rows: outputs must be contiguous, of the inputs' shapes")
         qp, qt, qh = _rows(q, "q")
         kp, kt, kh = (None, 0, 0) if k is None else _rows(k, "k")
-        self._check(self._lib.spec_rope_rows(self._h, rope._ref, qp, q.shape[-2], qt, qh, out[0].data_ptr(), kp, 0 if k is None else k.shape[-2],
-                                             kt, kh, None if k is None else out[1].data_ptr(), D, _i32(pos, "pos", q.shape[:-2]), T, _stream()),
-                    "spec_rope_rows")
+        self._check(self._lib.spec_rope_rows(self._h, rope._ref, qp, shape[-2], qt, qh, out[0].data_ptr(), kp, 0 if k is None else k.shape[-2],
+                                             kt, kh, None if k is None else out[1].data_ptr(), shape[-1], _i32(pos, "pos", shape[:-2]), pos.numel(),
+                                             self._raw_stream()), "spec_rope_rows")
         return out
 
     def cache_write(self, cache: KVCache, k: torch.Tensor, v: torch.Tensor, start: torch.Tensor, count: torch.Tensor | None = None,
                     nodes: torch.Tensor | None = None, rope: Rope | None = None):
         """Writes ``k``, ``v`` ``[S, N, heads, D]`` to positions ``start[s] + i``, ``i < count[s]`` (all N): node ``nodes[s, i]`` or ``i``."""
-        S, N = int(k.shape[0]), int(k.shape[1])
-        _need(k.dim() == 4 and k.shape == v.shape and tuple(k.shape[2:]) == (cache.heads, cache.head_dim) and S == cache.table.shape[0],
-              "cache_write: k and v must be [S, N, heads, head_dim] of the cache")
-        n = N if nodes is None else int(nodes.shape[1])
+        _need(k.dim() == 4 and k.shape == v.shape, "cache_write: k and v must be [S, N, heads, head_dim]")
+        S, N, heads, D = k.shape
+        _need(heads == cache.heads and D == cache.head_dim and S == cache.sequences, "cache_write: k and v must have the cache's heads, head_dim and sequences")
+        n = N if nodes is None else nodes.shape[1]
         self._check(self._lib.spec_cache_write(self._h, cache._ref, *_rows(k, "k"), *_rows(v, "v"), S, N, n, _i32(nodes, "nodes", (S, n)),
                                                _i32(start, "start", (S,)), _i32(count, "count", (S,)), None if rope is None else rope._ref,
-                                               _stream()), "spec_cache_write")
+                                               self._raw_stream()), "spec_cache_write")
 
     def cache_read(self, cache: KVCache, start: torch.Tensor, n: int, count: torch.Tensor | None = None, out=None):
         """Positions ``start[s] + i``, ``i < count[s]`` (``n``), as bfloat16 ``(k, v)`` ``[S, n, heads, D]``; zeros beyond."""
-        S = int(cache.table.shape[0])
+        S = cache.sequences
         if out is None:
-            out = tuple(torch.empty((S, n, cache.heads, cache.head_dim), dtype=torch.bfloat16, device=cache.k.device) for _ in range(2))
-        for t in out:
-            _need(tuple(t.shape) == (S, n, cache.heads, cache.head_dim) and t.is_contiguous(), "cache_read: outputs must be contiguous [S, n, heads, head_dim]")
+            k = torch.empty((S, n, cache.heads, cache.head_dim), dtype=torch.bfloat16, device=cache.k.device)
+            out = (k, torch.empty_like(k))
+        else:
+            for t in out:
+                _need(tuple(t.shape) == (S, n, cache.heads, cache.head_dim) and t.dtype == torch.bfloat16 and t.is_cuda and t.is_contiguous(),
+                      "cache_read: outputs must be contiguous bfloat16 [S, n, heads, head_dim]")
         self._check(self._lib.spec_cache_read(self._h, cache._ref, S, n, _i32(start, "start", (S,)), _i32(count, "count", (S,)),
-                                              _ptr(out[0], torch.bfloat16), _ptr(out[1], torch.bfloat16), _stream()), "spec_cache_read")
+                                              out[0].data_ptr(), out[1].data_ptr(), self._raw_stream()), "spec_cache_read")
         return out
 
     def tree_mask(self, parent: torch.Tensor, n_nodes: torch.Tensor | None = None):
@@ -492,7 +513,7 @@ class SpecContext:
         mask = torch.empty((S, N, (N + 31) // 32), dtype=torch.int32, device=parent.device)
         depth = torch.empty((S, N), dtype=torch.int32, device=parent.device)
         self._check(self._lib.spec_tree_mask(self._h, _i32(parent, "parent", (S, N)), S, N, _i32(n_nodes, "n_nodes", (S,)), mask.data_ptr(),
-                                             depth.data_ptr(), _stream()), "spec_tree_mask")
+                                             depth.data_ptr(), self._raw_stream()), "spec_tree_mask")
         return mask, depth
 
     def tree_attention(self, cache: KVCache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, mask: torch.Tensor, lens: torch.Tensor,
@@ -503,21 +524,25 @@ class SpecContext:
         Returns ``(out[S, N, Hq, D] bfloat16, lse[S, N, Hq] float32 or None)``; ``scale`` defaults to ``D ** -0.5``.
         """
         S, N, Hq, D = q.shape
-        _need(k.shape == v.shape and tuple(k.shape) == (S, N, cache.heads, cache.head_dim) and D == cache.head_dim and S == cache.table.shape[0],
+        _need(k.shape == v.shape and k.shape == (S, N, cache.heads, cache.head_dim) and D == cache.head_dim and S == cache.sequences,
               "tree_attention: q must be [S, N, Hq, head_dim], k and v [S, N, heads, head_dim] of the cache")
         if out is None:
-            out = (torch.empty((S, N, Hq, D), dtype=torch.bfloat16, device=q.device),
-                   torch.empty((S, N, Hq), dtype=torch.float32, device=q.device) if with_lse else None)
+            out = (_new(q), q.new_empty((S, N, Hq), dtype=torch.float32) if with_lse else None)
         else:
-            _need(out[0].shape == q.shape and (out[1] is None or out[1].shape == q.shape[:3]), "tree_attention: outputs must be [S, N, Hq, head_dim] and [S, N, Hq]")
-        need = self._lib.spec_tree_attention_bytes(self._h, cache._ref, S, N, Hq)
+            for y, shape, dtype in zip(out, (q.shape, q.shape[:3]), (torch.bfloat16, torch.float32)):
+                _need(y is None or (y.shape == shape and y.dtype == dtype and y.is_cuda and y.is_contiguous()),
+                      "tree_attention: outputs must be contiguous, bfloat16 [S, N, Hq, head_dim] and float32 [S, N, Hq]")
         if work is None:
-            work = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+            key = (S, N, Hq, cache.heads, D)
+            need = self._work_bytes.get(key)
+            if need is None:
+                need = self._work_bytes[key] = max(16, self._lib.spec_tree_attention_bytes(self._h, cache._ref, S, N, Hq))
+            work = q.new_empty(need, dtype=torch.uint8)
         self._check(self._lib.spec_tree_attention(self._h, cache._ref, *_rows(q, "q"), *_rows(k, "k"), *_rows(v, "v"), S, N, Hq,
                                                   _i32(mask, "mask", (S, N, (N + 31) // 32)), _i32(lens, "lens", (S,)),
                                                   _i32(n_nodes, "n_nodes", (S,)), D ** -0.5 if scale is None else scale,
-                                                  _ptr(out[0], torch.bfloat16), _ptr(out[1], torch.float32), work.data_ptr(), work.numel(),
-                                                  _stream()), "spec_tree_attention")
+                                                  out[0].data_ptr(), None if out[1] is None else out[1].data_ptr(), work.data_ptr(), work.numel(),
+                                                  self._raw_stream()), "spec_tree_attention")
         return out
 
     def debug_logits(self, rows: torch.Tensor) -> torch.Tensor:
