@@ -115,6 +115,19 @@ __device__ __forceinline__ float from_orderable_f32(uint32_t u) {
     return __uint_as_float((u & 0x80000000u) ? (u & 0x7FFFFFFFu) : ~u);
 }
 
+// r[j] for a j of the thread's own: registers have no addresses, so halves are chosen bit by bit.
+__device__ __forceinline__ float pick32(const uint32_t (&r)[32], int j) {
+    uint32_t a[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) a[i] = (j & 1) ? r[2 * i + 1] : r[2 * i];
+#pragma unroll
+    for (int n = 8, bit = 2; n >= 1; n >>= 1, bit <<= 1) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) a[i] = (j & bit) ? a[2 * i + 1] : a[2 * i];
+    }
+    return __uint_as_float(a[0]);
+}
+
 // Arg max of 32 consecutive columns as a tree of independent comparisons (depth 5 instead of a chain
 // of 32 dependent ones: this runs at the very end of a memory-bound launch, where nothing hides it).
 // A right-hand (higher) column wins only if strictly larger, so equal values keep the lowest column.
@@ -276,7 +289,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
-    if (threadIdx.x == 0) grid_launch_dependents();
+    if (MODE != MODE_SCORE && threadIdx.x == 0) grid_launch_dependents();
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer
@@ -490,6 +503,36 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                     sweep(as * ACC_COLS, best_v, best_i);
                     if (dual) sweep(ACC_COLS, best_v2, best_i2);
                 }
+                // Score mode, first tile of a unit: the list is empty, and all of a row's first columns would enter it in
+                // turn.  The maxima of 8 columns each say beforehand what a column has to reach: at least k_tab columns
+                // reach the k_tab-th largest of them.  (48 rows, V = 32000, 5 alternatives: 77 -> 52 us without the detour
+                // through 30 us of insertions at the end of the launch, where nothing hides them.)
+                float need = -INFINITY;
+                if (MODE == MODE_SCORE && KT > 1 && b0 == un.box_begin && n_valid >= 8 * p.k_tab) {
+                    float th[KT];
+#pragma unroll
+                    for (int j = 0; j < KT; ++j) th[j] = j < k_off ? INFINITY : -INFINITY;
+                    for (int c = 0; c * 32 < n_valid; ++c) {
+                        uint32_t r[32];
+                        __syncwarp();
+                        tmem_ld32(lane_base + as * ACC_COLS + c * 32, r);
+                        tmem_wait_ld();
+                        const int lim = n_valid - c * 32;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float v = -INFINITY;
+#pragma unroll
+                            for (int j = 8 * i; j < 8 * i + 8; ++j) v = fmaxf(v, j < lim ? __uint_as_float(r[j]) : -INFINITY);
+#pragma unroll
+                            for (int q = 0; q < KT; ++q) {  // sorted, largest first
+                                const float lo = fminf(th[q], v);
+                                th[q] = fmaxf(th[q], v);
+                                v = lo;
+                            }
+                        }
+                    }
+                    need = th[KT - 1];
+                }
                 for (int c = 0; !IS_ARGMAX && c * 32 < n_valid; ++c) {
                     uint32_t r[32];
                     __syncwarp();
@@ -526,7 +569,38 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                                 if (at == (unsigned)j && j < lim) sz = __uint_as_float(r[j]);
                         }
                     }
-                    if (MODE == MODE_TOPK || MODE == MODE_SCORE) {
+                    if (MODE == MODE_SCORE) {
+                        // Each row offers its own wanted columns (a unit's few columns are wanted by some row of the warp
+                        // nearly always, so going through the warp's columns in common would leave out hardly any).
+                        if (KT > 1) {
+                            unsigned want = 0;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                const float v = __uint_as_float(r[j]);
+                                want |= (j < lim && v > tv[KT - 1] && v >= need) ? (1u << j) : 0u;
+                            }
+                            if (row >= p.a_rows) want = 0u;  // (what lies beyond the rows is any bits)
+#pragma unroll 1
+                            while (__any_sync(0xffffffffu, want != 0u)) {
+                                const int j = want ? __ffs(want) - 1 : 0;  // ascending: equal values keep the lower id ahead
+                                const float v = want ? pick32(r, j) : -INFINITY;
+                                want &= want - 1u;
+                                const int c_id = cbase + j;
+#pragma unroll
+                                for (int q = KT - 1; q > 0; --q) {  // as below; nothing is larger than the slots above the list
+                                    const bool up = v > tv[q - 1], wr = v > tv[q];
+                                    const float nv = up ? tv[q - 1] : v;
+                                    const int ni = up ? ti[q - 1] : c_id;
+                                    tv[q] = wr ? nv : tv[q];
+                                    ti[q] = wr ? ni : ti[q];
+                                }
+                                if (v > tv[0]) {
+                                    tv[0] = v;
+                                    ti[0] = c_id;
+                                }
+                            }
+                        }
+                    } else if (MODE == MODE_TOPK) {
                         // Almost every chunk holds nothing that beats a row's current k-th value: one maximum over the
                         // 32 columns and one vote decide that.  Otherwise the columns that some row wants are fetched
                         // again one at a time (a column address is common to the warp) and offered to every row's list;
@@ -1102,88 +1176,95 @@ int launch_extend_table(spec_ctx* ctx, const int32_t* d_tab_idx, int k_tab, int 
 }
 
 // ------------------------------------------------------------------------------------------ scores of given tokens
-constexpr int SCORE_MAX_CHUNKS = 256;  // partial results per row: what a warp merges with eight lists per lane
+constexpr int SCORE_MAX_CHUNKS = 160;  // partial results per row: 32 entries of each are 40 KB of shared memory
 
-static Shape score_shape(spec_ctx* ctx, int M) { return cached_shape(ctx, M, SCORE_MAX_CHUNKS); }
+static Shape score_shape(spec_ctx* ctx, int M) { return cached_shape(ctx, M, SCORE_MAX_CHUNKS, false, false); }
+
 
 size_t score_bytes(spec_ctx* ctx, int M, int n_alt) {
     const Shape sh = score_shape(ctx, M);
     return (size_t)sh.n_chunks * M * (sizeof(float4) + (size_t)n_alt * 8);
 }
 
-// One warp per row joins the row's partial results: the statistics relative to the common maximum, then n_alt times
-// the largest head of the chunks' sorted lists (a lane looks after chunks lane, lane + 32, ...).
-__global__ void __launch_bounds__(128) merge_score_kernel(const float4* __restrict__ stat, const float* __restrict__ val,
-                                                          const int32_t* __restrict__ idx, int n_chunks, int M, int V, int n_alt,
-                                                          const int32_t* __restrict__ tokens, float* __restrict__ logp,
-                                                          float* __restrict__ entropy, int32_t* __restrict__ alt_idx,
-                                                          float* __restrict__ alt_logp, int* status) {
-    const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+// One CTA per row joins the row's partial results: warp 1 the statistics, relative to the common maximum; all threads
+// bring the chunks' sorted lists into shared memory, and warp 0 takes the largest of their heads n_alt times (a lane looks
+// after chunks lane, lane + 32, ...).
+constexpr int MERGE_THREADS = 128, MERGE_LISTS = SCORE_MAX_CHUNKS / 32;
+__global__ void __launch_bounds__(MERGE_THREADS) merge_score_kernel(const float4* stat, const float* val, const int32_t* idx, int n_chunks, int M,
+                                                                    int V, int n_alt, const int32_t* __restrict__ tokens,
+                                                                    float* __restrict__ logp, float* __restrict__ entropy,
+                                                                    int32_t* __restrict__ alt_idx, float* __restrict__ alt_logp, int* status) {
+    extern __shared__ unsigned long long keys[];  // [n_chunks, n_alt], ordered by value, then lower id
+    __shared__ float2 norm;                       // the row's maximum and the logarithm of its sum
+    const int row = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     grid_dependency_wait();
     grid_launch_dependents();
-    if (row >= M) return;
-    float4 s[SCORE_MAX_CHUNKS / 32];
-    float m = -INFINITY;
+    if (warp == 1) {
+        float4 s[MERGE_LISTS];
+        float m = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < SCORE_MAX_CHUNKS / 32; ++i) {
-        const int c = lane + 32 * i;
-        s[i] = c < n_chunks ? stat[(size_t)c * M + row] : make_float4(-INFINITY, 0.0f, 0.0f, -INFINITY);
-        m = fmaxf(m, s[i].x);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    float l = 0.0f, t = 0.0f, z = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < SCORE_MAX_CHUNKS / 32; ++i) {
-        const float shift = s[i].x == -INFINITY ? -200.0f : (s[i].x - m) * LOG2E, f = exp2f(shift);
-        l += s[i].y * f;
-        t += (s[i].z + shift * s[i].y) * f;
-        z = fmaxf(z, s[i].w);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        l += __shfl_xor_sync(0xffffffffu, l, o);
-        t += __shfl_xor_sync(0xffffffffu, t, o);
-        z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, o));
-    }
-    const float log_l = logf(l);
-    if (lane == 0) {
-        const int tok = tokens[row];
-        if (tok != -1 && (unsigned)tok >= (unsigned)V) atomicOr(status, SPEC_STATUS_TOKEN_RANGE);
-        logp[row] = tok == -1 ? 0.0f : (z - m) - log_l;  // (an id outside the vocabulary met no column: -inf)
-        entropy[row] = log_l - LN2 * (t / l);
-    }
-    int head[SCORE_MAX_CHUNKS / 32];
-#pragma unroll
-    for (int i = 0; i < SCORE_MAX_CHUNKS / 32; ++i) head[i] = 0;
-    for (int k = 0; k < n_alt; ++k) {
-        unsigned long long best = 0ull;
-        int from = 0;
-#pragma unroll
-        for (int i = 0; i < SCORE_MAX_CHUNKS / 32; ++i) {
+        for (int i = 0; i < MERGE_LISTS; ++i) {
             const int c = lane + 32 * i;
-            if (c < n_chunks && head[i] < n_alt) {
-                const size_t at = ((size_t)c * M + row) * n_alt + head[i];
-                const unsigned long long key = ((unsigned long long)orderable_f32(val[at]) << 32) | (uint32_t)~idx[at];
-                if (key > best) {
-                    best = key;
-                    from = i;
-                }
-            }
+            s[i] = c < n_chunks ? stat[(size_t)c * M + row] : make_float4(-INFINITY, 0.0f, 0.0f, -INFINITY);
+            m = fmaxf(m, s[i].x);
         }
-        unsigned long long top = best;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        float l = 0.0f, t = 0.0f, z = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < MERGE_LISTS; ++i) {
+            const float shift = s[i].x == -INFINITY ? -200.0f : (s[i].x - m) * LOG2E, f = exp2f(shift);
+            l += s[i].y * f;
+            t += (s[i].z + shift * s[i].y) * f;
+            z = fmaxf(z, s[i].w);
+        }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
-            const unsigned long long other = __shfl_xor_sync(0xffffffffu, top, o);
-            top = other > top ? other : top;
-        }
-        if (best == top) {  // ids are distinct: one lane
-#pragma unroll
-            for (int i = 0; i < SCORE_MAX_CHUNKS / 32; ++i) head[i] += i == from;
+            l += __shfl_xor_sync(0xffffffffu, l, o);
+            t += __shfl_xor_sync(0xffffffffu, t, o);
+            z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, o));
         }
         if (lane == 0) {
-            alt_idx[(size_t)row * n_alt + k] = (int32_t)~(uint32_t)top;
-            alt_logp[(size_t)row * n_alt + k] = (from_orderable_f32((uint32_t)(top >> 32)) - m) - log_l;
+            const int tok = tokens[row];
+            const float log_l = logf(l);
+            if (tok != -1 && (unsigned)tok >= (unsigned)V) atomicOr(status, SPEC_STATUS_TOKEN_RANGE);
+            logp[row] = tok == -1 ? 0.0f : (z - m) - log_l;  // (an id outside the vocabulary met no column: -inf)
+            entropy[row] = log_l - LN2 * (t / l);
+            norm = make_float2(m, log_l);
+        }
+    }
+    if (n_alt == 0) return;
+    for (int i = threadIdx.x; i < n_chunks * n_alt; i += MERGE_THREADS) {
+        const int c = i / n_alt;
+        const size_t at = ((size_t)c * M + row) * n_alt + (i - c * n_alt);
+        keys[i] = ((unsigned long long)orderable_f32(val[at]) << 32) | (uint32_t)~idx[at];
+    }
+    __syncthreads();
+    if (warp != 0) return;
+    int head[MERGE_LISTS];
+    unsigned long long key[MERGE_LISTS];
+#pragma unroll
+    for (int i = 0; i < MERGE_LISTS; ++i) {
+        head[i] = (lane + 32 * i) * n_alt;
+        key[i] = lane + 32 * i < n_chunks ? keys[head[i]] : 0ull;
+    }
+    for (int k = 0; k < n_alt; ++k) {
+        unsigned long long best = key[0];
+#pragma unroll
+        for (int i = 1; i < MERGE_LISTS; ++i) best = key[i] > best ? key[i] : best;
+        // the largest of all lanes: of the upper words first, then of the lower words that go with it
+        const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32));
+        const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32) == hi ? (uint32_t)best : 0u);
+        const unsigned long long top = ((unsigned long long)hi << 32) | lo;
+#pragma unroll
+        for (int i = 0; i < MERGE_LISTS; ++i)
+            if (key[i] == top) {  // ids are distinct: one list
+                const int next = ++head[i];
+                key[i] = next < (lane + 32 * i + 1) * n_alt ? keys[next] : 0ull;
+            }
+        if (lane == 0) {
+            alt_idx[(size_t)row * n_alt + k] = (int32_t)~lo;
+            alt_logp[(size_t)row * n_alt + k] = (from_orderable_f32(hi) - norm.x) - norm.y;
         }
     }
 }
@@ -1207,7 +1288,7 @@ int launch_score(spec_ctx* ctx, const void* d_hidden, int M, const int32_t* d_to
     auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(sh.grid), dim3(GEMM_THREADS), (size_t)sh.smem, st, tmA, tmA, *tmW, p); };
     cudaError_t e = n_alt == 0 ? go(head_gemm_kernel<MODE_SCORE, 1>) : (n_alt <= 8 ? go(head_gemm_kernel<MODE_SCORE, 8>) : go(head_gemm_kernel<MODE_SCORE, 32>));
     if ((rc = check_cuda(ctx, e, "score_tokens launch"))) return rc;
-    e = launch_pdl(merge_score_kernel, dim3((M + 3) / 4), dim3(128), 0, st, p.part_stat, p.part_val, p.part_idx, sh.n_chunks, M, ctx->V, n_alt,
+    e = launch_pdl(merge_score_kernel, dim3(M), dim3(MERGE_THREADS), sizeof(unsigned long long) * sh.n_chunks * n_alt, st, p.part_stat, p.part_val, p.part_idx, sh.n_chunks, M, ctx->V, n_alt,
                    d_tokens, d_logp, d_entropy, d_alt_idx, d_alt_logp, ctx->d_status);
     ctx->launches += 2;
     return check_cuda(ctx, e, "score_tokens merge launch");

@@ -307,7 +307,6 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (threadIdx.x == 0) grid_launch_dependents();
     grid_dependency_wait();
     const uint32_t tmem = sh.tmem;
     const uint32_t full = smem_u32(&sh.full[0]), empty = smem_u32(&sh.empty[0]), go = smem_u32(&sh.go[0]), stg_full = smem_u32(&sh.stg_full[0]), stg_empty = smem_u32(&sh.stg_empty[0]);
