@@ -769,6 +769,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 tc_fence_after();
                 return got;
             };
+            auto ready = [&]() { return mbar_test_wait(full + 8 * slot, phase); };
             // (descriptors of the first k-slice; the others are a constant further in their address field)
             const uint64_t q_desc = make_kmajor_sw128_desc(q_at), k_desc = make_kmajor_sw128_desc(0), v_desc = make_mnmajor_sw128_desc(0, TILE * 128);
             auto qk = [&](int stream, int q_tile, uint32_t k_at) {
@@ -800,23 +801,26 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     qk(0, 0, k_at);
                     qk(1, 1, k_at);
                     tc_commit(empty + 8 * ki);
+                    // (what can be done before the weights are there, or after the scores are on their way, is: the chain
+                    // from a stream's weights to its next scores is what the pace depends on)
                     for (int t = 0; t < n && ok; ++t) {
+                        const bool more = t + 1 < n;
                         if (!(ok = take(v_at, vi))) break;
+                        const bool early = more && ready();  // the next keys: looked at once before, waited for only after
+                        if (early) take(k_at, ki);
                         if (!(ok = wait(p_full, n_p[0]++ & 1u))) break;
                         tc_fence_after();
                         pv(0, v_at, t > 0);
-                        if (t + 1 < n) {
-                            if (!(ok = take(k_at, ki))) break;
+                        if (more) {
+                            if (!early && !(ok = take(k_at, ki))) break;
                             qk(0, 0, k_at);
                         }
                         if (!(ok = wait(p_full + 8, n_p[1]++ & 1u))) break;
                         tc_fence_after();
                         pv(1, v_at, t > 0);
+                        if (more) qk(1, 1, k_at);
                         tc_commit(empty + 8 * vi);
-                        if (t + 1 < n) {
-                            qk(1, 1, k_at);
-                            tc_commit(empty + 8 * ki);
-                        }
+                        if (more) tc_commit(empty + 8 * ki);
                     }
                 } else {  // one row tile, alternate keys
                     for (int t = 0; t < 2 && t < n && ok; ++t) {
@@ -826,16 +830,19 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     }
                     for (int t = 0; t < n && ok; ++t) {
                         const int i = t & 1;
+                        const bool more = t + 2 < n;
                         if (!(ok = take(v_at, vi))) break;
+                        const bool early = more && ready();
+                        if (early) take(k_at, ki);
                         if (!(ok = wait(p_full + 8 * i, n_p[i]++ & 1u))) break;
                         tc_fence_after();
                         pv(i, v_at, t > 1);
-                        tc_commit(empty + 8 * vi);
-                        if (t + 2 < n) {
-                            if (!(ok = take(k_at, ki))) break;
+                        if (more) {
+                            if (!early && !(ok = take(k_at, ki))) break;
                             qk(i, 0, k_at);
-                            tc_commit(empty + 8 * ki);
                         }
+                        tc_commit(empty + 8 * vi);
+                        if (more) tc_commit(empty + 8 * ki);
                     }
                 }
                 if (!ok) break;
