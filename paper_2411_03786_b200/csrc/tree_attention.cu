@@ -188,15 +188,18 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 // Four E4M3 codes times a power of two as bfloat16, two to a word: a code's sign, exponent and mantissa moved into a
-// bfloat16's fields read as its value times 2^-120 (subnormals as subnormals), and `f` holds scale * 2^120.
+// bfloat16's fields read as its value times 2^-120 (subnormals as subnormals), and `f` holds scale * 2^120.  (The integer
+// pipe is what converting is bound by: it has the shift to the right, the masks and the two joins, 6 instructions; the
+// shift to the left is a multiplication.)
 __device__ __forceinline__ void e4m3x4_bf16x4(uint32_t w, uint32_t f, uint32_t& lo, uint32_t& hi) {
-    const uint32_t low = (w << 4) & 0xF0F0F0F0u, high = ((w >> 4) & 0x07070707u) | (w & 0x80808080u);  // the bytes of the results
+    uint32_t left;
+    asm("mul.lo.u32 %0, %1, 16;" : "=r"(left) : "r"(w));
+    const uint32_t low = left & 0xF0F0F0F0u, high = ((w >> 4) & 0x07070707u) | (w & 0x80808080u);  // the bytes of the results
     lo = mul_bf16x2(__byte_perm(low, high, 0x5140), f);
     hi = mul_bf16x2(__byte_perm(low, high, 0x7362), f);
 }
 __device__ __forceinline__ uint32_t scale_bf16x2(uint32_t exp) {
-    const uint32_t b = exp > 127u + E8_MAX ? 0x7FC0u : (exp + 120u) << 7;  // beyond the largest: NaN
-    return b | (b << 16);
+    return exp > 127u + E8_MAX ? 0x7FC07FC0u : (exp + 120u) * 0x00800080u;  // beyond the largest: NaN
 }
 __device__ __forceinline__ void st_shared16(uint32_t addr, const uint4& v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
@@ -578,30 +581,37 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     if (!wait(stg_full + 8 * stg, stg_phase)) return false;
                     if (!wait(bar_empty, my_phase ^ 1u)) return false;
                     const uint32_t src = stg_at + stg * Geo::STAGE_BYTES, ex = exp_at + stg * TILE;
-                    constexpr int LPR = D / 16;
-                    const bool swap = (tid & 4) != 0 && D == 128;  // so that the 8 lanes of a phase write to different banks
-                    constexpr int PER = TILE * LPR / LOADERS;
-                    const int c = tid % LPR;
+                    // A thread has 16 codes of rows 32 (D = 64: 64) apart, a staging row's pieces dealt out so that the 8 lanes
+                    // that load or store together meet in no bank: lanes 0-3 the front of row r, 4-7 the back of row r + 1,
+                    // the next 8 the other two (the swizzle turns even pieces of one row into odd ones of the next).
+                    constexpr int LPR = D / 16, PER = TILE * LPR / LOADERS, STEP = LOADERS / LPR;
+                    const int r = D == 64 ? tid / LPR : (tid / 16) * 2 + (((tid >> 3) ^ (tid >> 2)) & 1), c = D == 64 ? tid % LPR : (tid & 7);
+                    const uint32_t from = src + r * D + c * 16, to = dst + tile_at(r, 2 * c);
                     uint4 v[PER];
                     uint32_t e[PER];
 #pragma unroll
                     for (int i = 0; i < PER; ++i) {
-                        const int r = i * (LOADERS / LPR) + tid / LPR;
-                        v[i] = ld_shared16(src + r * D + c * 16);
-                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e[i]) : "r"(ex + r) : "memory");
+                        v[i] = ld_shared16(from + i * STEP * D);
+                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e[i]) : "r"(ex + r + i * STEP) : "memory");
+                    }
+                    if (rows < TILE) {  // (whatever the staging tile held)
+#pragma unroll
+                        for (int i = 0; i < PER; ++i)
+                            if (r + i * STEP >= rows) {
+                                v[i] = make_uint4(0, 0, 0, 0);
+                                e[i] = 127;
+                            }
                     }
 #pragma unroll
                     for (int i = 0; i < PER; ++i) {
-                        const int r = i * (LOADERS / LPR) + tid / LPR;
                         const uint32_t f = scale_bf16x2(e[i]);
                         uint4 lo, hi;
                         e4m3x4_bf16x4(v[i].x, f, lo.x, lo.y);
                         e4m3x4_bf16x4(v[i].y, f, lo.z, lo.w);
                         e4m3x4_bf16x4(v[i].z, f, hi.x, hi.y);
                         e4m3x4_bf16x4(v[i].w, f, hi.z, hi.w);
-                        if (r >= rows) lo = hi = make_uint4(0, 0, 0, 0);  // (whatever the staging tile held)
-                        st_shared16(dst + tile_at(r, 2 * c + (swap ? 1 : 0)), swap ? hi : lo);
-                        st_shared16(dst + tile_at(r, 2 * c + (swap ? 0 : 1)), swap ? lo : hi);
+                        st_shared16(to + i * STEP * 128, lo);
+                        st_shared16((to ^ 16u) + i * STEP * 128, hi);
                     }
                     mbar_arrive(stg_empty + 8 * stg);
                     if (++stg == Geo::STAGES) {
