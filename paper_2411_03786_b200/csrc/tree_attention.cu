@@ -565,7 +565,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         uint32_t go_phase = 0;  // bit per slot
         for (;; ++n_seg) {
             if (!segment_there()) break;
-            const Segment& g = segment();
+            const Segment g = segment();  // (in registers: shared memory is looked at again after every barrier)
             if (!g.more) break;
             const bool ok = for_each_tile(g, [&](bool is_v, int t) {
                 const bool block = t >= g.n_prefix;
@@ -698,7 +698,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             bool ok = true;
             for (;; ++n_seg) {
                 ok = __all_sync(0xffffffffu, segment_there());
-                const Segment& g = segment();
+                const Segment g = segment();
                 if (!ok || !g.more) break;
                 const int32_t* table = cache.table + (long long)g.s * cache.max_pages;
                 const int n_pages = (g.len + page - 1) >> cache.page_shift;
