@@ -508,8 +508,8 @@ static int check_cache(spec_ctx* ctx, const spec_kv_cache* c, const char* who, C
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128)
         return fail(ctx, SPEC_ERR_UNSUPPORTED, "%s: page must be 16, 32, 64 or 128 tokens", who);
     if (c->heads < 1 || c->n_pages < 1 || c->max_pages < 1 || (long long)c->n_pages * c->heads * c->page >= (1ll << 31) ||
-        (long long)c->max_pages * c->page >= (1ll << 31))
-        return fail(ctx, SPEC_ERR_ARG, "%s: need heads, n_pages, max_pages >= 1, n_pages * heads * page < 2^31 and max_pages * page < 2^31", who);
+        (long long)c->max_pages * c->page > (1ll << 30))
+        return fail(ctx, SPEC_ERR_ARG, "%s: need heads, n_pages, max_pages >= 1, n_pages * heads * page < 2^31 and max_pages * page <= 2^30", who);
     int shift = 4;
     while ((1 << shift) < c->page) ++shift;
     *out = CacheArgs{c->d_k, c->d_v, c->d_k_exp, c->d_v_exp, c->d_table, c->n_pages, c->max_pages, shift, c->heads, c->head_dim, c->dtype == SPEC_E4M3};
@@ -592,6 +592,7 @@ static int check_block(spec_ctx* ctx, const spec_kv_cache* cache, int S, int N, 
     if (rc) return rc;
     if (S < 0 || S > 65535 || N < 1 || N > kMaxNodes) return fail(ctx, SPEC_ERR_ARG, "%s: need 0 <= S <= 65535, 1 <= N <= %d", who, kMaxNodes);
     if (Hq < c->heads || Hq % c->heads != 0 || Hq > 4096) return fail(ctx, SPEC_ERR_ARG, "%s: Hq must be a multiple of the cache's heads, at most 4096", who);
+    if ((long long)N * (Hq / c->heads) > (1 << 22)) return fail(ctx, SPEC_ERR_ARG, "%s: N * Hq / heads exceeds 2^22", who);
     return SPEC_OK;
 }
 

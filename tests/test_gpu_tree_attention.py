@@ -202,6 +202,31 @@ def test_extreme_scores(ctx):
     au.check_attention(got, au.attention(q, k, v, flat.double(), hv, mask, [L], D ** -0.5), 2.0 ** -7)
 
 
+@pytest.mark.parametrize("quantised", [False, True])
+def test_offsets_beyond_32_bits(ctx, quantised):
+    """A pool of pages in which bytes (and, in bfloat16, elements) are numbered beyond 2^31: its last pages behave like the first of a small one."""
+    import paper_2411_03786_b200 as ngs
+    S, N, Hkv, D, page, L = 2, 9, 4, 128, 64, 300
+    n_pages = (1 << 16) + 70  # 16.8 million vectors of 128
+    per = -(-(L + 3) // page)
+    small, _, _ = au.make_cache(S, L + 3, Hkv, D, page, quantised, 3, spare=0)
+    table = (small.table.long() + n_pages - S * per).int()
+    big = ngs.KVCache.empty(n_pages, Hkv, page, D, table, quantised)
+    for a, b in ((small.k, big.k), (small.v, big.v), (small.k_exp, big.k_exp), (small.v_exp, big.v_exp)):
+        if a is not None:
+            b[n_pages - S * per:] = a
+    assert big.k.numel() > 1 << 31
+    q, k, v = block(S, N, 8, Hkv, D, 4)
+    mask = au.pack(au.ancestors(parents(S, N, "tree", 5))).cuda()
+    lens = torch.tensor([L, 130], dtype=torch.int32).cuda()
+    out = []
+    for c in (small, big):
+        a = ctx.tree_attention(c, q, k, v, mask, lens, with_lse=True)
+        ctx.cache_write(c, k, v, lens, count=torch.full((S,), 3, dtype=torch.int32).cuda())
+        out.append((*a, *ctx.cache_read(c, torch.zeros_like(lens), L + 3)))
+    assert all(torch.equal(x, y) for x, y in zip(*out)) and ctx.get_status() == 0
+
+
 def test_same_result_every_time_and_on_another_stream(ctx):
     cache, _, _ = au.make_cache(3, 3000, 2, 128, 64, True, 4)
     q, k, v = block(3, 50, 8, 2, 128, 5)
