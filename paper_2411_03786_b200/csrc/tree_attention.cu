@@ -63,6 +63,7 @@ struct AttParams {
 struct Segment {
     int s, h, qt, t0, t1, n_prefix, len, live, rows;
     int whole;  // all key tiles of the (s, h)
+    int split;  // the streams take the even and the odd key tiles; else a row tile each
     int slot;   // partial result: 0 = the CTA's range starts here, 1 = it ends here
     int more;   // 0: there was none left
 };
@@ -128,6 +129,7 @@ struct Walk {
     int s, h, t, pass, slot;
     long long pos, hi;
 };
+template <bool Q8>
 __device__ __forceinline__ void advance(const AttParams& p, Walk& w, Segment& g) {
     int rows = 0;
     while (w.pos < w.hi && rows <= 0) {
@@ -146,6 +148,10 @@ __device__ __forceinline__ void advance(const AttParams& p, Walk& w, Segment& g)
                 g.len = len;
                 g.live = live;
                 g.whole = g.t1 - g.t0 == n_tiles;
+                // (a last single row tile beside pairs of the same keys: an E4M3 cache's tiles are converted for it alone, and
+                // two at a time take longer than one
+                // for both streams; 64 sequences of 144 nodes, 4 heads to a key head, 2048 keys: 657 us so, 761 us split)
+                g.split = rows <= TILE && (!Q8 || qt == 0);
                 g.slot = w.slot;
                 w.slot = 1;
             }
@@ -171,7 +177,7 @@ __device__ __forceinline__ void advance(const AttParams& p, Walk& w, Segment& g)
 // `lead`: streams that start side by side on different tiles (2 if they split the keys).
 template <typename F>
 __device__ __forceinline__ bool for_each_tile(const Segment& g, F&& f) {
-    const int lead = g.rows > TILE ? 1 : 2;
+    const int lead = g.split ? 2 : 1;
     const int t1 = g.t1;
     int k = g.t0, v = k;
     while (v < t1) {  // (one call of f: it is inlined)
@@ -346,7 +352,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             const bool there = __all_sync(0xffffffffu, segment_there());
             const Segment& g = segment();
             if (meet(!there || !g.more)) break;
-            const bool split = g.rows <= TILE;  // the streams split the keys
+            const bool split = g.split;
             const int tile_row = (split ? 0 : stream * TILE) + wq * 32 + lane;
             const bool valid = tile_row < g.rows;
             const bool warp_on = (split ? 0 : stream * TILE) + wq * 32 < g.rows;
@@ -806,7 +812,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 uint32_t k_at, v_at, ki, vi;
                 if (!(ok = wait(q_full, n_seg & 1u))) break;
                 tc_fence_after();
-                if (g.rows > TILE) {  // two row tiles, the same keys
+                if (!g.split) {  // two row tiles, the same keys
                     if (!(ok = take(k_at, ki))) break;
                     qk(0, 0, k_at);
                     qk(1, 1, k_at);
@@ -918,7 +924,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 for (uint32_t k = 0;; ++k) {
                     if (!wait(seg_empty + 8 * (k % SEGMENTS), ((k / SEGMENTS) & 1u) ^ 1u)) break;
                     Segment& g = sh.segment[k % SEGMENTS];
-                    advance(p, w, g);
+                    advance<Q8>(p, w, g);
                     const int more = g.more;
                     mbar_arrive(seg_full + 8 * (k % SEGMENTS));
                     if (!more) break;
