@@ -37,7 +37,7 @@
 
 namespace ngs {
 
-constexpr int SOFTMAX_WARPS = 16, LOADER_WARPS = 8, LOADERS = 32 * LOADER_WARPS, TMA_WARP = 24, MMA_WARP = 25, PLAN_WARP = 26;
+constexpr int SOFTMAX_WARPS = 16, LOADER_WARPS = 8, LOADERS = 32 * LOADER_WARPS, TMA_WARP = 24, MMA_WARP = 25, PLAN_WARP = 26, BLANK_WARP = 27;
 constexpr int TILE = 128;  // keys of a tile and rows of a row tile
 constexpr int ATT_SMEM = 227 * 1024;
 constexpr int ATT_THREADS = 896;  // whole warpgroups, which is what registers are moved between
@@ -53,7 +53,7 @@ struct AttParams {
     int G, n_qtiles, side, n_groups, passes;  // side: row-tile pairs that run side by side
     int rows_cap;                             // rows of a partial result
     float c;                                  // scale * log2(e)
-    long long* cum;                           // [S + 1] places (see Ranges) of a key head of the sequences before
+    struct JoinTask* tasks;                   // [grid]
     float2* part_ml;                          // [grid * 2, rows_cap]
     float* part_o;                            // [grid * 2, D / 4, rows_cap, 4]
     unsigned long long wait_limit_ns;
@@ -66,6 +66,13 @@ struct Segment {
     int split;  // the streams take the even and the odd key tiles; else a row tile each
     int slot;   // partial result: 0 = the CTA's range starts here, 1 = it ends here
     int more;   // 0: there was none left
+};
+// An (s, h) and row-tile pair that several CTAs walked: its partial rows are joined.  Recorded by the second of them.
+struct __align__(16) JoinTask {
+    int s, h, qt, rows;
+    int n;      // parts; 0: nothing to join
+    int first;  // slot of the first CTA's part
+    int pad[2];
 };
 struct AttShared {
     uint64_t full[8], empty[8], go[8], stg_full[6], stg_empty[6], s_full[2], p_full[2], o_full, q_full, xch, seg_full[SEGMENTS], seg_empty[SEGMENTS];
@@ -900,11 +907,6 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 const int s = s0 + lane;
                 const int n = s0 == 0 ? n_first : (s < a.S ? places(sequence_tiles(a, s, len, live, np)) : 0);
                 const long long upto = before + (s0 == 0 ? first_upto : scan(n));
-                if (blockIdx.x == 0 && s < a.S) {
-                    p.cum[s + 1] = upto;
-                    if (s == 0) p.cum[0] = 0;
-                    if (a.len[s] < 0 || (long long)a.len[s] > ((long long)cache.max_pages << cache.page_shift)) atomicOr(a.status, SPEC_STATUS_CAPACITY);
-                }
                 const long long from = (upto - n) * cache.heads;
                 if (n > 0 && x >= from && x < upto * cache.heads) {
                     mine = 1;
@@ -913,14 +915,18 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     w.t = (int)(x - from - (long long)w.h * n);
                 }
                 before = __shfl_sync(0xffffffffu, upto, 31);
-                if (blockIdx.x != 0 && before * cache.heads > x) break;
+                if (before * cache.heads > x) break;
             }
             const unsigned who = __ballot_sync(0xffffffffu, mine);
             const int src = who ? __ffs(who) - 1 : 0;
+            const int first_pass = w.pass;
             w.s = __shfl_sync(0xffffffffu, w.s, src);
             w.h = __shfl_sync(0xffffffffu, w.h, src);
             w.t = __shfl_sync(0xffffffffu, w.t, src);
             if (lane == 0) {
+                const int s = w.s, h = w.h, t = w.t;
+                const long long u0 = w.pos - t;  // the first place of the (s, h)
+                const bool inside = w.pos < w.hi && t > START;  // an (s, h) has tiles before this range
                 for (uint32_t k = 0;; ++k) {
                     if (!wait(seg_empty + 8 * (k % SEGMENTS), ((k / SEGMENTS) & 1u) ^ 1u)) break;
                     Segment& g = sh.segment[k % SEGMENTS];
@@ -928,6 +934,36 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     const int more = g.more;
                     mbar_arrive(seg_full + 8 * (k % SEGMENTS));
                     if (!more) break;
+                }
+                JoinTask task = {s, h, first_pass * p.side + (int)(blockIdx.x % p.side), 0, 0, 0, {0, 0}};
+                if (inside && u0 + START >= ranges.begin(group - 1) && task.qt < p.n_qtiles) {
+                    const int n = places(sequence_tiles(a, s, len, live, np));
+                    task.rows = min(2 * TILE, live * p.G - task.qt * 2 * TILE);
+                    task.n = task.rows > 0 ? (int)(ranges.group_of(u0 + n - 1) - group) + 2 : 0;
+                    task.first = u0 > ranges.begin(group - 1);  // that range begins with another (s, h)
+                }
+                p.tasks[blockIdx.x] = task;
+            }
+        } else if (warp == BLANK_WARP) {
+            // -------------------------------------------------------------------------------- nodes that are not live
+            const long long n_nodes = (long long)a.S * a.N;
+            for (long long i0 = 32ll * blockIdx.x; i0 < n_nodes; i0 += 32ll * gridDim.x) {
+                const long long i = i0 + lane;
+                bool blank = false;
+                if (i < n_nodes) {
+                    const int s = (int)quotient(i, a.N), node = (int)(i - (long long)s * a.N);
+                    int len, live, np;
+                    sequence_tiles(a, s, len, live, np);
+                    blank = node >= live;
+                    if (node == 0 && (a.len[s] < 0 || (long long)a.len[s] > ((long long)cache.max_pages << cache.page_shift)))
+                        atomicOr(a.status, SPEC_STATUS_CAPACITY);
+                }
+                for (unsigned left = __ballot_sync(0xffffffffu, blank); left; left &= left - 1) {
+                    const long long at = (i0 + __ffs(left) - 1) * a.Hq;
+                    uint4* out = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + at * D);
+                    for (int j = lane; j < a.Hq * (D / 8); j += 32) out[j] = make_uint4(0, 0, 0, 0);
+                    if (a.lse)
+                        for (int j = lane; j < a.Hq; j += 32) a.lse[at + j] = -INFINITY;
                 }
             }
         }
@@ -939,35 +975,22 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
 }
 
 // Joins the partial rows of every (s, h, row-tile pair) whose key tiles were spread over several CTAs, in the CTAs'
-// order, and writes the rows that attend to nothing.  A lane per row, 16 columns per warp.
+// order.  A lane per row, 16 columns per warp.
 template <int D>
 __global__ void __launch_bounds__(2 * D) join_kernel(const __grid_constant__ AttParams p) {
     const TreeAttnArgs& a = p.a;
     const int lane = threadIdx.x & 31, cols = threadIdx.x >> 5;  // columns [16 cols, 16 cols + 16)
     grid_launch_dependents();
     grid_dependency_wait();
-    const int s = (int)(blockIdx.x / a.cache.heads), h = (int)(blockIdx.x % a.cache.heads), qt = blockIdx.y;
-    const int r = blockIdx.z * 32 + lane;
-    int len, live, np;
-    const int tiles = sequence_tiles(a, s, len, live, np);
-    const long long per_pass = p.cum[a.S] * a.cache.heads;
-    const Ranges ranges(p, per_pass * p.passes);
-    if (r >= min(2 * TILE, a.N * p.G - qt * 2 * TILE)) return;
-    const int R = qt * 2 * TILE + r, node = R / p.G, gq = R - node * p.G;
-    const long long out_row = ((long long)s * a.N + node) * a.Hq + h * p.G + gq;
+    const int cta = p.side + blockIdx.x, r = blockIdx.y * 32 + lane;
+    const JoinTask task = p.tasks[cta];
+    const int n = task.n;
+    if (n == 0 || r >= task.rows) return;
+    const int R = task.qt * 2 * TILE + r, node = R / p.G, gq = R - node * p.G;
+    const long long out_row = ((long long)task.s * a.N + node) * a.Hq + task.h * p.G + gq;
     uint4* out = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + out_row * D + 16 * cols);
-    if (node >= live) {
-        out[0] = out[1] = make_uint4(0, 0, 0, 0);
-        if (a.lse && cols == 0) a.lse[out_row] = -INFINITY;
-        return;
-    }
-    const long long u0 = (qt / p.side) * per_pass + p.cum[s] * a.cache.heads + (long long)h * (tiles + START), u1 = u0 + START + tiles;
-    const int g0 = (int)ranges.group_of(u0 + START), g1 = (int)ranges.group_of(u1 - 1);  // of the first and the last tile
-    if (g0 == g1) return;
-    // the first group's range may begin with another (s, h): then its part is the one at the range's end
-    const long long at0 = ((long long)g0 * p.side + qt % p.side) * 2 + (u0 > ranges.begin(g0) ? 1 : 0), at1 = ((long long)(g0 + 1) * p.side + qt % p.side) * 2;
+    const long long at0 = 2ll * (cta - p.side) + task.first, at1 = 2ll * cta;
     auto part = [&](int i) { return i == 0 ? at0 : at1 + (long long)(i - 1) * p.side * 2; };
-    const int n = g1 - g0 + 1;
     float m = -INFINITY, l = 0.0f, x[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) x[j] = 0.0f;
@@ -1015,11 +1038,11 @@ static void plan(int num_sms, int S, int N, int Hq, int heads, int head_dim, Att
     p.passes = (p.n_qtiles + p.side - 1) / p.side;
     p.rows_cap = std::min(2 * TILE, rows);
     const size_t parts = (size_t)p.n_groups * p.side * 2 * p.rows_cap;
-    const size_t cum = ((size_t)S + 2) / 2 * 16;
-    p.cum = nullptr;
-    p.part_o = reinterpret_cast<float*>(cum);
-    p.part_ml = reinterpret_cast<float2*>(cum + parts * head_dim * 4);
-    bytes = cum + parts * (head_dim * 4 + 8);
+    const size_t tasks = (size_t)p.n_groups * p.side * sizeof(JoinTask);
+    p.tasks = nullptr;
+    p.part_o = reinterpret_cast<float*>(tasks);
+    p.part_ml = reinterpret_cast<float2*>(tasks + parts * head_dim * 4);
+    bytes = tasks + parts * (head_dim * 4 + 8);
 }
 
 size_t tree_attention_bytes(int num_sms, int S, int N, int Hq, int heads, int head_dim) {
@@ -1083,8 +1106,10 @@ static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
         return rc;
     cudaError_t e = launch_pdl(kernel, dim3(p.n_groups * p.side), dim3(ATT_THREADS), (size_t)Geometry<D, Q8>::SMEM, st, tm_k, tm_v, tm_bk, tm_bv, p);
     if ((rc = check_cuda(ctx, e, "spec_tree_attention launch"))) return rc;
-    e = launch_pdl(join_kernel<D>, dim3(p.a.S * p.a.cache.heads, p.n_qtiles, (p.rows_cap + 31) / 32), dim3(2 * D), 0, st, p);
-    ctx->launches += 2;
+    ++ctx->launches;
+    if (p.n_groups == 1) return SPEC_OK;  // nothing is spread
+    e = launch_pdl(join_kernel<D>, dim3((p.n_groups - 1) * p.side, (p.rows_cap + 31) / 32), dim3(2 * D), 0, st, p);
+    ++ctx->launches;
     return check_cuda(ctx, e, "spec_tree_attention join launch");
 }
 
@@ -1094,7 +1119,7 @@ int launch_tree_attention(spec_ctx* ctx, const TreeAttnArgs& a, cudaStream_t st)
     plan(ctx->num_sms, a.S, a.N, a.Hq, a.cache.heads, a.cache.head_dim, p, bytes);
     p.a = a;
     p.c = a.scale * LOG2E;
-    p.cum = reinterpret_cast<long long*>(a.work);
+    p.tasks = reinterpret_cast<JoinTask*>(a.work);
     p.part_o = reinterpret_cast<float*>((char*)a.work + (size_t)p.part_o);
     p.part_ml = reinterpret_cast<float2*>((char*)a.work + (size_t)p.part_ml);
     p.wait_limit_ns = WAIT_LIMIT_NS;

@@ -117,6 +117,12 @@ def test_live_nodes(ctx):
     assert (got[0][2] == 0).all() and (got[1][2] == -math.inf).all()
 
 
+@pytest.mark.parametrize("quantised", [False, True])
+def test_live_nodes_over_row_tiles(ctx, quantised):
+    """Sequences whose live rows fill three row tiles, end in the third, the second or the first, side by side."""
+    run(ctx, 6, 150, 4, 2, 128, [300, 40, 1000, 257, 0, 129], 64, quantised, live=[150, 129, 128, 65, 64, 3], seed=6)
+
+
 def test_scale_argument(ctx):
     run(ctx, 1, 8, 2, 1, 64, [300], 16, False, scale=0.02)
 
