@@ -505,8 +505,8 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                 }
                 // Score mode, first tile of a unit: the list is empty, and all of a row's first columns would enter it in
                 // turn.  The maxima of 8 columns each say beforehand what a column has to reach: at least k_tab columns
-                // reach the k_tab-th largest of them.  (48 rows, V = 32000, 5 alternatives: 77 -> 52 us without the detour
-                // through 30 us of insertions at the end of the launch, where nothing hides them.)
+                // reach the k_tab-th largest of them.  (48 rows, V = 32000, 5 alternatives: 55 us; 77 us with all
+                // the insertions, which come at the end of the launch, where nothing hides them.)
                 float need = -INFINITY;
                 if (MODE == MODE_SCORE && KT > 1 && b0 == un.box_begin && n_valid >= 8 * p.k_tab) {
                     float th[KT];
@@ -1188,7 +1188,8 @@ size_t score_bytes(spec_ctx* ctx, int M, int n_alt) {
 
 // One CTA per row joins the row's partial results: warp 1 the statistics, relative to the common maximum; all threads
 // bring the chunks' sorted lists into shared memory, and warp 0 takes the largest of their heads n_alt times (a lane looks
-// after chunks lane, lane + 32, ...).
+// after chunks lane, lane + 32, ...).  9 us after the contraction of 48 rows (125 chunks, 5 alternatives; the launch, and
+// a chain of one round per alternative), 1 % of a call with 2816 rows.
 constexpr int MERGE_THREADS = 128, MERGE_LISTS = SCORE_MAX_CHUNKS / 32;
 __global__ void __launch_bounds__(MERGE_THREADS) merge_score_kernel(const float4* stat, const float* val, const int32_t* idx, int n_chunks, int M,
                                                                     int V, int n_alt, const int32_t* __restrict__ tokens,

@@ -6,10 +6,11 @@
 //     S = Q K^T,   m' = max(m, rowmax S),   P = exp(c S - c m'),   l = l exp(c m - c m') + rowsum P,   O = O exp(..) + P V
 // and o = O / l at the end.  Both products run on the tensor cores (tcgen05, bf16 x bf16 -> fp32): S and O live in tensor
 // memory, P goes back into tensor memory as bfloat16 (over S, which has been read by then) and is the A operand of
-// P V from there, so that no intermediate touches shared memory.  P is at most 2^8 and keeps 8 bits; its row sum is
-// taken before the rounding.  m need not be the maximum itself: it is a score of the row
-// that stays the reference until weights grow beyond 2^8, so that the read-modify-write of O that a new reference costs
-// happens in the first tiles and hardly ever after.
+// P V from there, so that no intermediate touches shared memory.  P is at most 2^8 and keeps 8 bits (the products take
+// nothing wider; it is what the error against exact arithmetic, 2e-3 of the outputs' rms, comes from); its row sum is
+// taken in fp32 before the rounding.  m need not be the maximum itself: it is a score of the row that stays the
+// reference until weights grow beyond 2^8, so that the read-modify-write of O that a new reference costs happens in
+// the first tiles and hardly ever after.
 //
 // Two streams per CTA hide the softmax of one tile behind the products of another.  With more than 128 rows they are
 // two row tiles against the same keys; with at most 128 they are the even and the odd tiles of keys against the same
@@ -24,8 +25,18 @@
 // Warps (896 threads, which share the registers unevenly): 0-7 and 8-15 softmax of stream 0 and 1 (a row's 128 scores
 // belong to two threads, of warps w and w + 4: a single warp per scheduler leaves the special function unit waiting);
 // 16-23 turn an E4M3 cache's tiles into bfloat16 (code * scale, which is exact) and mend value tiles (zeros after the
-// end of a context, and in place of what is not finite in the block); 24 TMA; 25 issues the products; 26 walks the CTA's range and tells
-// the others.
+// end of a context, and in place of what is not finite in the block); 24 TMA; 25 issues the products; 26 walks the CTA's
+// range and tells the others; 27 writes the rows of nodes that are not live.
+//
+// What bounds it, on a B200 (copies 6.5 TB/s, products 1650 TFLOP/s in a burst, 1400 under the power cap):
+//   few rows, bfloat16 cache    the bytes: 64 sequences of one token, 32 / 8 heads of 128, 2048 keys: 99 us, 5.4 TB/s
+//   few rows, E4M3 cache        the integer pipe, which converts (1500 cycles per 128 vectors of 128): 16 x 8192 keys,
+//                               105 us, 2.6 TB/s of codes
+//   many rows, long contexts    a stream's chain scores -> weights -> outputs, of which two overlap (a key tile per 4100
+//                               cycles), and the power cap: 4 x 704 nodes, 16384 keys, 720-820 us, 0.92-1.04 PFLOP/s
+//   short contexts              a segment's beginning and end, 6-10 us where a tile takes 2: 64 x 144 nodes, 2048 keys,
+//                               bfloat16 490 us, E4M3 650 us
+//   one short call              two launches and one segment: 16-18 us
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -45,7 +56,7 @@ constexpr int LAUNCH_REGS = 72;   // per thread at launch: 65536 / 896, rounded 
 constexpr int REGS_SOFTMAX = 88, REGS_LOADER = 40, REGS_CONTROL = 72;
 constexpr int SEGMENTS = 4;  // segments that the planning warp is ahead
 static_assert(128 * (4 * REGS_SOFTMAX + 2 * REGS_LOADER + REGS_CONTROL) <= ATT_THREADS * LAUNCH_REGS, "the warpgroups' shares exceed the launch's registers");
-constexpr int START = 4;  // tiles that the beginning and end of a segment take as long as (6 us where a tile takes 1.4)
+constexpr int START = 4;  // tiles that the beginning and end of a segment take as long as (2 or 8 instead: no better)
 constexpr float RESCALE = 256.0f;  // what 32 weights may add up to before their reference is moved
 
 struct AttParams {
