@@ -36,7 +36,7 @@
 //                               cycles), and the power cap: 4 x 704 nodes, 16384 keys, 720-820 us, 0.92-1.04 PFLOP/s
 //   short contexts              a segment's beginning and end, 6-10 us where a tile takes 2: 64 x 144 nodes, 2048 keys,
 //                               bfloat16 490 us, E4M3 650 us
-//   one short call              two launches and one segment: 16-18 us
+//   one short call              two launches and a segment: 10-15 us
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -985,18 +985,24 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     if (warp == MMA_WARP) tmem_dealloc(tmem, 512);
 }
 
-// Joins the partial rows of every (s, h, row-tile pair) whose key tiles were spread over several CTAs, in the CTAs'
-// order.  A lane per row, 16 columns per warp.
+// Joins the partial rows of every (s, h, row-tile pair) whose key tiles were spread over several CTAs, in an order that
+// only their number decides.  16 columns per warp; a lane per row, and with 16 rows or fewer several lanes per row, which
+// share the parts (one token of 32 heads, 4095 keys: 18 parts for each of 8 key heads; the call 17.4 -> 14.3 us).  It is
+// a chain of memory latencies (the record, a round of parts, the output): the loads of 4 parts are in flight (8: fewer
+// warps to an SM, slower).
+constexpr int JOIN_DEPTH = 4;
 template <int D>
 __global__ void __launch_bounds__(2 * D) join_kernel(const __grid_constant__ AttParams p) {
     const TreeAttnArgs& a = p.a;
     const int lane = threadIdx.x & 31, cols = threadIdx.x >> 5;  // columns [16 cols, 16 cols + 16)
     grid_launch_dependents();
     grid_dependency_wait();
-    const int cta = p.side + blockIdx.x, r = blockIdx.y * 32 + lane;
+    const int cta = p.side + blockIdx.x, r0 = blockIdx.y * 32;
     const JoinTask task = p.tasks[cta];
-    const int n = task.n;
-    if (n == 0 || r >= task.rows) return;
+    const int n = task.n, rows = min(task.rows - r0, 32);
+    if (n == 0 || rows <= 0) return;
+    const int bits = rows > 16 ? 5 : (rows > 8 ? 4 : (rows > 4 ? 3 : 2)), lanes = 1 << bits, sharers = 32 >> bits;  // lanes: for distinct rows
+    const int r = r0 + min(lane & (lanes - 1), rows - 1), mine = lane >> bits;
     const int R = task.qt * 2 * TILE + r, node = R / p.G, gq = R - node * p.G;
     const long long out_row = ((long long)task.s * a.N + node) * a.Hq + task.h * p.G + gq;
     uint4* out = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + out_row * D + 16 * cols);
@@ -1005,20 +1011,20 @@ __global__ void __launch_bounds__(2 * D) join_kernel(const __grid_constant__ Att
     float m = -INFINITY, l = 0.0f, x[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) x[j] = 0.0f;
-    for (int i0 = 0; i0 < n; i0 += 4) {  // four parts' loads in flight
-        float2 ml[4];
-        float4 o[4][4];
+    for (int i0 = mine; i0 < n; i0 += JOIN_DEPTH * sharers) {
+        float2 ml[JOIN_DEPTH];
+        float4 o[JOIN_DEPTH][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i0 + i >= n) continue;
-            const long long at = part(i0 + i);
+        for (int i = 0; i < JOIN_DEPTH; ++i) {
+            if (i0 + i * sharers >= n) continue;
+            const long long at = part(i0 + i * sharers);
             ml[i] = p.part_ml[at * p.rows_cap + r];
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[i][j] = reinterpret_cast<const float4*>(p.part_o)[(at * (D / 4) + 4 * cols + j) * p.rows_cap + r];
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i0 + i >= n) continue;
+        for (int i = 0; i < JOIN_DEPTH; ++i) {
+            if (i0 + i * sharers >= n) continue;
             const float top = fmaxf(m, ml[i].x), f0 = m == -INFINITY ? 0.0f : exp2f((m - top) * p.c), f = ml[i].x == -INFINITY ? 0.0f : exp2f((ml[i].x - top) * p.c);
             m = top;
             l = l * f0 + ml[i].y * f;
@@ -1031,6 +1037,16 @@ __global__ void __launch_bounds__(2 * D) join_kernel(const __grid_constant__ Att
             }
         }
     }
+    __syncwarp();
+    for (int d = lanes; d < 32; d <<= 1) {
+        const float m1 = __shfl_xor_sync(0xffffffffu, m, d), top = fmaxf(m, m1);
+        const float f0 = m == -INFINITY ? 0.0f : exp2f((m - top) * p.c), f1 = m1 == -INFINITY ? 0.0f : exp2f((m1 - top) * p.c);
+        m = top;
+        l = l * f0 + __shfl_xor_sync(0xffffffffu, l, d) * f1;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] = x[j] * f0 + __shfl_xor_sync(0xffffffffu, x[j], d) * f1;
+    }
+    if (lane >= rows) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
