@@ -33,9 +33,9 @@
 //   few rows, E4M3 cache        the integer pipe, which converts (1500 cycles per 128 vectors of 128): 16 x 8192 keys,
 //                               105 us, 2.6 TB/s of codes
 //   many rows, long contexts    a stream's chain scores -> weights -> outputs, of which two overlap (a key tile per 4100
-//                               cycles), and the power cap: 4 x 704 nodes, 16384 keys, 720-820 us, 0.92-1.04 PFLOP/s
+//                               cycles), and the power cap: 4 x 704 nodes, 16384 keys, 700-820 us, 0.92-1.07 PFLOP/s
 //   short contexts              a segment's beginning and end, 6-10 us where a tile takes 2: 64 x 144 nodes, 2048 keys,
-//                               bfloat16 490 us, E4M3 650 us
+//                               bfloat16 470 us, E4M3 560 us
 //   one short call              two launches and a segment: 10-15 us
 #include <cuda_bf16.h>
 #include <math.h>
@@ -77,6 +77,7 @@ struct Segment {
     int split;  // the streams take the even and the odd key tiles; else a row tile each
     int slot;   // partial result: 0 = the CTA's range starts here, 1 = it ends here
     int more;   // 0: there was none left
+    int first;  // tile t >= n_prefix is the block's tile t - first
 };
 // An (s, h) and row-tile pair that several CTAs walked: its partial rows are joined.  Recorded by the second of them.
 struct __align__(16) JoinTask {
@@ -162,7 +163,7 @@ __device__ __forceinline__ void advance(const AttParams& p, Walk& w, Segment& g)
                 g.s = w.s;
                 g.h = w.h;
                 g.qt = qt;
-                g.n_prefix = n_prefix;
+                g.n_prefix = g.first = n_prefix;
                 g.len = len;
                 g.live = live;
                 g.whole = g.t1 - g.t0 == n_tiles;
@@ -189,6 +190,34 @@ __device__ __forceinline__ void advance(const AttParams& p, Walk& w, Segment& g)
     }
     g.rows = rows;
     g.more = rows > 0;
+}
+
+// Tiles of the block that the rows of a segment attend to, by a warp: the bits of their nodes lie one after another.
+// Rows of drafts attend to their own few nodes, so that of a wide block's tiles most are empty for most rows.  Beyond
+// MASK_WORDS looking would take longer than a tile or two, and all tiles count as attended to.  A segment takes those
+// from the first to the last of them (8-bit cache: 64 sequences of 144 nodes in rows of 9, 2048 keys: 644 -> 561 us; one
+// of 666 nodes, 14 / 2 heads of 64, 873 keys: 40 -> 30 us; one token: 14.4 -> 14.8 us).
+constexpr int MASK_WORDS = 8192;
+__device__ __forceinline__ uint32_t block_tiles(const AttParams& p, const Segment& g, int lane) {
+    const int W = (p.a.N + 31) / 32, n0 = g.qt * 2 * TILE / p.G, n1 = (g.qt * 2 * TILE + g.rows - 1) / p.G + 1, words = (n1 - n0) * W;
+    if (words > MASK_WORDS) return 0xFFFFFFFFu;
+    const int32_t* bits = p.a.mask + ((long long)g.s * p.a.N + n0) * W;
+    const int turn = 32 % W;
+    uint32_t tiles = 0;
+    int w = lane % W;  // the word's place in its node's mask
+#pragma unroll 1
+    for (int i0 = lane; i0 < words; i0 += 32 * 16) {
+        int32_t x[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] = i0 + 32 * j < words ? bits[i0 + 32 * j] : 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            if (x[j]) tiles |= 1u << (w >> 2);
+            w += turn;
+            if (w >= W) w -= W;
+        }
+    }
+    return __reduce_or_sync(0xffffffffu, tiles);
 }
 
 // Calls f(is_v, tile) for the key and value tiles of a segment in the order in which the products consume them;
@@ -403,7 +432,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 __syncwarp();
                 tc_fence_after();
                 if (warp_on) {
-                    const int valid_keys = t < g.n_prefix ? g.len - t * TILE : g.live - (t - g.n_prefix) * TILE;
+                    const int valid_keys = t < g.n_prefix ? g.len - t * TILE : g.live - (t - g.first) * TILE;
                     const bool masked = t >= g.n_prefix || valid_keys < TILE;
                     auto load = [&](int i, uint32_t(&x)[32]) {  // scores [32 i, 32 i + 32) of the row, -inf where it has none
                         tmem_ld32(s_tm + 32 * i, x);
@@ -412,7 +441,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                             const int left = valid_keys - 32 * i;
                             uint32_t seen = left >= 32 ? 0xFFFFFFFFu : (left <= 0 ? 0u : (1u << left) - 1u);
                             if (t >= g.n_prefix) {
-                                const int words = (a.N + 31) / 32, at = (t - g.n_prefix) * 4 + i, node = (g.qt * 2 * TILE + tile_row) / p.G;
+                                const int words = (a.N + 31) / 32, at = (t - g.first) * 4 + i, node = (g.qt * 2 * TILE + tile_row) / p.G;
                                 seen &= (valid && at < words) ? (uint32_t)a.mask[((long long)g.s * a.N + node) * words + at] : 0u;
                             }
                             hide(x, seen);
@@ -533,7 +562,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                         // values of the block that are not finite were taken as 0 in the products, where a weight of 0
                         // would have made them NaN; rows that do attend to them get them here
                         const int words = (a.N + 31) / 32;
-                        const int from = max(g.t0 - g.n_prefix, 0) * TILE, to = min((g.t1 - g.n_prefix) * TILE, g.live);
+                        const int from = (max(g.t0, g.n_prefix) - g.first) * TILE, to = min((g.t1 - g.first) * TILE, g.live);
                         for (int n = from; n < to; ++n) {
                             if (!((a.mask[((long long)g.s * a.N + node) * words + (n >> 5)] >> (n & 31)) & 1)) continue;
                             const __nv_bfloat16* v = (const __nv_bfloat16*)a.v + ((long long)g.s * a.N + n) * a.v_tok + (long long)g.h * a.v_head + 32 * i;
@@ -599,7 +628,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     slot = 0;
                     phase ^= 1u;
                 }
-                const int rows = block ? g.live - (t - g.n_prefix) * TILE : g.len - t * TILE;  // may exceed the tile
+                const int rows = block ? g.live - (t - g.first) * TILE : g.len - t * TILE;  // may exceed the tile
                 if (!Q8 && !(is_v && (block || rows < TILE))) return true;  // all TMA's
                 if (Q8 && !block) {
                     if (!wait(stg_full + 8 * stg, stg_phase)) return false;
@@ -681,7 +710,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                             const int r = i * (LOADERS / CH) + tid / CH, c = tid % CH;
                             v[i] = make_uint4(0, 0, 0, 0);
                             if (r >= rows) continue;
-                            const long long tok = (long long)g.s * a.N + (t - g.n_prefix) * TILE + r;
+                            const long long tok = (long long)g.s * a.N + (t - g.first) * TILE + r;
                             const __nv_bfloat16* src = is_v ? (const __nv_bfloat16*)a.v + tok * a.v_tok + (long long)g.h * a.v_head
                                                             : (const __nv_bfloat16*)a.k + tok * a.k_tok + (long long)g.h * a.k_head;
                             v[i] = *reinterpret_cast<const uint4*>(src + c * 8);
@@ -761,7 +790,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     }
                     __syncwarp();
                     if (block) {
-                        if (lane < Geo::HALVES) tma_load_3d(dst + lane * (TILE * 128), is_v ? &tm_bv : &tm_bk, 64 * lane, g.h, g.s * a.N + (t - g.n_prefix) * TILE, bar);
+                        if (lane < Geo::HALVES) tma_load_3d(dst + lane * (TILE * 128), is_v ? &tm_bv : &tm_bk, 64 * lane, g.h, g.s * a.N + (t - g.first) * TILE, bar);
                     } else if (lane < pages) {
                         const bool good = (unsigned)pid < (unsigned)cache.n_pages;
                         if (!good) atomicOr(a.status, SPEC_STATUS_CAPACITY);
@@ -934,18 +963,39 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             w.s = __shfl_sync(0xffffffffu, w.s, src);
             w.h = __shfl_sync(0xffffffffu, w.h, src);
             w.t = __shfl_sync(0xffffffffu, w.t, src);
-            if (lane == 0) {
-                const int s = w.s, h = w.h, t = w.t;
-                const long long u0 = w.pos - t;  // the first place of the (s, h)
-                const bool inside = w.pos < w.hi && t > START;  // an (s, h) has tiles before this range
-                for (uint32_t k = 0;; ++k) {
-                    if (!wait(seg_empty + 8 * (k % SEGMENTS), ((k / SEGMENTS) & 1u) ^ 1u)) break;
-                    Segment& g = sh.segment[k % SEGMENTS];
-                    advance<Q8>(p, w, g);
-                    const int more = g.more;
-                    mbar_arrive(seg_full + 8 * (k % SEGMENTS));
-                    if (!more) break;
+            const int s = w.s, h = w.h, t = w.t;
+            const long long u0 = w.pos - t;  // the first place of the (s, h)
+            const bool inside = w.pos < w.hi && t > START;  // an (s, h) has tiles before this range
+            int known_s = -1, known_qt = -1;
+            uint32_t known = 0;  // tiles of the block that some node of the known rows attends to
+            for (uint32_t k = 0;; ++k) {
+                if (!__all_sync(0xffffffffu, wait(seg_empty + 8 * (k % SEGMENTS), ((k / SEGMENTS) & 1u) ^ 1u))) break;
+                Segment& g = sh.segment[k % SEGMENTS];
+                if (lane == 0) advance<Q8>(p, w, g);
+                __syncwarp();
+                const int n_pre = g.n_prefix, from = max(g.t0 - n_pre, 0), to = g.t1 - n_pre;
+                if (g.more && to > 0) {
+                    if (a.N > TILE && (g.s != known_s || g.qt != known_qt)) {  // (consecutive key heads see the same bits)
+                        known_s = g.s;
+                        known_qt = g.qt;
+                        known = block_tiles(p, g, lane);
+                    }
+                    uint32_t live_tiles = (a.N > TILE ? known : 1u) & (0xFFFFFFFFu << from);
+                    if (to < 32) live_tiles &= (1u << to) - 1u;
+                    if (live_tiles == 0 && g.t0 >= n_pre) live_tiles = 1u << from;  // one tile there has to be
+                    __syncwarp();
+                    if (lane == 0) {  // from the first to the last of them
+                        const int first = live_tiles ? __ffs(live_tiles) - 1 : from;
+                        g.first = n_pre + from - first;
+                        g.t1 = max(g.t0, n_pre) + (live_tiles ? 32 - __clz(live_tiles) - first : 0);
+                    }
                 }
+                const int more = g.more;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(seg_full + 8 * (k % SEGMENTS));
+                if (!more) break;
+            }
+            if (lane == 0) {
                 JoinTask task = {s, h, first_pass * p.side + (int)(blockIdx.x % p.side), 0, 0, 0, {0, 0}};
                 if (inside && u0 + START >= ranges.begin(group - 1) && task.qt < p.n_qtiles) {
                     const int n = places(sequence_tiles(a, s, len, live, np));

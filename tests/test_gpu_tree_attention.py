@@ -123,6 +123,13 @@ def test_live_nodes_over_row_tiles(ctx, quantised):
     run(ctx, 6, 150, 4, 2, 128, [300, 40, 1000, 257, 0, 129], 64, quantised, live=[150, 129, 128, 65, 64, 3], seed=6)
 
 
+@pytest.mark.parametrize("quantised", [False, True])
+@pytest.mark.parametrize("N,Hq,length", [(415, 7, 0), (415, 7, 300), (700, 4, 1), (520, 1, 129), (1100, 1, 64)])
+def test_wide_blocks_of_rows(ctx, quantised, N, Hq, length):
+    """Blocks of many tiles of which a row attends to one or two, from the front, the middle or the end."""
+    run(ctx, 2, N, Hq, 1, 64, [length, length + 200], 32, quantised, kind="rows", seed=N, live=[N, N - 130])
+
+
 def test_scale_argument(ctx):
     run(ctx, 1, 8, 2, 1, 64, [300], 16, False, scale=0.02)
 
