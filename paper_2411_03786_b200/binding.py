@@ -80,6 +80,7 @@ def load_library(build: bool = True) -> C.CDLL:
     lib.build_model_ngram_table_rows.argtypes = [vp, vp, C.c_int, C.c_int, C.c_int, i32p, fp, vp]
     lib.spec_extend_model_table.argtypes = [vp, i32p, C.c_int, C.c_int, i32p, vp]
     lib.spec_debug_expire_wait.argtypes = [vp, C.c_ulonglong, C.c_int, vp]
+    lib.spec_debug_wait_limit.argtypes = [vp, C.c_ulonglong]
     lib.spec_context_index_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
     lib.spec_context_index_bytes.restype = C.c_size_t
     lib.spec_context_index_build.argtypes = [vp, vp, i32p, i32p, C.c_int, C.c_int, ip, C.c_int, C.c_int, C.c_int, vp]
@@ -269,6 +270,9 @@ class SpecContext:
     def debug_expire_wait(self, limit_ns: int = 20000, mark_verify_incomplete: bool = False):
         self._check(self._lib.spec_debug_expire_wait(self._h, int(limit_ns), int(mark_verify_incomplete), _stream()),
                     "spec_debug_expire_wait")
+
+    def debug_wait_limit(self, limit_ns: int = 2_000_000_000):
+        self._check(self._lib.spec_debug_wait_limit(self._h, int(limit_ns)), "spec_debug_wait_limit")
 
     def build_model_unigram(self, k_uni: int):
         """Returns ``(ids[k_uni] by ascending distance, dist2[V])``."""

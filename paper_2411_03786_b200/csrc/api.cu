@@ -477,6 +477,13 @@ int spec_debug_expire_wait(spec_ctx* ctx, unsigned long long limit_ns, int mark_
     return launch_wait_probe(ctx, limit_ns, mark_verify_incomplete ? 1 : 0, (cudaStream_t)stream);
 }
 
+int spec_debug_wait_limit(spec_ctx* ctx, unsigned long long limit_ns) {
+    if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "spec_debug_wait_limit: ctx is NULL");
+    if (limit_ns > WAIT_LIMIT_NS) return fail(ctx, SPEC_ERR_ARG, "spec_debug_wait_limit: the limit may not exceed two seconds");
+    ctx->wait_limit_ns = limit_ns;
+    return SPEC_OK;
+}
+
 size_t spec_score_bytes(spec_ctx* ctx, int M, int n_alt) {
     if (!ctx || M < 1 || M > SPEC_MAX_VERIFY_ROWS || n_alt < 0 || n_alt > kMaxKTab || n_alt > ctx->V) return 0;
     return score_bytes(ctx, M, n_alt);

@@ -17,6 +17,7 @@ constexpr int kMaxW = 16;
 constexpr int kMaxQ = 4;
 constexpr int kMaxNQ = 4;
 constexpr int kMaxKTab = 32;
+constexpr unsigned long long WAIT_LIMIT_NS = 2000000000ull;  // default limit of every device-side wait
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
@@ -80,6 +81,7 @@ struct spec_ctx {
     } index;
     void* d_centred = nullptr;  // unigram scratch: bf16 [V, d] output embeddings minus their mean
     float* d_colsum = nullptr;  // unigram scratch: [64 + 1, d] partial column sums and the mean
+    unsigned long long wait_limit_ns = ngs::WAIT_LIMIT_NS;  // 0: kernels start as if a wait had expired (test aid)
     long long launches = 0;
     char err[256] = {0};
 };

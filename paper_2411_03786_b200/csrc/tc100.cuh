@@ -6,7 +6,6 @@
 namespace ngs {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr unsigned long long WAIT_LIMIT_NS = 2000000000ull;  // default limit of every device-side wait
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -57,6 +56,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
             }
         }
     }
+}
+// Copies and products that a CTA which gives up has in flight write to its memory and barriers: every thread gives them a
+// bounded chance to land (they take microseconds) before its shared and tensor memory go to the next CTA.
+__device__ __forceinline__ void let_copies_land() {
+    const unsigned long long until = global_timer_ns() + 1000000ull;
+    while (global_timer_ns() < until) {}
 }
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* tm, int x, int y, uint32_t bar) {

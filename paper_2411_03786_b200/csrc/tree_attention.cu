@@ -348,10 +348,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         mbar_init(smem_u32(&sh.xch), SOFTMAX_WARPS / 2);
         for (int i = 0; i < SEGMENTS; ++i) {
             mbar_init(smem_u32(&sh.seg_full[i]), 1);
-            mbar_init(smem_u32(&sh.seg_empty[i]), SOFTMAX_WARPS + LOADER_WARPS + 2);
+            mbar_init(smem_u32(&sh.seg_empty[i]), SOFTMAX_WARPS + LOADERS + 2);
         }
         for (int i = 0; i < 16; ++i) sh.nonfinite[i] = 0;
-        sh.abort_flag = 0;
+        sh.abort_flag = p.wait_limit_ns == 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == MMA_WARP) {
@@ -377,7 +377,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     uint32_t n_seg = 0;  // segments that this warp has been through
     auto segment = [&]() -> const Segment& { return sh.segment[n_seg % SEGMENTS]; };
     auto segment_there = [&]() { return wait(seg_full + 8 * (n_seg % SEGMENTS), (n_seg / SEGMENTS) & 1u); };
-    auto segment_done = [&]() {  // by one lane, after the warp's last look at it
+    auto segment_done = [&]() {  // after the last look at it: by one lane for its warp, or by each of the loaders
         mbar_arrive(seg_empty + 8 * (n_seg % SEGMENTS));
     };
 
@@ -611,6 +611,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         }
     } else if (warp < SOFTMAX_WARPS + LOADER_WARPS) {
         // ------------------------------------------------------------------------------------ tiles written by threads
+        // (A wait that has expired is noticed by a warp's lanes at different times.  The other roles vote; here a lane leaves
+        // by itself, so that nothing between this and the end of the role may wait for the warp's other lanes: they would be
+        // waited for without a limit.  A vote at every wait: one token of 64 sequences over 2048 keys 103 -> 111 us.)
         set_regs_down<REGS_LOADER>();
         const int tid = threadIdx.x - 32 * SOFTMAX_WARPS;
         constexpr int CH = D / 8;  // 16-byte chunks of a bf16 vector
@@ -735,8 +738,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 return true;
             });
             if (!ok) break;
-            __syncwarp();
-            if (lane == 0) segment_done();
+            segment_done();
         }
     } else {
         set_regs_down<REGS_CONTROL>();
@@ -744,22 +746,21 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             // -------------------------------------------------------------------------------- TMA
             // A lane fetches one page's part of a tile.  Page numbers are read 32 at a time, a window ahead of their use (two
             // registers, by the window's parity: a load is never waited for where it is issued).
-            uint32_t slot = 0, phase = 0, issued = 0;
+            uint32_t slot = 0, phase = 0;
             constexpr uint32_t RING = Q8 ? Geo::STAGES : Geo::SLOTS;
             const int page = 1 << cache.page_shift, per_tile = TILE >> cache.page_shift;
             const int all_rows = (cache.n_pages * cache.heads) << cache.page_shift;  // a coordinate beyond the cache: reads as 0
-            bool ok = true;
             for (;; ++n_seg) {
-                ok = __all_sync(0xffffffffu, segment_there());
+                if (!__all_sync(0xffffffffu, segment_there())) break;
                 const Segment g = segment();
-                if (!ok || !g.more) break;
+                if (!g.more) break;
                 const int32_t* table = cache.table + (long long)g.s * cache.max_pages;
                 const int n_pages = (g.len + page - 1) >> cache.page_shift;
                 const int wsh = cache.page_shift - 2, in_window = (1 << wsh) - 1;  // tiles of a window: 4 to 32
                 auto fetch = [&](int window) { return window * 32 + lane < n_pages ? table[window * 32 + lane] : 0; };
                 const int w0 = g.t0 >> wsh;
                 int even = fetch(w0 + (w0 & 1)), odd = fetch(w0 + 1 - (w0 & 1));
-                ok = for_each_tile(g, [&](bool is_v, int t) {
+                const bool ok = for_each_tile(g, [&](bool is_v, int t) {
                     const bool block = t >= g.n_prefix;
                     const int rows = block ? TILE : min(g.len - t * TILE, TILE);
                     const bool mended = !Q8 && is_v && (block || rows < TILE);  // goes through the other threads' hands
@@ -804,16 +805,11 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                             for (int i = 0; i < Geo::HALVES; ++i) tma_load_2d(dst + i * (TILE * 128) + lane * page * 128, tm, 64 * i, row, bar);
                         }
                     }
-                    ++issued;
                     return true;
                 });
                 if (!ok) break;
                 __syncwarp();
                 if (lane == 0) segment_done();
-            }
-            if (!ok && lane == 0) {  // give copies in flight a bounded chance to land before the CTA exits
-                const uint64_t until = global_timer_ns() + 1000000ull;
-                while (issued && global_timer_ns() < until) {}
             }
         } else if (warp == MMA_WARP && lane == 0) {
             // -------------------------------------------------------------------------------- products
@@ -1031,7 +1027,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     }
     tc_fence_before();
     __syncthreads();
-    if (threadIdx.x == 0 && *abort_flag) atomicOr(a.status, SPEC_STATUS_TIMEOUT);
+    if (*abort_flag) {
+        if (threadIdx.x == 0) atomicOr(a.status, SPEC_STATUS_TIMEOUT);
+        let_copies_land();
+    }
     if (warp == MMA_WARP) tmem_dealloc(tmem, 512);
 }
 
@@ -1199,7 +1198,7 @@ int launch_tree_attention(spec_ctx* ctx, const TreeAttnArgs& a, cudaStream_t st)
     p.tasks = reinterpret_cast<JoinTask*>(a.work);
     p.part_o = reinterpret_cast<float*>((char*)a.work + (size_t)p.part_o);
     p.part_ml = reinterpret_cast<float2*>((char*)a.work + (size_t)p.part_ml);
-    p.wait_limit_ns = WAIT_LIMIT_NS;
+    p.wait_limit_ns = ctx->wait_limit_ns;
     if (a.cache.quantised) return a.cache.head_dim == 64 ? launch<64, true>(ctx, p, st) : launch<128, true>(ctx, p, st);
     return a.cache.head_dim == 64 ? launch<64, false>(ctx, p, st) : launch<128, false>(ctx, p, st);
 }
