@@ -441,9 +441,9 @@ int verify_lmhead_argmax_noalloc(const void* d_unembed, int V, int d, const void
 int spec_debug_expire_wait(spec_ctx* ctx, unsigned long long limit_ns, int mark_verify_incomplete, void* stream);
 
 /*
- * Test aid: limit of the device-side waits of later spec_tree_attention calls on this context, at most the two seconds that
- * a context starts with.  0: their CTAs start as if a wait had expired and give up at the first thing that is not there yet;
- * the call returns, sets SPEC_STATUS_TIMEOUT, and its outputs mean nothing.
+ * Test aid: limit of the device-side waits of later calls on this context, at most the two seconds that a context starts
+ * with.  0: CTAs start as if a wait had expired and give up at the first thing that is not there yet; the call returns and
+ * sets SPEC_STATUS_TIMEOUT, a verification reports -1 for every row, and other outputs mean nothing.
  */
 int spec_debug_wait_limit(spec_ctx* ctx, unsigned long long limit_ns);
 

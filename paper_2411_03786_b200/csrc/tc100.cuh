@@ -45,6 +45,7 @@ __device__ __forceinline__ unsigned long long global_timer_ns() {
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
                                           unsigned long long limit_ns) {
     if (mbar_try_wait(bar, parity)) return true;
+    if (*abort_flag) return false;
     const unsigned long long t0 = global_timer_ns();
     for (uint32_t it = 1;; ++it) {
         if (mbar_try_wait(bar, parity)) return true;

@@ -44,3 +44,30 @@ def test_the_limit_is_checked():
     with pytest.raises(ngs.SpecError):
         ctx.debug_wait_limit(2_000_000_001)
     ctx.close()
+
+
+@pytest.mark.parametrize("V,d,M", [(5003, 256, 7), (1000, 1000, 300), (32000, 512, 129)])
+def test_head_calls_give_up_together(V, d, M):
+    import paper_2411_03786_b200 as ngs
+    g = torch.Generator().manual_seed(V)
+    w = (torch.randn(V, d, generator=g) / 32).bfloat16().cuda()
+    h = torch.randn(M, d, generator=g).bfloat16().cuda()
+    tok = torch.randint(0, V, (M,), generator=g).int().cuda()
+    ctx = ngs.SpecContext(w, w)
+    calls = [lambda n=n: ctx.score_tokens(h, tok, n_alt=n) for n in (0, 5, 20)] + [lambda: ctx.verify_lmhead_argmax(h, with_max=True)]
+    want = [f() for f in calls]
+    assert ctx.get_status() == 0
+    for limit in (0, 1):
+        ctx.debug_wait_limit(limit)
+        for f in calls:
+            for _ in range(5):
+                out = f()
+            bits = ctx.get_status()
+            assert bits == ngs.STATUS_TIMEOUT if limit == 0 else bits in (0, ngs.STATUS_TIMEOUT)
+        if limit == 0:
+            assert (out[0] == -1).all()  # an incomplete verification does not pass for a result
+    ctx.debug_wait_limit()
+    for f, a in zip(calls, want):
+        assert all(x is None and y is None or torch.equal(x, y) for x, y in zip(f(), a))
+    assert ctx.get_status() == 0
+    ctx.close()
