@@ -89,10 +89,22 @@ struct __align__(16) JoinTask {
 struct AttShared {
     uint64_t full[8], empty[8], go[8], stg_full[6], stg_empty[6], s_full[2], p_full[2], o_full, q_full, xch, seg_full[SEGMENTS], seg_empty[SEGMENTS];
     Segment segment[SEGMENTS];
-    int nonfinite[16];
+    int nonfinite[16], bad_pages[16];  // by segment: its number + 1 if a value of the block is not finite, a page is not one of the pool's
     uint32_t tmem;
     int abort_flag;
 };
+
+// What is read in place of a page that is not there: its keys as NaN (and the scales of its keys, 255), the scales of its
+// values as 1.
+template <int N, int BYTE>
+struct __align__(16) Filled {
+    uint8_t byte[N];
+    constexpr Filled() : byte() {
+        for (int i = 0; i < N; ++i) byte[i] = BYTE;
+    }
+};
+__device__ const Filled<TILE * 128, 255> nan_page;
+__device__ const Filled<TILE, 127> unit_scales;
 
 template <int D, bool Q8>
 struct Geometry {
@@ -298,6 +310,15 @@ __device__ __forceinline__ void hide(uint32_t (&s)[32], uint32_t seen) {  // sco
         if (!((seen >> j) & 1u)) s[j] = 0xFF800000u;
 }
 
+// Positions [at, at + 32) of sequence s that lie in pages of the pool, as bits; `at` is one of the sequence's positions.
+__device__ __forceinline__ uint32_t paged(const CacheArgs& c, int s, int at, int len) {
+    const int32_t* table = c.table + (long long)s * c.max_pages + (at >> c.page_shift);
+    auto bits = [&](int page) { return (unsigned)page < (unsigned)c.n_pages ? 0xFFFFFFFFu : 0u; };
+    const uint32_t first = bits(table[0]);
+    if (c.page_shift > 4) return first;
+    return (first & 0xFFFFu) | (at + 16 < len ? bits(table[1]) << 16 : 0u);
+}
+
 __device__ __forceinline__ uint32_t nonfinite_to_zero(uint32_t v, bool& found) {
     if ((v & 0x7F80u) == 0x7F80u) {
         v &= 0xFFFF0000u;
@@ -350,7 +371,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             mbar_init(smem_u32(&sh.seg_full[i]), 1);
             mbar_init(smem_u32(&sh.seg_empty[i]), SOFTMAX_WARPS + LOADERS + 2);
         }
-        for (int i = 0; i < 16; ++i) sh.nonfinite[i] = 0;
+        for (int i = 0; i < 16; ++i) sh.nonfinite[i] = sh.bad_pages[i] = 0;
         sh.abort_flag = p.wait_limit_ns == 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -451,6 +472,21 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
 #pragma unroll 1
                     for (;;) {
                         if (look) {
+                            if (t < g.n_prefix && __any_sync(0xffffffffu, sh.bad_pages[n_seg & 15u] == (int)n_seg + 1)) {
+                                // keys of missing pages: their NaN (which a maximum passes over) become -inf in this warp's half
+#pragma unroll 1
+                                for (int i = 2 * half; i < 2 * half + 2; ++i) {
+                                    const int at = t * TILE + 32 * i;
+                                    if (at >= g.len) break;
+                                    uint32_t x[32], (&lo)[16] = *reinterpret_cast<uint32_t(*)[16]>(&x[0]), (&hi)[16] = *reinterpret_cast<uint32_t(*)[16]>(&x[16]);
+                                    tmem_ld32(s_tm + 32 * i, x);
+                                    tmem_wait_ld();
+                                    hide(x, paged(cache, g.s, at, g.len));
+                                    tmem_st16(s_tm + 32 * i, lo);
+                                    tmem_st16(s_tm + 32 * i + 16, hi);
+                                    tmem_wait_st();
+                                }
+                            }
                             float top = -INFINITY;
 #pragma unroll 1
                             for (int i = 0; i < 4; ++i) {
@@ -776,9 +812,19 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                         else odd = fetch(window + 1);
                     }
                     if (Q8 && block) return true;
+                    const int pages = block ? 0 : (rows + page - 1) >> cache.page_shift;
+                    // A page that is not one of the pool's: its keys are made NaN, so that no weights come of the tile before
+                    // the softmax warps have looked for its maximum, which is when they hide the positions of missing pages
+                    // (masks in every tile instead, for the case that there are any: 64 x 144 nodes, E4M3: 563 -> 573 us); its values
+                    // are 0.
+                    const bool good = lane >= pages || (unsigned)pid < (unsigned)cache.n_pages;
+                    if (!good) {
+                        atomicOr(a.status, SPEC_STATUS_CAPACITY);
+                        sh.bad_pages[n_seg & 15u] = (int)n_seg + 1;
+                    }
                     const bool got = wait(bar_empty, my_phase ^ 1u);
                     if (!__all_sync(0xffffffffu, got)) return false;
-                    const int pages = block ? 0 : (rows + page - 1) >> cache.page_shift;
+                    __syncwarp();  // (what lane 0's arrival publishes includes the line above)
                     const uint32_t bar = mended ? bar_go : bar_full;
                     if (lane == 0) {
                         mbar_expect_tx(bar, (uint32_t)(block ? TILE : pages * page) * (Q8 ? D + 1 : 2 * D));
@@ -788,16 +834,18 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     if (block) {
                         if (lane < Geo::HALVES) tma_load_3d(dst + lane * (TILE * 128), is_v ? &tm_bv : &tm_bk, 64 * lane, g.h, g.s * a.N + (t - g.first) * TILE, bar);
                     } else if (lane < pages) {
-                        const bool good = (unsigned)pid < (unsigned)cache.n_pages;
-                        if (!good) atomicOr(a.status, SPEC_STATUS_CAPACITY);
                         const int row = good ? (pid * cache.heads + g.h) << cache.page_shift : all_rows;
                         const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
                         if (Q8) {
                             tma_load_2d(dst + lane * page * D, tm, 0, row, bar);
-                            bulk_load(ex + lane * page, (is_v ? cache.v_exp : cache.k_exp) + (good ? row : 0), page, bar);
+                            bulk_load(ex + lane * page, good ? (is_v ? cache.v_exp : cache.k_exp) + row : (is_v ? unit_scales.byte : nan_page.byte), page, bar);
                         } else {
 #pragma unroll
-                            for (int i = 0; i < Geo::HALVES; ++i) tma_load_2d(dst + i * (TILE * 128) + lane * page * 128, tm, 64 * i, row, bar);
+                            for (int i = 0; i < Geo::HALVES; ++i) {
+                                const uint32_t to = dst + i * (TILE * 128) + lane * page * 128;
+                                if (good || is_v) tma_load_2d(to, tm, 64 * i, row, bar);
+                                else bulk_load(to, nan_page.byte, page * 128, bar);
+                            }
                         }
                     }
                     return true;
