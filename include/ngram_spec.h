@@ -290,7 +290,8 @@ int verify_lmhead_argmax_fp8(spec_ctx* ctx, const void* d_hidden, int M, uint8_t
  *              SPEC_STATUS_TOKEN_RANGE, for any other id outside [0, V).
  *   d_entropy  [M] float32 out: entropy of softmax(z), in nats.
  *   d_alt_idx  [M, n_alt] int32 out, d_alt_logp [M, n_alt] float32 out: the n_alt likeliest tokens and their log
- *              probabilities, descending, equal ones by ascending id.  0 <= n_alt <= min(32, V); NULL if 0.
+ *              probabilities, descending, equal ones by ascending id.  0 <= n_alt <= min(32, V); NULL if 0.  A logit that
+ *              is NaN or -inf is no alternative; where there are fewer than n_alt others, the rest is id -1 with -inf.
  *   d_work     spec_score_bytes() of scratch, 16-byte aligned, for this call alone; needs no initial value.
  * bf16 x bf16 products accumulate in fp32 on the tensor cores; the statistics are fp32, relative to the running
  * maximum.  If a bounded device-side wait expires (SPEC_STATUS_TIMEOUT) the outputs mean nothing.

@@ -1264,9 +1264,11 @@ __global__ void __launch_bounds__(MERGE_THREADS) merge_score_kernel(const float4
                 const int next = ++head[i];
                 key[i] = next < (lane + 32 * i + 1) * n_alt ? keys[next] : 0ull;
             }
-        if (lane == 0) {
-            alt_idx[(size_t)row * n_alt + k] = (int32_t)~lo;
-            alt_logp[(size_t)row * n_alt + k] = (from_orderable_f32(hi) - norm.x) - norm.y;
+        if (lane == 0) {  // (a list that no logit entered holds an id beyond the vocabulary)
+            const int id = (int32_t)~lo;
+            const bool there = (unsigned)id < (unsigned)V;
+            alt_idx[(size_t)row * n_alt + k] = there ? id : -1;
+            alt_logp[(size_t)row * n_alt + k] = there ? (from_orderable_f32(hi) - norm.x) - norm.y : -INFINITY;
         }
     }
 }
