@@ -149,6 +149,18 @@ def _i32(t: torch.Tensor | None, name: str, shape):
     return t.data_ptr()
 
 
+def _out(t: torch.Tensor, shape, dtype: torch.dtype, what: str):
+    if t is None or not t.is_cuda or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise SpecError(f"{what}: expected a contiguous {dtype} CUDA tensor of shape {tuple(shape)}")
+
+
+def _scratch(work: torch.Tensor, what: str):
+    """Pointer and bytes of a caller's workspace."""
+    if not work.is_cuda or not work.is_contiguous():
+        raise SpecError(f"{what}: work must be a contiguous CUDA tensor")
+    return work.data_ptr(), work.numel() * work.element_size()
+
+
 class KVCache:
     """A paged key/value cache in the caller's tensors (see ``spec_kv_cache`` in the header).
 
@@ -457,14 +469,17 @@ class SpecContext:
             idx = tokens.new_empty((M, n_alt)) if n_alt > 0 else None
             out = (logp, torch.empty_like(logp), idx, None if idx is None else torch.empty_like(idx, dtype=torch.float32))
         else:
-            for y, shape, dtype in zip(out, ((M,), (M,), (M, n_alt), (M, n_alt)), (torch.float32, torch.float32, torch.int32, torch.float32)):
-                _need((y is None and n_alt == 0) or (y is not None and y.shape == shape and y.dtype == dtype and y.is_cuda and y.is_contiguous()),
-                      "score_tokens: outputs must be contiguous float32 [M], float32 [M], int32 [M, n_alt], float32 [M, n_alt]")
+            _need(len(out) == 4, "score_tokens: out must be (logp, entropy, alt_ids, alt_logp)")
+            for y, shape, dtype, name in zip(out[: 4 if n_alt else 2], ((M,), (M,), (M, n_alt), (M, n_alt)), (torch.float32, torch.float32, torch.int32, torch.float32),
+                                             ("logp", "entropy", "alt_ids", "alt_logp")):
+                _out(y, shape, dtype, f"score_tokens: {name}")
+            if not n_alt:
+                out = (out[0], out[1], None, None)
         if work is None:
             work = hidden.new_empty(max(16, self._lib.spec_score_bytes(self._h, M, n_alt)), dtype=torch.uint8)
         ptr = lambda y: None if y is None else y.data_ptr()
         self._check(self._lib.score_tokens(self._h, hidden.data_ptr(), M, _i32(tokens, "tokens", (M,)), n_alt, ptr(out[0]), ptr(out[1]), ptr(out[2]),
-                                           ptr(out[3]), work.data_ptr(), work.numel(), self._raw_stream()), "score_tokens")
+                                           ptr(out[3]), *_scratch(work, "score_tokens"), self._raw_stream()), "score_tokens")
         return out
 
     def rope_rows(self, rope: Rope, q: torch.Tensor, k: torch.Tensor | None, pos: torch.Tensor, out=None):
@@ -477,8 +492,10 @@ class SpecContext:
         if out is None:
             out = (_new(q), None if k is None else _new(k))
         else:
-            for x, y in zip((q, k), out):
-                _need(x is None or (y.shape == x.shape and y.dtype == x.dtype and y.is_contiguous()), "rope_rows: outputs must be contiguous, of the inputs' shapes")
+            _need(len(out) == 2, "rope_rows: out must be (q_out, k_out)")
+            for x, y, name in zip((q, k), out, ("q_out", "k_out")):
+                if x is not None:
+                    _out(y, x.shape, torch.bfloat16, f"rope_rows: {name}")
         qp, qt, qh = _rows(q, "q")
         kp, kt, kh = (None, 0, 0) if k is None else _rows(k, "k")
         self._check(self._lib.spec_rope_rows(self._h, rope._ref, qp, shape[-2], qt, qh, out[0].data_ptr(), kp, 0 if k is None else k.shape[-2],
@@ -504,9 +521,9 @@ class SpecContext:
             k = torch.empty((S, n, cache.heads, cache.head_dim), dtype=torch.bfloat16, device=cache.k.device)
             out = (k, torch.empty_like(k))
         else:
-            for t in out:
-                _need(tuple(t.shape) == (S, n, cache.heads, cache.head_dim) and t.dtype == torch.bfloat16 and t.is_cuda and t.is_contiguous(),
-                      "cache_read: outputs must be contiguous bfloat16 [S, n, heads, head_dim]")
+            _need(len(out) == 2, "cache_read: out must be (k, v)")
+            for t, name in zip(out, "kv"):
+                _out(t, (S, n, cache.heads, cache.head_dim), torch.bfloat16, f"cache_read: {name}")
         self._check(self._lib.spec_cache_read(self._h, cache._ref, S, n, _i32(start, "start", (S,)), _i32(count, "count", (S,)),
                                               out[0].data_ptr(), out[1].data_ptr(), self._raw_stream()), "spec_cache_read")
         return out
@@ -533,9 +550,10 @@ class SpecContext:
         if out is None:
             out = (_new(q), q.new_empty((S, N, Hq), dtype=torch.float32) if with_lse else None)
         else:
-            for y, shape, dtype in zip(out, (q.shape, q.shape[:3]), (torch.bfloat16, torch.float32)):
-                _need(y is None or (y.shape == shape and y.dtype == dtype and y.is_cuda and y.is_contiguous()),
-                      "tree_attention: outputs must be contiguous, bfloat16 [S, N, Hq, head_dim] and float32 [S, N, Hq]")
+            _need(len(out) == 2, "tree_attention: out must be (out, lse or None)")
+            _out(out[0], q.shape, torch.bfloat16, "tree_attention: out")
+            if out[1] is not None:
+                _out(out[1], q.shape[:3], torch.float32, "tree_attention: lse")
         if work is None:
             key = (S, N, Hq, cache.heads, D)
             need = self._work_bytes.get(key)
@@ -545,7 +563,7 @@ class SpecContext:
         self._check(self._lib.spec_tree_attention(self._h, cache._ref, *_rows(q, "q"), *_rows(k, "k"), *_rows(v, "v"), S, N, Hq,
                                                   _i32(mask, "mask", (S, N, (N + 31) // 32)), _i32(lens, "lens", (S,)),
                                                   _i32(n_nodes, "n_nodes", (S,)), D ** -0.5 if scale is None else scale,
-                                                  out[0].data_ptr(), None if out[1] is None else out[1].data_ptr(), work.data_ptr(), work.numel(),
+                                                  out[0].data_ptr(), None if out[1] is None else out[1].data_ptr(), *_scratch(work, "tree_attention"),
                                                   self._raw_stream()), "spec_tree_attention")
         return out
 

@@ -1,0 +1,62 @@
+"""What the calls around the model's attention take from a user, and what they refuse."""
+import pytest
+import torch
+
+import attn_util as au
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    import paper_2411_03786_b200 as ngs
+    g = torch.Generator().manual_seed(0)
+    w = torch.randn(100, 64, generator=g).bfloat16().cuda()
+    c = ngs.SpecContext(w, w)
+    yield c
+    c.close()
+
+
+def operands(S=2, N=3, Hq=4, Hkv=2, D=64, tokens=64):
+    cache, _, _ = au.make_cache(S, tokens, Hkv, D, 16, False, 4)
+    g = torch.Generator().manual_seed(5)
+    q, k, v = (torch.randn(S, N, h, D, generator=g).bfloat16().cuda() for h in (Hq, Hkv, Hkv))
+    mask = au.pack(torch.eye(N, dtype=torch.bool).expand(S, N, N)).cuda()
+    return cache, q, k, v, mask, torch.full((S,), min(20, tokens), dtype=torch.int32).cuda()
+
+
+def rope(ngs, D=64):
+    return ngs.Rope((10000.0 ** (-torch.arange(0, D, 2) / D)).float().cuda())
+
+
+def test_outputs_and_workspaces_in_host_memory_are_refused(ctx):
+    import paper_2411_03786_b200 as ngs
+    cache, q, k, v, mask, lens = operands()
+    pos = torch.zeros(2, 3, dtype=torch.int32).cuda()
+    h, tok = torch.randn(4, 64).bfloat16().cuda(), torch.zeros(4, dtype=torch.int32).cuda()
+    ok = ctx.rope_rows(rope(ngs), q, k, pos)
+    scores = ctx.score_tokens(h, tok, n_alt=2)
+    att = ctx.tree_attention(cache, q, k, v, mask, lens, with_lse=True)
+    read = ctx.cache_read(cache, lens, 2)
+    big = torch.empty(1 << 27, dtype=torch.uint8)
+    for f in (lambda: ctx.rope_rows(rope(ngs), q, k, pos, out=(ok[0].cpu(), ok[1])),
+              lambda: ctx.rope_rows(rope(ngs), q, k, pos, out=(ok[0], ok[1].cpu())),
+              lambda: ctx.rope_rows(rope(ngs), q, k, pos, out=(ok[0], None)),
+              lambda: ctx.score_tokens(h, tok, work=big),
+              lambda: ctx.score_tokens(h, tok, n_alt=2, out=(scores[0].cpu(), *scores[1:])),
+              lambda: ctx.score_tokens(h, tok, n_alt=2, out=(*scores[:2], None, None)),
+              lambda: ctx.score_tokens(h, tok, n_alt=2, out=scores[:2]),
+              lambda: ctx.cache_read(cache, lens, 2, out=(read[0], read[1].cpu())),
+              lambda: ctx.tree_attention(cache, q, k, v, mask, lens, work=big),
+              lambda: ctx.tree_attention(cache, q, k, v, mask, lens, work=big.cuda()[::2]),
+              lambda: ctx.tree_attention(cache, q, k, v, mask, lens, out=(None, att[1])),
+              lambda: ctx.tree_attention(cache, q, k, v, mask, lens, out=(att[0], att[1].cpu()))):
+        with pytest.raises(ngs.SpecError):
+            f()
+    # a workspace counts by its bytes, whatever its type
+    need = ctx._lib.spec_tree_attention_bytes(ctx._h, cache._ref, 2, 3, 4)
+    got = ctx.tree_attention(cache, q, k, v, mask, lens, with_lse=True, work=torch.empty((need + 3) // 4, dtype=torch.float32, device="cuda"))
+    assert torch.equal(got[0], att[0]) and torch.equal(got[1], att[1])
+    with pytest.raises(ngs.SpecError):
+        ctx.tree_attention(cache, q, k, v, mask, lens, work=torch.empty(need // 4 - 4, dtype=torch.float32, device="cuda"))
+    assert ctx.get_status() == 0
