@@ -150,8 +150,9 @@ def _i32(t: torch.Tensor | None, name: str, shape):
 
 
 def _out(t: torch.Tensor, shape, dtype: torch.dtype, what: str):
-    if t is None or not t.is_cuda or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        raise SpecError(f"{what}: expected a contiguous {dtype} CUDA tensor of shape {tuple(shape)}")
+    # (pinned host memory will do, as in _ptr)
+    if t is None or not (t.is_cuda or t.is_pinned()) or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise SpecError(f"{what}: expected a contiguous {dtype} CUDA (or pinned host) tensor of shape {tuple(shape)}")
 
 
 def _scratch(work: torch.Tensor, what: str):

@@ -60,3 +60,20 @@ def test_outputs_and_workspaces_in_host_memory_are_refused(ctx):
     with pytest.raises(ngs.SpecError):
         ctx.tree_attention(cache, q, k, v, mask, lens, work=torch.empty(need // 4 - 4, dtype=torch.float32, device="cuda"))
     assert ctx.get_status() == 0
+
+
+def test_outputs_in_pinned_host_memory(ctx):
+    """As the older calls allow: results that reach the host without a copy."""
+    import paper_2411_03786_b200 as ngs
+    cache, q, k, v, mask, lens = operands()
+    pos = torch.arange(6, dtype=torch.int32).view(2, 3).cuda()
+    h, tok = torch.randn(4, 64).bfloat16().cuda(), torch.zeros(4, dtype=torch.int32).cuda()
+    calls = (lambda out: ctx.rope_rows(rope(ngs), q, k, pos, out=out), lambda out: ctx.score_tokens(h, tok, n_alt=2, out=out),
+             lambda out: ctx.cache_read(cache, lens, 2, out=out), lambda out: ctx.tree_attention(cache, q, k, v, mask, lens, with_lse=True, out=out))
+    for f in calls:
+        want = f(None)
+        got = tuple(torch.empty_like(t, device="cpu").pin_memory() for t in want)
+        f(got)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b.cpu()) for a, b in zip(got, want))
+    assert ctx.get_status() == 0
