@@ -131,14 +131,23 @@ def _need(ok: bool, what: str):
 
 
 def _rows(t: torch.Tensor, name: str):
-    """Pointer, token stride and head stride of ``t[S, N, heads, D]`` or ``t[T, heads, D]`` whose head vectors are
-    contiguous and whose sequences follow one another at N token strides."""
+    """Pointer, token stride and head stride of ``t[S, N, heads, D]`` or ``t[T, heads, D]`` (see _strides)."""
     if not t.is_cuda or t.dtype is not torch.bfloat16:
         raise SpecError(f"{name}: expected a bfloat16 CUDA tensor")
-    st = t.stride()
-    if st[-1] != 1 or (len(st) == 4 and t.shape[0] > 1 and st[0] != st[1] * t.shape[1]):
-        raise SpecError(f"{name}: head vectors must be contiguous, and sequences N tokens apart")
-    return t.data_ptr(), st[-3], st[-2]
+    return t.data_ptr(), *_strides(t, name)
+
+
+def _strides(t: torch.Tensor, name: str):
+    """Token and head stride of ``t`` whose head vectors are contiguous and whose sequences follow one another at N token
+    strides.  With one node to a sequence the sequences are the tokens, and the stride of the nodes means nothing."""
+    *seq, tok, head, one = t.stride()
+    if seq and seq[0] != tok * t.shape[1] and t.shape[0] > 1:
+        tok = seq[0]
+        if t.shape[1] > 1:
+            raise SpecError(f"{name}: sequences must be N tokens apart")
+    if one != 1:
+        raise SpecError(f"{name}: head vectors must be contiguous")
+    return tok, head
 
 
 def _i32(t: torch.Tensor | None, name: str, shape):

@@ -34,3 +34,16 @@ def test_tensors_have_to_be_on_a_gpu():
         ngs.KVCache(kv, kv, table)
     with pytest.raises(ngs.SpecError):
         ngs.Rope(torch.zeros(32))
+
+
+def test_strides_of_rows():
+    """Token and head strides that the calls are given, and the layouts that have none."""
+    from paper_2411_03786_b200.binding import _strides
+    t = torch.zeros(4, 3, 12, 64)
+    assert _strides(t, "t") == (768, 64) and _strides(t[:, :, :8], "t") == (768, 64) and _strides(t[0], "t") == (768, 64)
+    fused = torch.zeros(4, 12, 64)
+    assert _strides(fused[:, :8].unsqueeze(1), "t") == (768, 64)  # one node to a sequence
+    assert _strides(t[:, 2:], "t") == (3 * 768, 64) and _strides(t[:1, 1:], "t") == (768, 64)
+    for bad in (t[:, :2], t[..., ::2], t.transpose(0, 1)):
+        with pytest.raises(ngs.SpecError):
+            _strides(bad, "t")

@@ -77,3 +77,28 @@ def test_outputs_in_pinned_host_memory(ctx):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b.cpu()) for a, b in zip(got, want))
     assert ctx.get_status() == 0
+
+
+def test_one_node_of_each_sequence_out_of_a_fused_projection(ctx):
+    """Plain decoding: queries, keys and values cut out of one [S, Hq + 2 Hkv, D] product."""
+    import paper_2411_03786_b200 as ngs
+    S, Hq, Hkv, D = 5, 8, 2, 64
+    cache, _, _ = au.make_cache(S, 40, Hkv, D, 16, False, 4)
+    qkv = torch.randn(S, Hq + 2 * Hkv, D, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    cut = tuple(t.unsqueeze(1) for t in qkv.split([Hq, Hkv, Hkv], 1))
+    pos = torch.arange(S, dtype=torch.int32).view(S, 1).cuda()
+    lens = (torch.arange(S) * 7).int().cuda()
+    mask = torch.ones(S, 1, 1, dtype=torch.int32).cuda()
+    out = []
+    for q, k, v in (cut, tuple(t.contiguous() for t in cut)):
+        r = ctx.rope_rows(rope(ngs), q, k, pos)
+        a = ctx.tree_attention(cache, q, k, v, mask, lens, with_lse=True)
+        c = ngs.KVCache(cache.k.clone(), cache.v.clone(), cache.table)
+        ctx.cache_write(c, k, v, lens, rope=rope(ngs))
+        out.append((*r, *a, c.k, c.v))
+    assert all(torch.equal(x, y) for x, y in zip(*out)) and ctx.get_status() == 0
+    # the last of several nodes, likewise
+    t = torch.randn(S, 3, Hq + 2 * Hkv, D).bfloat16().cuda()[:, -1:]
+    q, k, v = t.split([Hq, Hkv, Hkv], 2)
+    a = ctx.tree_attention(cache, q, k, v, mask, lens)[0]
+    assert torch.equal(a, ctx.tree_attention(cache, q.contiguous(), k.contiguous(), v.contiguous(), mask, lens)[0])
