@@ -131,22 +131,30 @@ def _need(ok: bool, what: str):
 
 
 def _rows(t: torch.Tensor, name: str):
-    """Pointer, token stride and head stride of ``t[S, N, heads, D]`` or ``t[T, heads, D]`` (see _strides)."""
+    """Pointer, token stride and head stride of ``t[..., heads, D]`` (see _strides)."""
     if not t.is_cuda or t.dtype is not torch.bfloat16:
         raise SpecError(f"{name}: expected a bfloat16 CUDA tensor")
     return t.data_ptr(), *_strides(t, name)
 
 
 def _strides(t: torch.Tensor, name: str):
-    """Token and head stride of ``t`` whose head vectors are contiguous and whose sequences follow one another at N token
-    strides.  With one node to a sequence the sequences are the tokens, and the stride of the nodes means nothing."""
-    *seq, tok, head, one = t.stride()
-    if seq and seq[0] != tok * t.shape[1] and t.shape[0] > 1:
-        tok = seq[0]
-        if t.shape[1] > 1:
-            raise SpecError(f"{name}: sequences must be N tokens apart")
+    """Token and head stride of ``t[..., heads, D]`` whose head vectors are contiguous and whose tokens are all one stride
+    apart.  The stride of a dimension of one means nothing: with one node to a sequence the sequences are the tokens."""
+    *lead, head, one = t.stride()
     if one != 1:
         raise SpecError(f"{name}: head vectors must be contiguous")
+    tok = lead[-1]
+    if len(lead) > 2 or (len(lead) == 2 and lead[0] != tok * t.shape[1]):
+        after = None  # where the next dimension has to go on
+        for n, st in zip(reversed(t.shape[:-2]), reversed(lead)):
+            if n == 0:
+                break
+            if n > 1:
+                if after is None:
+                    tok = after = st
+                elif st != after:
+                    raise SpecError(f"{name}: tokens must be one stride apart (sequences N tokens)")
+                after *= n
     return tok, head
 
 
@@ -498,6 +506,7 @@ class SpecContext:
         Returns contiguous ``(q_out, k_out)``, or writes to ``out``, whose tensors may be ``q`` and ``k`` themselves.
         """
         shape = q.shape
+        _need(len(shape) > 2, "rope_rows: q must be [T, Hq, D] or [S, N, Hq, D]")
         _need(k is None or (k.shape[-1] == shape[-1] and k.shape[:-2] == shape[:-2]), "rope_rows: q and k must have the same tokens and head size")
         if out is None:
             out = (_new(q), None if k is None else _new(k))

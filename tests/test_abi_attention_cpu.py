@@ -47,3 +47,14 @@ def test_strides_of_rows():
     for bad in (t[:, :2], t[..., ::2], t.transpose(0, 1)):
         with pytest.raises(ngs.SpecError):
             _strides(bad, "t")
+
+
+def test_strides_of_more_dimensions():
+    from paper_2411_03786_b200.binding import _strides
+    t = torch.zeros(2, 5, 3, 12, 64)
+    assert _strides(t, "t") == (768, 64) and _strides(t[:, :, :, 4:], "t") == (768, 64)
+    assert _strides(t[:, :1, :1], "t") == (5 * 3 * 768, 64) and _strides(t[:1, :, 1:2], "t") == (3 * 768, 64) and _strides(t[1:, 2:3], "t") == (768, 64)
+    assert _strides(t[:, :0], "t")[1] == 64 and _strides(torch.zeros(1, 1, 1, 2, 16), "t")[1] == 16
+    for bad in (t[:, :, :2], t[:, :4], t.transpose(0, 1), t.transpose(1, 2)):
+        with pytest.raises(ngs.SpecError):
+            _strides(bad, "t")

@@ -102,3 +102,18 @@ def test_one_node_of_each_sequence_out_of_a_fused_projection(ctx):
     q, k, v = t.split([Hq, Hkv, Hkv], 2)
     a = ctx.tree_attention(cache, q, k, v, mask, lens)[0]
     assert torch.equal(a, ctx.tree_attention(cache, q.contiguous(), k.contiguous(), v.contiguous(), mask, lens)[0])
+
+
+def test_rope_of_more_dimensions(ctx):
+    """Tokens in several dimensions are taken where they are one stride apart, and refused where not."""
+    import paper_2411_03786_b200 as ngs
+    t = torch.randn(2, 3, 4, 6, 64).bfloat16().cuda()
+    pos = torch.arange(24, dtype=torch.int32).view(2, 3, 4).cuda()
+    want = ctx.rope_rows(rope(ngs), t.view(24, 6, 64), None, pos.view(24))[0].view(t.shape)
+    assert torch.equal(ctx.rope_rows(rope(ngs), t, None, pos)[0], want)
+    assert torch.equal(ctx.rope_rows(rope(ngs), t[:, :, :, 2:], None, pos)[0], want[:, :, :, 2:])
+    assert torch.equal(ctx.rope_rows(rope(ngs), t[:, :1, 3:], None, pos[:, :1, 3:].contiguous())[0], want[:, :1, 3:])
+    for x in (t[:, :, :2], t[:, :2], t.transpose(1, 2), t[0, 0, 0]):
+        with pytest.raises(ngs.SpecError):
+            ctx.rope_rows(rope(ngs), x, None, torch.zeros(x.shape[:-2], dtype=torch.int32).cuda())
+    assert ctx.get_status() == 0
