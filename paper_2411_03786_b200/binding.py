@@ -577,8 +577,10 @@ class SpecContext:
             key = (S, N, Hq, cache.heads, D)
             need = self._work_bytes.get(key)
             if need is None:
-                need = self._work_bytes[key] = max(16, self._lib.spec_tree_attention_bytes(self._h, cache._ref, S, N, Hq))
-            work = q.new_empty(need, dtype=torch.uint8)
+                need = self._lib.spec_tree_attention_bytes(self._h, cache._ref, S, N, Hq)
+                if need:  # (0: something else is refused, which is not a property of the sizes)
+                    self._work_bytes[key] = need
+            work = q.new_empty(max(need, 16), dtype=torch.uint8)
         self._check(self._lib.spec_tree_attention(self._h, cache._ref, *_rows(q, "q"), *_rows(k, "k"), *_rows(v, "v"), S, N, Hq,
                                                   _i32(mask, "mask", (S, N, (N + 31) // 32)), _i32(lens, "lens", (S,)),
                                                   _i32(n_nodes, "n_nodes", (S,)), D ** -0.5 if scale is None else scale,

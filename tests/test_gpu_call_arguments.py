@@ -117,3 +117,14 @@ def test_rope_of_more_dimensions(ctx):
         with pytest.raises(ngs.SpecError):
             ctx.rope_rows(rope(ngs), x, None, torch.zeros(x.shape[:-2], dtype=torch.int32).cuda())
     assert ctx.get_status() == 0
+
+
+def test_a_refused_cache_does_not_spoil_the_next_call(ctx):
+    """A cache that is refused for its pages, then a good one of the same sizes."""
+    import paper_2411_03786_b200 as ngs
+    cache, q, k, v, mask, lens = operands(S=2, N=5, Hq=6, Hkv=2)
+    t = torch.zeros(8, 2, 8, 64, dtype=torch.bfloat16, device="cuda")  # pages of 8
+    with pytest.raises(ngs.SpecError):
+        ctx.tree_attention(ngs.KVCache(t, t.clone(), cache.table), q, k, v, mask, lens)
+    assert ctx.tree_attention(cache, q, k, v, mask, lens)[0].isfinite().all()
+    assert ctx.get_status() == 0
