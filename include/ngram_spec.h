@@ -315,7 +315,7 @@ int score_tokens(spec_ctx* ctx, const void* d_hidden, int M, const int32_t* d_to
  * scale byte 255 and reads as NaN.
  *
  * Limits: head_dim 64 or 128; page 16, 32, 64 or 128; n_pages * heads * page < 2^31; max_pages * page <= 2^30; S <= 65535;
- * N <= 4096, Hq <= 4096, N * Hq / heads <= 2^22; all pointers to elements and scales 16-byte aligned.  Strides count
+ * N <= 4096, Hq <= 4096, N * Hq / heads <= 2^22 (a call of no sequences, nodes or tokens does nothing); all pointers to elements and scales 16-byte aligned.  Strides count
  * elements, are multiples of 8, and head vectors are contiguous; node i of sequence s is token s*N + i.  A length or
  * position outside a sequence's pages, or a page outside [0, n_pages), sets
  * SPEC_STATUS_CAPACITY: such a position is skipped, such a length leaves the sequence's outputs as for an empty row.

@@ -492,12 +492,12 @@ size_t spec_score_bytes(spec_ctx* ctx, int M, int n_alt) {
 int score_tokens(spec_ctx* ctx, const void* d_hidden, int M, const int32_t* d_tokens, int n_alt, float* d_logp, float* d_entropy,
                  int32_t* d_alt_idx, float* d_alt_logp, void* d_work, size_t work_bytes, void* stream) {
     if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "score_tokens: ctx is NULL");
-    if (!d_hidden || !d_tokens || !d_logp || !d_entropy || !d_work) return fail(ctx, SPEC_ERR_ARG, "score_tokens: NULL pointer");
-    if (!aligned16(d_hidden) || !aligned16(d_work)) return fail(ctx, SPEC_ERR_ARG, "score_tokens: d_hidden and d_work must be 16-byte aligned");
     if (M < 0 || M > SPEC_MAX_VERIFY_ROWS) return fail(ctx, SPEC_ERR_ARG, "score_tokens: need 0 <= M <= %d", SPEC_MAX_VERIFY_ROWS);
-    if (n_alt < 0 || n_alt > kMaxKTab || n_alt > ctx->V || (n_alt > 0 && (!d_alt_idx || !d_alt_logp)))
-        return fail(ctx, SPEC_ERR_ARG, "score_tokens: need 0 <= n_alt <= min(%d, V), with both outputs for n_alt > 0", kMaxKTab);
+    if (n_alt < 0 || n_alt > kMaxKTab || n_alt > ctx->V) return fail(ctx, SPEC_ERR_ARG, "score_tokens: need 0 <= n_alt <= min(%d, V)", kMaxKTab);
     if (M == 0) return SPEC_OK;
+    if (!d_hidden || !d_tokens || !d_logp || !d_entropy || !d_work) return fail(ctx, SPEC_ERR_ARG, "score_tokens: NULL pointer");
+    if (n_alt > 0 && (!d_alt_idx || !d_alt_logp)) return fail(ctx, SPEC_ERR_ARG, "score_tokens: n_alt > 0 needs both outputs of the alternatives");
+    if (!aligned16(d_hidden) || !aligned16(d_work)) return fail(ctx, SPEC_ERR_ARG, "score_tokens: d_hidden and d_work must be 16-byte aligned");
     const size_t need = score_bytes(ctx, M, n_alt);
     if (work_bytes < need) return fail(ctx, SPEC_ERR_ARG, "score_tokens: %zu bytes of scratch given, %zu needed", work_bytes, need);
     cudaSetDevice(ctx->device);
@@ -505,8 +505,10 @@ int score_tokens(spec_ctx* ctx, const void* d_hidden, int M, const int32_t* d_to
 }
 
 // ------------------------------------------------------------------------------------------ attention and its cache
-static int check_cache(spec_ctx* ctx, const spec_kv_cache* c, const char* who, CacheArgs* out) {
-    if (!c || !c->d_k || !c->d_v || !c->d_table) return fail(ctx, SPEC_ERR_ARG, "%s: NULL cache pointer", who);
+// (A batch of no sequences has an empty table, which may have no address.  Likewise below: sizes are looked at first, and a call
+// that has nothing to do looks at no pointer of what is empty.)
+static int check_cache(spec_ctx* ctx, const spec_kv_cache* c, int S, const char* who, CacheArgs* out) {
+    if (!c || !c->d_k || !c->d_v || (S > 0 && !c->d_table)) return fail(ctx, SPEC_ERR_ARG, "%s: NULL cache pointer", who);
     if (!aligned16(c->d_k) || !aligned16(c->d_v)) return fail(ctx, SPEC_ERR_ARG, "%s: cache pointers must be 16-byte aligned", who);
     if (c->dtype != SPEC_BF16 && c->dtype != SPEC_E4M3) return fail(ctx, SPEC_ERR_ARG, "%s: cache dtype must be SPEC_BF16 or SPEC_E4M3", who);
     if (c->dtype == SPEC_E4M3 && (!c->d_k_exp || !c->d_v_exp || !aligned16(c->d_k_exp) || !aligned16(c->d_v_exp)))
@@ -541,14 +543,15 @@ int spec_rope_rows(spec_ctx* ctx, const spec_rope* rope, const void* d_q, int Hq
                    void* stream) {
     const char* who = "spec_rope_rows";
     if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
-    if (!rope || !d_pos) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
+    if (!rope) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
     if (head_dim < 16 || head_dim > 512 || head_dim % 16 != 0) return fail(ctx, SPEC_ERR_ARG, "%s: need 16 <= head_dim <= 512, head_dim %% 16 == 0", who);
     if (T < 0 || Hq < 1 || Hk < 0 || Hq > 4096 || Hk > 4096) return fail(ctx, SPEC_ERR_ARG, "%s: need T >= 0, 1 <= Hq <= 4096, 0 <= Hk <= 4096", who);
     RopeArgs r;
     int rc = check_rope(ctx, rope, head_dim, who, &r);
-    if (rc || (rc = check_rows(ctx, d_q, q_tok, q_head, who, "q")) || (rc = check_rows(ctx, d_q_out, 0, 0, who, "q_out"))) return rc;
+    if (rc || T == 0) return rc;
+    if (!d_pos) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
+    if ((rc = check_rows(ctx, d_q, q_tok, q_head, who, "q")) || (rc = check_rows(ctx, d_q_out, 0, 0, who, "q_out"))) return rc;
     if (Hk && ((rc = check_rows(ctx, d_k, k_tok, k_head, who, "k")) || (rc = check_rows(ctx, d_k_out, 0, 0, who, "k_out")))) return rc;
-    if (T == 0) return SPEC_OK;
     cudaSetDevice(ctx->device);
     return launch_rope_rows(ctx, r, d_q, Hq, q_tok, q_head, d_q_out, d_k, Hk, k_tok, k_head, d_k_out, head_dim, d_pos, T, (cudaStream_t)stream);
 }
@@ -560,12 +563,13 @@ int spec_cache_write(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_k,
     if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
     CacheArgs c;
     RopeArgs r{nullptr, 0, 0, 1.0f};
-    int rc = check_cache(ctx, cache, who, &c);
-    if (rc || (rc = check_rows(ctx, d_k, k_tok, k_head, who, "k")) || (rc = check_rows(ctx, d_v, v_tok, v_head, who, "v"))) return rc;
-    if (!d_start) return fail(ctx, SPEC_ERR_ARG, "%s: d_start is NULL", who);
+    int rc = check_cache(ctx, cache, S, who, &c);
+    if (rc) return rc;
     if (S < 0 || S > 65535 || N < 0 || n < 0 || (!d_nodes && n > N)) return fail(ctx, SPEC_ERR_ARG, "%s: need 0 <= S <= 65535, N >= 0, n >= 0, and n <= N without d_nodes", who);
     if (rope && (rc = check_rope(ctx, rope, c.head_dim, who, &r))) return rc;
-    if (S == 0 || n == 0) return SPEC_OK;
+    if (S == 0 || n == 0 || N == 0) return SPEC_OK;  // (of no nodes every one that is named is skipped)
+    if ((rc = check_rows(ctx, d_k, k_tok, k_head, who, "k")) || (rc = check_rows(ctx, d_v, v_tok, v_head, who, "v"))) return rc;
+    if (!d_start) return fail(ctx, SPEC_ERR_ARG, "%s: d_start is NULL", who);
     cudaSetDevice(ctx->device);
     return launch_cache_write(ctx, c, d_k, k_tok, k_head, d_v, v_tok, v_head, S, N, n, d_nodes, d_start, d_count, r, (cudaStream_t)stream);
 }
@@ -575,11 +579,12 @@ int spec_cache_read(spec_ctx* ctx, const spec_kv_cache* cache, int S, int n, con
     const char* who = "spec_cache_read";
     if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
     CacheArgs c;
-    int rc = check_cache(ctx, cache, who, &c);
-    if (rc || (rc = check_rows(ctx, d_k_out, 0, 0, who, "k_out")) || (rc = check_rows(ctx, d_v_out, 0, 0, who, "v_out"))) return rc;
-    if (!d_start) return fail(ctx, SPEC_ERR_ARG, "%s: d_start is NULL", who);
+    int rc = check_cache(ctx, cache, S, who, &c);
+    if (rc) return rc;
     if (S < 0 || S > 65535 || n < 0) return fail(ctx, SPEC_ERR_ARG, "%s: need 0 <= S <= 65535, n >= 0", who);
     if (S == 0 || n == 0) return SPEC_OK;
+    if ((rc = check_rows(ctx, d_k_out, 0, 0, who, "k_out")) || (rc = check_rows(ctx, d_v_out, 0, 0, who, "v_out"))) return rc;
+    if (!d_start) return fail(ctx, SPEC_ERR_ARG, "%s: d_start is NULL", who);
     cudaSetDevice(ctx->device);
     return launch_cache_read(ctx, c, S, n, d_start, d_count, d_k_out, d_v_out, (cudaStream_t)stream);
 }
@@ -587,17 +592,17 @@ int spec_cache_read(spec_ctx* ctx, const spec_kv_cache* cache, int S, int n, con
 int spec_tree_mask(spec_ctx* ctx, const int32_t* d_parent, int S, int N, const int32_t* d_nnodes, int32_t* d_mask, int32_t* d_depth,
                    void* stream) {
     if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "spec_tree_mask: ctx is NULL");
+    if (S < 0 || S > 65535 || N < 0 || N > kMaxNodes) return fail(ctx, SPEC_ERR_ARG, "spec_tree_mask: need 0 <= S <= 65535, 0 <= N <= %d", kMaxNodes);
+    if (S == 0 || N == 0) return SPEC_OK;
     if (!d_parent || !d_mask) return fail(ctx, SPEC_ERR_ARG, "spec_tree_mask: NULL pointer");
-    if (S < 0 || S > 65535 || N < 1 || N > kMaxNodes) return fail(ctx, SPEC_ERR_ARG, "spec_tree_mask: need 0 <= S <= 65535, 1 <= N <= %d", kMaxNodes);
-    if (S == 0) return SPEC_OK;
     cudaSetDevice(ctx->device);
     return launch_tree_mask(ctx, d_parent, S, N, d_nnodes, d_mask, d_depth, (cudaStream_t)stream);
 }
 
 static int check_block(spec_ctx* ctx, const spec_kv_cache* cache, int S, int N, int Hq, const char* who, CacheArgs* c) {
-    int rc = check_cache(ctx, cache, who, c);
+    int rc = check_cache(ctx, cache, S, who, c);
     if (rc) return rc;
-    if (S < 0 || S > 65535 || N < 1 || N > kMaxNodes) return fail(ctx, SPEC_ERR_ARG, "%s: need 0 <= S <= 65535, 1 <= N <= %d", who, kMaxNodes);
+    if (S < 0 || S > 65535 || N < 0 || N > kMaxNodes) return fail(ctx, SPEC_ERR_ARG, "%s: need 0 <= S <= 65535, 0 <= N <= %d", who, kMaxNodes);
     if (Hq < c->heads || Hq % c->heads != 0 || Hq > 4096) return fail(ctx, SPEC_ERR_ARG, "%s: Hq must be a multiple of the cache's heads, at most 4096", who);
     if ((long long)N * (Hq / c->heads) > (1 << 22)) return fail(ctx, SPEC_ERR_ARG, "%s: N * Hq / heads exceeds 2^22", who);
     return SPEC_OK;
@@ -605,7 +610,7 @@ static int check_block(spec_ctx* ctx, const spec_kv_cache* cache, int S, int N, 
 
 size_t spec_tree_attention_bytes(spec_ctx* ctx, const spec_kv_cache* cache, int S, int N, int Hq) {
     CacheArgs c;
-    if (!ctx || check_block(ctx, cache, S, N, Hq, "spec_tree_attention_bytes", &c)) return 0;
+    if (!ctx || check_block(ctx, cache, S, N, Hq, "spec_tree_attention_bytes", &c) || S == 0 || N == 0) return 0;
     return tree_attention_bytes(ctx->num_sms, S, N, Hq, c.heads, c.head_dim);
 }
 
@@ -617,7 +622,10 @@ int spec_tree_attention(spec_ctx* ctx, const spec_kv_cache* cache, const void* d
     if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
     TreeAttnArgs a{};
     int rc = check_block(ctx, cache, S, N, Hq, who, &a.cache);
-    if (rc || (rc = check_rows(ctx, d_q, q_tok, q_head, who, "q")) || (rc = check_rows(ctx, d_k, k_tok, k_head, who, "k")) ||
+    if (rc) return rc;
+    if (!(scale > 0.0f) || scale > 3e38f) return fail(ctx, SPEC_ERR_ARG, "%s: scale must be positive and finite", who);
+    if (S == 0 || N == 0) return SPEC_OK;
+    if ((rc = check_rows(ctx, d_q, q_tok, q_head, who, "q")) || (rc = check_rows(ctx, d_k, k_tok, k_head, who, "k")) ||
         (rc = check_rows(ctx, d_v, v_tok, v_head, who, "v")) || (rc = check_rows(ctx, d_out, 0, 0, who, "out")) ||
         (rc = check_rows(ctx, d_work, 0, 0, who, "work")))
         return rc;
@@ -625,10 +633,8 @@ int spec_tree_attention(spec_ctx* ctx, const spec_kv_cache* cache, const void* d
     if ((a.cache.heads > 1 && (k_head <= 0 || v_head <= 0)) || ((long long)S * N > 1 && (k_tok <= 0 || v_tok <= 0)) || k_head >= (1ll << 38) ||
         v_head >= (1ll << 38) || k_tok >= (1ll << 38) || v_tok >= (1ll << 38))
         return fail(ctx, SPEC_ERR_ARG, "%s: strides of k and v must be positive and below 2^38", who);
-    if (!(scale > 0.0f) || scale > 3e38f) return fail(ctx, SPEC_ERR_ARG, "%s: scale must be positive and finite", who);
     const size_t need = tree_attention_bytes(ctx->num_sms, S, N, Hq, a.cache.heads, a.cache.head_dim);
     if (work_bytes < need) return fail(ctx, SPEC_ERR_ARG, "%s: %zu bytes of scratch given, %zu needed", who, work_bytes, need);
-    if (S == 0) return SPEC_OK;
     a.q = d_q; a.k = d_k; a.v = d_v;
     a.q_tok = q_tok; a.q_head = q_head;
     a.k_tok = k_tok; a.k_head = k_head;

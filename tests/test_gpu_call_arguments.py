@@ -128,3 +128,40 @@ def test_a_refused_cache_does_not_spoil_the_next_call(ctx):
         ctx.tree_attention(ngs.KVCache(t, t.clone(), cache.table), q, k, v, mask, lens)
     assert ctx.tree_attention(cache, q, k, v, mask, lens)[0].isfinite().all()
     assert ctx.get_status() == 0
+
+
+def test_empty_calls_do_nothing(ctx):
+    """No sequences, no nodes, no tokens, no rows: tensors without an address."""
+    import paper_2411_03786_b200 as ngs
+    D, before = 64, ctx.launch_count()
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")
+    rows = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device="cuda")
+    f = rope(ngs)
+    a, b = ctx.rope_rows(f, rows(0, 4, D), rows(0, 2, D), i32(0))
+    assert a.shape == (0, 4, D) and b.shape == (0, 2, D)
+    assert ctx.rope_rows(f, rows(3, 0, 4, D), None, i32(3, 0))[0].shape == (3, 0, 4, D)
+    assert [t.shape for t in ctx.score_tokens(rows(0, 64), i32(0), n_alt=3)] == [(0,), (0,), (0, 3), (0, 3)]
+    for quantised in (False, True):
+        none = ngs.KVCache.empty(2, 2, 16, D, i32(0, 4), quantised)
+        ctx.cache_write(none, rows(0, 3, 2, D), rows(0, 3, 2, D), i32(0), rope=f)
+        assert ctx.cache_read(none, i32(0), 5)[0].shape == (0, 5, 2, D)
+        mask, depth = ctx.tree_mask(i32(0, 3))
+        assert mask.shape == (0, 3, 1) and depth.shape == (0, 3)
+        o, l = ctx.tree_attention(none, rows(0, 3, 4, D), rows(0, 3, 2, D), rows(0, 3, 2, D), mask, i32(0), with_lse=True)
+        assert o.shape == (0, 3, 4, D) and l.shape == (0, 3, 4)
+        some = ngs.KVCache.empty(2, 2, 16, D, i32(3, 1), quantised)
+        some.k.zero_()
+        ctx.cache_write(some, rows(3, 0, 2, D), rows(3, 0, 2, D), i32(3))
+        ctx.cache_write(some, rows(3, 0, 2, D), rows(3, 0, 2, D), i32(3), nodes=i32(3, 2))  # nodes that there are not
+        ctx.cache_write(some, rows(3, 2, 2, D) + 1, rows(3, 2, 2, D) + 1, i32(3), nodes=i32(3, 0))
+        assert (some.k == 0).all()
+        assert ctx.cache_read(some, i32(3), 0)[1].shape == (3, 0, 2, D)
+        mask, depth = ctx.tree_mask(i32(3, 0))
+        assert mask.shape == (3, 0, 0) and depth.shape == (3, 0)
+        o, l = ctx.tree_attention(some, rows(3, 0, 4, D), rows(3, 0, 2, D), rows(3, 0, 2, D), mask, i32(3), with_lse=True)
+        assert o.shape == (3, 0, 4, D) and l.shape == (3, 0, 4)
+    assert ctx.launch_count() == before and ctx.get_status() == 0
+    with pytest.raises(ngs.SpecError):  # sizes are looked at all the same
+        ctx.tree_attention(some, rows(3, 0, 3, D), rows(3, 0, 2, D), rows(3, 0, 2, D), mask, i32(3))
+    with pytest.raises(ngs.SpecError):
+        ctx.score_tokens(rows(0, 64), i32(0), n_alt=33)
