@@ -312,7 +312,9 @@ int score_tokens(spec_ctx* ctx, const void* d_hidden, int M, const int32_t* d_to
  * element (1-4-3 bits, bias 7, no infinities) and one scale per vector of head_dim elements, a power of two kept as
  * its exponent + 127: the smallest with max |x| <= 448 * scale, exponent in [-120, 7]; code = E4M3 nearest to
  * x / scale, ties to the even code.  Larger magnitudes and infinities are held as 448 * 2^7; a vector with a NaN has
- * scale byte 255 and reads as NaN.
+ * scale byte 255 and reads as NaN, as it does with any scale byte above 134.  The codes 0x7F and 0xFF, E4M3's own NaN, are
+ * written in such vectors only, and a caller's own writer has to do the same: under another scale byte spec_cache_read
+ * gives NaN for them, but spec_tree_attention, which does not look at single codes, 480 * scale with the code's sign.
  *
  * Limits: head_dim 64 or 128; page 16, 32, 64 or 128; n_pages * heads * page < 2^31; max_pages * page <= 2^30; S <= 65535;
  * N <= 4096, Hq <= 4096, N * Hq / heads <= 2^22 (a call of no sequences, nodes or tokens does nothing); all pointers to elements and scales 16-byte aligned.  Strides count

@@ -183,7 +183,8 @@ class KVCache:
     """A paged key/value cache in the caller's tensors (see ``spec_kv_cache`` in the header).
 
     ``k``, ``v`` are ``[n_pages, heads, page, head_dim]``, bfloat16 or uint8 (E4M3 codes); ``table[S, max_pages]`` int32
-    holds each sequence's pages; an E4M3 cache has ``k_exp``, ``v_exp`` ``[n_pages, heads, page]`` uint8.
+    holds each sequence's pages; an E4M3 cache has ``k_exp``, ``v_exp`` ``[n_pages, heads, page]`` uint8.  A program that writes
+    codes itself marks a vector with a NaN by scale byte 255: attention does not look for E4M3's own NaN codes.
     """
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k_exp: torch.Tensor | None = None, v_exp: torch.Tensor | None = None):

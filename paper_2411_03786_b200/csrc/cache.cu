@@ -291,9 +291,9 @@ __global__ void __launch_bounds__(CACHE_THREADS, 4) cache_write_kernel(CacheArgs
     }
 }
 
-// 8 E4M3 codes times a power of two, as bfloat16 (exact).
+// 8 E4M3 codes times a power of two, as bfloat16 (exact).  Scales beyond the format's largest read as NaN.
 __device__ __forceinline__ uint4 dequantise8(uint2 codes, uint8_t scale) {
-    const float f = scale == 255 ? __uint_as_float(0x7FC00000u) : ldexpf(1.0f, (int)scale - 127);
+    const float f = (int)scale > 127 + E8_MAX ? __uint_as_float(0x7FC00000u) : ldexpf(1.0f, (int)scale - 127);
     const uint32_t w[4] = {codes.x & 0xFFFFu, codes.x >> 16, codes.y & 0xFFFFu, codes.y >> 16};
     uint32_t r[4];
 #pragma unroll

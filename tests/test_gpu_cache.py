@@ -240,3 +240,34 @@ def test_refusals(ctx):
         with pytest.raises((ngs.SpecError, IndexError)):
             f()
     assert ctx.get_status() == 0
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_and_cache_read_hold_the_same(ctx, D):
+    """One key to a sequence: attention gives its value vector as it is.  All finite codes, all scale bytes of the format
+    down to 2^-100 (below, products of the smallest codes are not numbers that fp32 holds in full), and those beyond it."""
+    import paper_2411_03786_b200 as ngs
+    finite = torch.tensor([b for b in range(256) if b & 127 != 127], dtype=torch.uint8)
+    per = -(-finite.numel() // D)
+    rows = torch.cat([finite, finite[: per * D - finite.numel()]]).view(per, D)
+    scales = list(range(27, 135)) + [135, 200, 254, 255]
+    S = per * len(scales)
+    codes = rows.repeat(len(scales), 1)
+    exp = torch.tensor(scales, dtype=torch.uint8).repeat_interleave(per)
+    cache = ngs.KVCache.empty(S, 1, 16, D, torch.arange(S, dtype=torch.int32, device="cuda").view(S, 1), True)
+    cache.k.zero_(), cache.k_exp.fill_(127), cache.v.fill_(255), cache.v_exp.fill_(255)
+    cache.v[:, 0, 0], cache.v_exp[:, 0, 0] = codes.cuda(), exp.cuda()
+    zero, one = torch.zeros(S, dtype=torch.int32).cuda(), torch.ones(S, dtype=torch.int32).cuda()
+    read = ctx.cache_read(cache, zero, 1)[1][:, 0, 0]
+    want = au.dequantise(codes, exp)
+    want[exp > 134] = math.nan
+    q, kv = torch.ones(S, 1, 2, D).bfloat16().cuda(), torch.ones(S, 1, 1, D).bfloat16().cuda()
+    seen = ctx.tree_attention(cache, q, kv, kv, torch.zeros(S, 1, 1, dtype=torch.int32).cuda(), one)[0][:, 0]
+    for got in (read, seen[:, 0], seen[:, 1]):
+        got = got.double().cpu()
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(nan=0.0), want.nan_to_num(nan=0.0))
+    # and as keys: a vector that is NaN is NaN to every row
+    cache.k_exp.fill_(127), cache.v.zero_(), cache.v_exp.fill_(127)
+    cache.k_exp[:, 0, 0] = exp.cuda()
+    lse = ctx.tree_attention(cache, q, kv, kv, torch.zeros(S, 1, 1, dtype=torch.int32).cuda(), one, with_lse=True)[1]
+    assert torch.equal(lse.isnan().all(-1).flatten().cpu(), exp > 134) and ctx.get_status() == 0
