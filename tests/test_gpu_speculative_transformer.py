@@ -61,3 +61,26 @@ def test_blocks_of_one_token_agree_with_rows(example):
         # normalised activations (of size 1): bfloat16 in two orders of summation
         assert (hidden[:, 0].float() - whole[:, i].float()).abs().max() < 0.1
     assert ctx.get_status() == 0
+
+
+@pytest.mark.parametrize("quantised", [False, True])
+def test_drafts_are_accepted(example, quantised):
+    """A model that says what follows each token (its head is its next token's embedding) on a text that goes round in
+    circles: drafts from the history are accepted, and several nodes of a row are committed at once."""
+    import paper_2411_03786_b200 as ngs
+    torch.manual_seed(3)
+    model = example.Model(V=500, seed=5)
+    for w in model.layers:  # the residual stream is the last token's embedding alone
+        w["out"].zero_(), w["down"].zero_()
+    after = (torch.arange(model.V) * 7 + 3) % 12  # every token leads into a circle within the first 12
+    model.unembed.zero_()
+    for a in range(12):
+        model.unembed[after[a]] += model.embed[a]
+    prompt = torch.arange(36, device="cuda").int().view(1, 36) % 12
+    model.ctx.close()
+    model.ctx = ngs.SpecContext(model.embed, model.unembed)
+    hist, lens, logp, rate = example.decode(model, prompt.expand(2, 36).contiguous(), 20, quantised=quantised)
+    assert rate > 2.0
+    for s in range(2):
+        text = hist[s, : int(lens[s])].tolist()
+        assert all(text[i + 1] == int(after[text[i]]) for i in range(36, len(text) - 1))
