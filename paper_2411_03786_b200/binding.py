@@ -134,12 +134,19 @@ def _rows(t: torch.Tensor, name: str):
     """Pointer, token stride and head stride of ``t[..., heads, D]`` (see _strides)."""
     if not t.is_cuda or t.dtype is not torch.bfloat16:
         raise SpecError(f"{name}: expected a bfloat16 CUDA tensor")
+    st = t.stride()  # (the two usual forms without a call)
+    if len(st) == 4 and st[3] == 1 and st[0] == st[1] * t.shape[1]:
+        return t.data_ptr(), st[1], st[2]
+    if len(st) == 3 and st[2] == 1:
+        return t.data_ptr(), st[0], st[1]
     return t.data_ptr(), *_strides(t, name)
 
 
 def _strides(t: torch.Tensor, name: str):
     """Token and head stride of ``t[..., heads, D]`` whose head vectors are contiguous and whose tokens are all one stride
     apart.  The stride of a dimension of one means nothing: with one node to a sequence the sequences are the tokens."""
+    if t.dim() < 3:
+        raise SpecError(f"{name}: expected [..., heads, head_dim]")
     *lead, head, one = t.stride()
     if one != 1:
         raise SpecError(f"{name}: head vectors must be contiguous")
@@ -495,10 +502,14 @@ class SpecContext:
             if not n_alt:
                 out = (out[0], out[1], None, None)
         if work is None:
-            work = hidden.new_empty(max(16, self._lib.spec_score_bytes(self._h, M, n_alt)), dtype=torch.uint8)
+            need = max(16, self._lib.spec_score_bytes(self._h, M, n_alt))
+            work = hidden.new_empty(need, dtype=torch.uint8)
+            scratch = work.data_ptr(), need
+        else:
+            scratch = _scratch(work, "score_tokens")
         ptr = lambda y: None if y is None else y.data_ptr()
         self._check(self._lib.score_tokens(self._h, hidden.data_ptr(), M, _i32(tokens, "tokens", (M,)), n_alt, ptr(out[0]), ptr(out[1]), ptr(out[2]),
-                                           ptr(out[3]), *_scratch(work, "score_tokens"), self._raw_stream()), "score_tokens")
+                                           ptr(out[3]), *scratch, self._raw_stream()), "score_tokens")
         return out
 
     def rope_rows(self, rope: Rope, q: torch.Tensor, k: torch.Tensor | None, pos: torch.Tensor, out=None):
@@ -507,7 +518,6 @@ class SpecContext:
         Returns contiguous ``(q_out, k_out)``, or writes to ``out``, whose tensors may be ``q`` and ``k`` themselves.
         """
         shape = q.shape
-        _need(len(shape) > 2, "rope_rows: q must be [T, Hq, D] or [S, N, Hq, D]")
         _need(k is None or (k.shape[-1] == shape[-1] and k.shape[:-2] == shape[:-2]), "rope_rows: q and k must have the same tokens and head size")
         if out is None:
             out = (_new(q), None if k is None else _new(k))
@@ -581,11 +591,15 @@ class SpecContext:
                 need = self._lib.spec_tree_attention_bytes(self._h, cache._ref, S, N, Hq)
                 if need:  # (0: something else is refused, which is not a property of the sizes)
                     self._work_bytes[key] = need
-            work = q.new_empty(max(need, 16), dtype=torch.uint8)
+            need = max(need, 16)
+            work = q.new_empty(need, dtype=torch.uint8)
+            scratch = work.data_ptr(), need
+        else:
+            scratch = _scratch(work, "tree_attention")
         self._check(self._lib.spec_tree_attention(self._h, cache._ref, *_rows(q, "q"), *_rows(k, "k"), *_rows(v, "v"), S, N, Hq,
                                                   _i32(mask, "mask", (S, N, (N + 31) // 32)), _i32(lens, "lens", (S,)),
                                                   _i32(n_nodes, "n_nodes", (S,)), D ** -0.5 if scale is None else scale,
-                                                  out[0].data_ptr(), None if out[1] is None else out[1].data_ptr(), *_scratch(work, "tree_attention"),
+                                                  out[0].data_ptr(), None if out[1] is None else out[1].data_ptr(), *scratch,
                                                   self._raw_stream()), "spec_tree_attention")
         return out
 
