@@ -386,7 +386,8 @@ int spec_tree_mask(spec_ctx* ctx, const int32_t* d_parent, int S, int N, const i
  *   d_out [S, N, Hq, head_dim] bfloat16, d_lse [S, N, Hq] float32 or NULL, contiguous.
  *   d_work: spec_tree_attention_bytes() of scratch, 16-byte aligned, for this call alone; needs no initial value.
  * Products are bf16 x bf16 with fp32 accumulation; statistics are fp32; the weights exp(s - max) are rounded to
- * bfloat16 for their product with the values.  Results do not depend on the order in which blocks of work finish.
+ * bfloat16 for their product with the values.  Results do not depend on the order in which blocks of work finish.  Outputs
+ * and scratch may not overlap what the call reads.
  */
 size_t spec_tree_attention_bytes(spec_ctx* ctx, const spec_kv_cache* cache, int S, int N, int Hq);
 int spec_tree_attention(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_q, long long q_tok, long long q_head, const void* d_k,

@@ -1,16 +1,19 @@
 // What surrounds the attention of a verification call: rotary positions of the block's queries and keys, the paged
 // key/value cache (bfloat16, or E4M3 codes with a power-of-two scale per vector) and the bit masks of draft trees.
 //
-// All four kernels move each byte once and compute next to nothing on it, so HBM (or, for a decode step's few
-// tokens, the launch) bounds them; a thread handles 16 bytes of a head at a time.
+// All four kernels move each byte once and compute little on it; a thread handles 16 bytes of a head at a time.  A prompt
+// is bound by its bytes, a decode step's few tokens by the launch, rotary rows of few heads by what is done once per token,
+// and a mask by the walk to the root, a step of which waits for the one before.
 //
 //   rotary positions        y0 = (x0 cos a - x1 sin a) f, y1 = (x0 sin a + x1 cos a) f, a = pos * freq, in fp32, rounded once
 //   E4M3 vector             scale = the smallest 2^e with max |x| <= 448 * 2^e, code = E4M3 nearest to x / scale
 //
 // On a B200 (copies 6.5 TB/s), 8 prompts of 4001 tokens, 8 heads of 128, keys rotated on the way: written to an E4M3 cache
-// in 58 us (197 MB, 3.4 TB/s: the sine and cosine of each token and the conversions share the time with the loads), read
-// back in 40 us (197 MB, 4.9 TB/s).  Rotation of 32001 tokens, 32 + 8 heads of 128, half of each: 123 us (656 MB, 5.3 TB/s).
-// A decode step's 48 tokens: 4 us, the launch.
+// in 57 us (197 MB, 3.5 TB/s; 44 without rotation, and 44 rotated into a bfloat16 cache: only the sine and cosine of each
+// token and the conversions together are more than the loads hide), read back in 44 us (197 MB, 4.5 TB/s).  Rotation of 32001 tokens,
+// 32 + 8 heads of 128, half of each: 122 us (656 MB, 5.4 TB/s); of 32000 tokens with 3 + 1 heads of 64 or 1 + 1 of 128: 34 us
+// (33 MB, 1 TB/s: a CTA of one or two warps for each token's table).  A decode step's 48 tokens: 2 to 4 us, the launch.  Masks of 64 x 144
+// nodes: 10 us; of one chain of 4096: 242 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -165,16 +168,17 @@ __device__ __forceinline__ long long cache_slot(const CacheArgs& c, int s, int p
     return (((long long)page * c.heads) << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
 }
 
+// The largest magnitude of 8 bfloat16, as its bits: they order like the magnitudes, NaN above all.
+__device__ __forceinline__ uint32_t top16(const uint4& v) {
+    const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+    return max(m & 0xFFFFu, m >> 16);
+}
+
 // Quantises a vector that LANES neighbouring lanes hold 8 elements each of.  The scale is the smallest power of two
 // that brings the largest magnitude to at most 448: E4M3 keeps three mantissa bits at every exponent, so a power of
 // two loses nothing against a finer scale, dividing by it rounds nothing, and a reader gets code * scale exactly in
 // bfloat16.  Its exponent stays in [-120, 7]: magnitudes above 448 * 2^7 (infinities too) are held as that.  A vector
 // with a NaN is held as the scale byte 255 and reads as NaN throughout.
-// magnitudes of bfloat16 order like their bits, NaN above all
-__device__ __forceinline__ uint32_t top16(const uint4& v) {
-    const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
-    return max(m & 0xFFFFu, m >> 16);
-}
 __device__ __forceinline__ uint2 quantise_to(const uint4& v, uint32_t top, uint32_t& scale) {
     int e = (int)(top >> 7) - 127 - 8 + ((top & 0x7Fu) > 0x60u ? 1 : 0);  // 448 = 1.75 * 2^8
     e = top == 0u ? 0 : min(max(e, E8_MIN), E8_MAX);

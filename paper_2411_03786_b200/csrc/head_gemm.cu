@@ -1196,7 +1196,6 @@ constexpr int SCORE_MAX_CHUNKS = 160;  // partial results per row: 32 entries of
 
 static Shape score_shape(spec_ctx* ctx, int M) { return cached_shape(ctx, M, SCORE_MAX_CHUNKS, false, false); }
 
-
 size_t score_bytes(spec_ctx* ctx, int M, int n_alt) {
     const Shape sh = score_shape(ctx, M);
     return (size_t)sh.n_chunks * M * (sizeof(float4) + (size_t)n_alt * 8);
@@ -1204,7 +1203,7 @@ size_t score_bytes(spec_ctx* ctx, int M, int n_alt) {
 
 // One CTA per row joins the row's partial results: warp 1 the statistics, relative to the common maximum; all threads
 // bring the chunks' sorted lists into shared memory, and warp 0 takes the largest of their heads n_alt times (a lane looks
-// after chunks lane, lane + 32, ...).  9 us after the contraction of 48 rows (125 chunks, 5 alternatives; the launch, and
+// after chunks lane, lane + 32, ...).  9 us after the contraction of 48 rows (148 chunks, 5 alternatives; the launch, and
 // a chain of one round per alternative), 1 % of a call with 2816 rows.
 constexpr int MERGE_THREADS = 128, MERGE_LISTS = SCORE_MAX_CHUNKS / 32;
 __global__ void __launch_bounds__(MERGE_THREADS) merge_score_kernel(const float4* stat, const float* val, const int32_t* idx, int n_chunks, int M,

@@ -29,13 +29,17 @@
 // range and tells the others; 27 writes the rows of nodes that are not live.
 //
 // What bounds it, on a B200 (copies 6.5 TB/s, products 1650 TFLOP/s in a burst, 1400 under the power cap):
-//   few rows, bfloat16 cache    the bytes: 64 sequences of one token, 32 / 8 heads of 128, 2048 keys: 99 us, 5.4 TB/s
-//   few rows, E4M3 cache        the integer pipe, which converts (1500 cycles per 128 vectors of 128): 16 x 8192 keys,
-//                               105 us, 2.6 TB/s of codes
+//   few rows, bfloat16 cache    the bytes: 64 sequences of one token, 32 / 8 heads of 128, 2048 keys: 99-102 us, 5.3 TB/s
+//   few rows, E4M3 cache        the loader warps, which are at one tile together: wait, loads, conversion, stores, fence, 1500
+//                               cycles for 128 vectors of 128, of which integer instructions alone would take 430 (but 11
+//                               more of them for 16 codes made 102 us 123): 16 x 8192 keys, 102 us, 2.6 TB/s of codes, no
+//                               faster than a bfloat16 cache (92 us) yet
 //   many rows, long contexts    a stream's chain scores -> weights -> outputs, of which two overlap (a key tile per 4100
-//                               cycles), and the power cap: 4 x 704 nodes, 16384 keys, 700-820 us, 0.92-1.07 PFLOP/s
+//                               cycles), and the power cap: 4 x 704 nodes, 16384 keys, 690-820 us, 0.92-1.09 PFLOP/s
+//   prompts                     the same, with masks in every tile of the block: a chain of 4096 nodes, 32 / 8 heads, 508 us,
+//                               0.27 PFLOP/s of what is visible; 32 / 32 heads, 618 us (hidden tiles are not left out there)
 //   short contexts              a segment's beginning and end, 6-10 us where a tile takes 2: 64 x 144 nodes, 2048 keys,
-//                               bfloat16 470 us, E4M3 560 us
+//                               bfloat16 470 us, E4M3 550-575 us
 //   one short call              two launches and a segment: 10-15 us
 #include <cuda_bf16.h>
 #include <math.h>
