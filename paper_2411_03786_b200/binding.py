@@ -485,7 +485,8 @@ class SpecContext:
     def score_tokens(self, hidden: torch.Tensor, tokens: torch.Tensor, n_alt: int = 0, out=None, work: torch.Tensor | None = None):
         """Log probability of ``tokens[M]`` after ``hidden[M, d]``, entropy, and the ``n_alt`` likeliest tokens.
 
-        Returns ``(logp[M], entropy[M], alt_ids[M, n_alt] or None, alt_logp[M, n_alt] or None)``.
+        Returns ``(logp[M], entropy[M], alt_ids[M, n_alt] or None, alt_logp[M, n_alt] or None)``; an alternative that does not
+        exist (logits of NaN or -inf are none) has id -1 and -inf.
         """
         M = hidden.shape[0]
         _need(hidden.dim() == 2 and hidden.shape[1] == self.d and hidden.dtype == torch.bfloat16 and hidden.is_cuda and hidden.is_contiguous(),
