@@ -66,7 +66,7 @@ enum {
     SPEC_STATUS_INDEX = 16       /* a context index could not take a window: that sequence is drafted by scanning until the index is rebuilt */
 };
 
-enum { SPEC_F32 = 0, SPEC_BF16 = 1, SPEC_E4M3 = 2 };
+enum { SPEC_F32 = 0, SPEC_BF16 = 1, SPEC_E4M3 = 2, SPEC_E2M1 = 3 };
 enum { SPEC_FLAG_DEDUP = 1, SPEC_FLAG_MODEL_FILL = 2, SPEC_FLAG_KEY_NEXT_TOKEN = 4, SPEC_FLAG_PARTIAL_TAIL = 8 };
 /* OR into the draft flags to reserve n (0..255) of the B draft rows for the model strategy */
 #define SPEC_FLAG_RESERVE(n) (((n) & 0xFF) << 8)
@@ -316,6 +316,13 @@ int score_tokens(spec_ctx* ctx, const void* d_hidden, int M, const int32_t* d_to
  * written in such vectors only, and a caller's own writer has to do the same: under another scale byte spec_cache_read
  * gives NaN for them, but spec_tree_attention, which does not look at single codes, 480 * scale with the code's sign.
  *
+ * SPEC_E2M1 stores four bits per element (sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), element 2i
+ * in the low half of byte i and 2i+1 in the high one, and a scale byte for each 16 consecutive elements: the upper byte of a
+ * half-precision number without its sign, that is five exponent bits and three mantissa bits, scale = half(byte << 7).  It is the
+ * smallest with max |x| <= 6 * scale, at most 10240 (byte 226); the code is the E2M1 nearest to x / scale, ties to the even code
+ * (a zero may have either sign).  Larger magnitudes and infinities are held as 61440; 16 elements with a NaN have scale byte 255, and
+ * any scale byte above 226 reads as NaN.  code * scale is exact in bfloat16 and in half precision.
+ *
  * Limits: head_dim 64 or 128; page 16, 32, 64 or 128; n_pages * heads * page < 2^31; max_pages * page <= 2^30; S <= 65535;
  * N <= 4096, Hq <= 4096, N * Hq / heads <= 2^22 (a call of no sequences, nodes or tokens does nothing); all pointers to elements and scales 16-byte aligned.  Strides count
  * elements, are multiples of 8, and head vectors are contiguous; node i of sequence s is token s*N + i.  A length or
@@ -323,12 +330,13 @@ int score_tokens(spec_ctx* ctx, const void* d_hidden, int M, const int32_t* d_to
  * SPEC_STATUS_CAPACITY: such a position is skipped, such a length leaves the sequence's outputs as for an empty row.
  */
 typedef struct spec_kv_cache {
-    void* d_k;              /* [n_pages, heads, page, head_dim] */
+    void* d_k;              /* [n_pages, heads, page, head_dim], SPEC_E2M1: head_dim / 2 bytes of two codes */
     void* d_v;
-    uint8_t* d_k_exp;       /* SPEC_E4M3: [n_pages, heads, page] scale exponent + 127; else NULL */
+    uint8_t* d_k_exp;       /* SPEC_E4M3: [n_pages, heads, page] scale exponent + 127; SPEC_E2M1: [n_pages, heads, page, head_dim / 16] scale
+                               bytes; else NULL */
     uint8_t* d_v_exp;
     const int32_t* d_table; /* [S, max_pages] page numbers */
-    int dtype;              /* SPEC_BF16 or SPEC_E4M3 */
+    int dtype;              /* SPEC_BF16, SPEC_E4M3 or SPEC_E2M1 */
     int n_pages, max_pages, page, heads, head_dim;
 } spec_kv_cache;
 

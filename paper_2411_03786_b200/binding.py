@@ -11,7 +11,7 @@ from .build import LIB, build_library
 
 FLAG_DEDUP, FLAG_MODEL_FILL, FLAG_KEY_NEXT_TOKEN, FLAG_PARTIAL_TAIL = 1, 2, 4, 8
 STATUS_TOKEN_RANGE, STATUS_CAPACITY, STATUS_TIMEOUT, STATUS_GROUPS, STATUS_INDEX = 1, 2, 4, 8, 16
-SPEC_F32, SPEC_BF16, SPEC_E4M3 = 0, 1, 2
+SPEC_F32, SPEC_BF16, SPEC_E4M3, SPEC_E2M1 = 0, 1, 2, 3
 
 _HEADER = os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "include", "ngram_spec.h")
 _lib = None
@@ -192,31 +192,51 @@ class KVCache:
     ``k``, ``v`` are ``[n_pages, heads, page, head_dim]``, bfloat16 or uint8 (E4M3 codes); ``table[S, max_pages]`` int32
     holds each sequence's pages; an E4M3 cache has ``k_exp``, ``v_exp`` ``[n_pages, heads, page]`` uint8.  A program that writes
     codes itself marks a vector with a NaN by scale byte 255: attention does not look for E4M3's own NaN codes.
+
+    A cache of 4 bits has ``k_scale``, ``v_scale`` ``[n_pages, heads, page, head_dim / 16]`` uint8 instead, and ``k``, ``v``
+    are uint8 ``[n_pages, heads, page, head_dim / 2]``: two E2M1 codes to a byte, the even element in the low half.
     """
 
-    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k_exp: torch.Tensor | None = None, v_exp: torch.Tensor | None = None):
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k_exp: torch.Tensor | None = None, v_exp: torch.Tensor | None = None,
+                 *, k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None):
         _need(k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.dtype in (torch.bfloat16, torch.uint8),
               "KVCache: k and v must be [n_pages, heads, page, head_dim], both bfloat16 or both uint8")
-        _need((k.dtype == torch.uint8) == (k_exp is not None) == (v_exp is not None), "KVCache: k_exp and v_exp belong to uint8 codes")
+        four = k_scale is not None
+        _need(four == (v_scale is not None) and not (four and (k_exp is not None or v_exp is not None)), "KVCache: k_scale and v_scale belong together, without k_exp and v_exp")
+        codes = four or k_exp is not None
+        _need((k.dtype == torch.uint8) == codes and (four or codes == (v_exp is not None)), "KVCache: k_exp and v_exp, or k_scale and v_scale, belong to uint8 codes")
         _need(table.dim() == 2 and table.dtype == torch.int32, "KVCache: table must be int32 [S, max_pages]")
         for t in (k_exp, v_exp):
             _need(t is None or (t.dtype == torch.uint8 and t.shape == k.shape[:3]), "KVCache: scales must be uint8 [n_pages, heads, page]")
-        for t in (k, v, table, k_exp, v_exp):
-            _need(t is None or (t.is_cuda and t.is_contiguous()), "KVCache: tensors must be contiguous CUDA tensors")
-        self.k, self.v, self.table, self.k_exp, self.v_exp = k, v, table, k_exp, v_exp
+        for t in (k_scale, v_scale):
+            _need(t is None or (t.dtype == torch.uint8 and t.dim() == 4 and t.shape[:3] == k.shape[:3] and 8 * t.shape[3] == k.shape[3]),
+                  "KVCache: scales must be uint8 [n_pages, heads, page, head_dim / 16]")
+        for t in (k, v, table, k_exp, v_exp, k_scale, v_scale):
+            _need(t is None or (t.is_cuda and t.is_contiguous() and t.device == k.device), "KVCache: tensors must be contiguous CUDA tensors of one device")
+        self.k, self.v, self.table, self.k_exp, self.v_exp, self.k_scale, self.v_scale = k, v, table, k_exp, v_exp, k_scale, v_scale
         self.n_pages, self.heads, self.page, self.head_dim = (int(x) for x in k.shape)
+        if four:
+            self.head_dim *= 2
         self.sequences = int(table.shape[0])
         ptr = lambda t: None if t is None else t.data_ptr()
-        self._struct = _KVCacheStruct(ptr(k), ptr(v), ptr(k_exp), ptr(v_exp), ptr(table), SPEC_BF16 if k.dtype == torch.bfloat16 else SPEC_E4M3,
+        self._struct = _KVCacheStruct(ptr(k), ptr(v), ptr(k_scale if four else k_exp), ptr(v_scale if four else v_exp), ptr(table),
+                                      SPEC_E2M1 if four else (SPEC_E4M3 if codes else SPEC_BF16),
                                       self.n_pages, int(table.shape[1]), self.page, self.heads, self.head_dim)
         self._ref = C.byref(self._struct)
 
     @classmethod
-    def empty(cls, n_pages: int, heads: int, page: int, head_dim: int, table: torch.Tensor, quantised: bool = False) -> "KVCache":
-        shape = (n_pages, heads, page, head_dim)
-        k, v = (torch.empty(shape, dtype=torch.uint8 if quantised else torch.bfloat16, device=table.device) for _ in range(2))
-        ke, ve = (torch.empty(shape[:3], dtype=torch.uint8, device=table.device) if quantised else None for _ in range(2))
-        return cls(k, v, table, ke, ve)
+    def empty(cls, n_pages: int, heads: int, page: int, head_dim: int, table: torch.Tensor, quantised: bool = False, bits: int | None = None) -> "KVCache":
+        """``bits``: 16 (bfloat16), 8 (E4M3) or 4 (E2M1); ``quantised`` is the older way to ask for 8."""
+        bits = (8 if quantised else 16) if bits is None else bits
+        _need(bits in (4, 8, 16), "KVCache.empty: bits must be 4, 8 or 16")
+        _need(bits != 4 or head_dim % 16 == 0, "KVCache.empty: head_dim must be a multiple of 16")
+        new = lambda *shape, dtype=torch.uint8: torch.empty(shape, dtype=dtype, device=table.device)
+        shape = (n_pages, heads, page)
+        if bits == 4:
+            return cls(new(*shape, head_dim // 2), new(*shape, head_dim // 2), table, k_scale=new(*shape, head_dim // 16), v_scale=new(*shape, head_dim // 16))
+        if bits == 8:
+            return cls(new(*shape, head_dim), new(*shape, head_dim), table, new(*shape), new(*shape))
+        return cls(new(*shape, head_dim, dtype=torch.bfloat16), new(*shape, head_dim, dtype=torch.bfloat16), table)
 
 
 class Rope:

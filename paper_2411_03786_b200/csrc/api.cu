@@ -510,9 +510,10 @@ int score_tokens(spec_ctx* ctx, const void* d_hidden, int M, const int32_t* d_to
 static int check_cache(spec_ctx* ctx, const spec_kv_cache* c, int S, const char* who, CacheArgs* out) {
     if (!c || !c->d_k || !c->d_v || (S > 0 && !c->d_table)) return fail(ctx, SPEC_ERR_ARG, "%s: NULL cache pointer", who);
     if (!aligned16(c->d_k) || !aligned16(c->d_v)) return fail(ctx, SPEC_ERR_ARG, "%s: cache pointers must be 16-byte aligned", who);
-    if (c->dtype != SPEC_BF16 && c->dtype != SPEC_E4M3) return fail(ctx, SPEC_ERR_ARG, "%s: cache dtype must be SPEC_BF16 or SPEC_E4M3", who);
-    if (c->dtype == SPEC_E4M3 && (!c->d_k_exp || !c->d_v_exp || !aligned16(c->d_k_exp) || !aligned16(c->d_v_exp)))
-        return fail(ctx, SPEC_ERR_ARG, "%s: an E4M3 cache needs its scales, 16-byte aligned", who);
+    if (c->dtype != SPEC_BF16 && c->dtype != SPEC_E4M3 && c->dtype != SPEC_E2M1)
+        return fail(ctx, SPEC_ERR_ARG, "%s: cache dtype must be SPEC_BF16, SPEC_E4M3 or SPEC_E2M1", who);
+    if (c->dtype != SPEC_BF16 && (!c->d_k_exp || !c->d_v_exp || !aligned16(c->d_k_exp) || !aligned16(c->d_v_exp)))
+        return fail(ctx, SPEC_ERR_ARG, "%s: an E4M3 or E2M1 cache needs its scales, 16-byte aligned", who);
     if (c->head_dim != 64 && c->head_dim != 128) return fail(ctx, SPEC_ERR_UNSUPPORTED, "%s: head_dim must be 64 or 128", who);
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128)
         return fail(ctx, SPEC_ERR_UNSUPPORTED, "%s: page must be 16, 32, 64 or 128 tokens", who);
@@ -521,7 +522,7 @@ static int check_cache(spec_ctx* ctx, const spec_kv_cache* c, int S, const char*
         return fail(ctx, SPEC_ERR_ARG, "%s: need heads, n_pages, max_pages >= 1, n_pages * heads * page < 2^31 and max_pages * page <= 2^30", who);
     int shift = 4;
     while ((1 << shift) < c->page) ++shift;
-    *out = CacheArgs{c->d_k, c->d_v, c->d_k_exp, c->d_v_exp, c->d_table, c->n_pages, c->max_pages, shift, c->heads, c->head_dim, c->dtype == SPEC_E4M3};
+    *out = CacheArgs{c->d_k, c->d_v, c->d_k_exp, c->d_v_exp, c->d_table, c->n_pages, c->max_pages, shift, c->heads, c->head_dim, c->dtype};
     return SPEC_OK;
 }
 static int check_rope(spec_ctx* ctx, const spec_rope* r, int head_dim, const char* who, RopeArgs* out) {

@@ -1,5 +1,6 @@
 // What surrounds the attention of a verification call: rotary positions of the block's queries and keys, the paged
-// key/value cache (bfloat16, or E4M3 codes with a power-of-two scale per vector) and the bit masks of draft trees.
+// key/value cache (bfloat16, E4M3 codes with a power-of-two scale per vector, or E2M1 codes with a scale for each 16 of
+// them) and the bit masks of draft trees.
 //
 // All four kernels move each byte once and compute little on it; a thread handles 16 bytes of a head at a time.  A prompt
 // is bound by its bytes, a decode step's few tokens by the launch, rotary rows of few heads by what is done once per token,
@@ -205,11 +206,37 @@ __device__ __forceinline__ void quantise_vectors(const uint4& k, const uint4& v,
     vq = quantise_to(v, m >> 16, vs);
 }
 
+// What a scale byte of a 4-bit cache stands for.
+__device__ __forceinline__ float scale4(uint32_t byte) { return __half2float(__ushort_as_half((unsigned short)(byte > S4_MAX ? 0x7E00u : byte << 7))); }
+
+// Quantises 16 elements, of which two neighbouring lanes hold 8 each, to E2M1; `top`: bits of the largest magnitude.  A code
+// has two significant bits, so a scale of a power of two alone would leave up to half of the range unused: this one has four.
+// max / 6, rounded towards zero all the way, gives the byte or the one below it, which 6 * scale >= max (exact in fp32) decides.  A quotient x / scale
+// is rounded to a multiple of 2^-13 on the way: x has 8 significant bits and the border between two codes times a scale 7, so that
+// they differ by 2^-10 of the quotient's unit or not at all, and the error of the reciprocal (2^-20) leaves no trace: ties are ties.
+__device__ __forceinline__ uint32_t quantise4(const uint4& v, uint32_t top, uint32_t& byte) {
+    const float a = __uint_as_float(top << 16);
+    uint32_t b = __half_as_ushort(__float2half_rd(__fmul_rd(a, 0x1.555554p-3f))) >> 7;
+    b = min(b, S4_MAX);
+    if (__half2float(__ushort_as_half((unsigned short)(b << 7))) * 6.0f < a) ++b;
+    byte = top > 0x7F80u ? 255u : min(b, S4_MAX);
+    const float inv = byte == 0u || byte == 255u ? 0.0f : 1.0f / scale4(byte);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    constexpr float C = 1536.0f;  // its neighbours are 2^-13 away
+    uint32_t r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float x = fmaf(__uint_as_float(w[j] << 16), inv, C) - C, y = fmaf(__uint_as_float(w[j] & 0xFFFF0000u), inv, C) - C;
+        asm("{\n .reg .b8 q;\n cvt.rn.satfinite.e2m1x2.f32 q, %1, %2;\n cvt.u32.u8 %0, q;\n}\n" : "=r"(r[j]) : "f"(y), "f"(x));
+    }
+    return byte == 255u ? 0u : __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
+}
+
 // A CTA writes `n_tok` tokens of one sequence, all heads of K and V: the rotation table is made once per token.  A thread
 // has CACHE_DEPTH vectors' chunks of K and V on their way before it makes its part of the table and looks up the slots.
 constexpr int CACHE_DEPTH = 4, WRITE_MAX_TOK = 32;
 enum { ROPE_NONE, ROPE_HALF, ROPE_PAIRS };
-template <int D, bool QUANT, int ROPE>
+template <int D, int DTYPE, int ROPE>
 __global__ void __launch_bounds__(CACHE_THREADS, 4) cache_write_kernel(CacheArgs c, const __nv_bfloat16* __restrict__ k, long long k_tok,
                                                                     long long k_head, const __nv_bfloat16* __restrict__ v, long long v_tok,
                                                                     long long v_head, int N, int n, int n_tok, const int32_t* __restrict__ nodes,
@@ -275,7 +302,19 @@ __global__ void __launch_bounds__(CACHE_THREADS, 4) cache_write_kernel(CacheArgs
                 if (rotated) kv[j] = rope_chunk<ROPE == ROPE_PAIRS, ROPE == ROPE_PAIRS ? 4 : 8>(kv[j], o, table + t * half, e, half);
             }
             const long long at = on ? slot + ((long long)head[j] << c.page_shift) : 0;
-            if (QUANT) {
+            if (DTYPE == SPEC_E2M1) {
+                uint32_t m = top16(kv[j]) | (top16(vv[j]) << 16), ks, vs;
+                m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                const uint32_t kq = quantise4(kv[j], m & 0xFFFFu, ks), vq = quantise4(vv[j], m >> 16, vs);
+                if (on) {
+                    *reinterpret_cast<uint32_t*>((uint8_t*)c.k + (at * D + e) / 2) = kq;
+                    *reinterpret_cast<uint32_t*>((uint8_t*)c.v + (at * D + e) / 2) = vq;
+                    if (lane % 2 == 0) {
+                        c.k_exp[(at * D + e) / GROUP] = (uint8_t)ks;
+                        c.v_exp[(at * D + e) / GROUP] = (uint8_t)vs;
+                    }
+                }
+            } else if (DTYPE == SPEC_E4M3) {
                 uint2 kq, vq;
                 uint32_t ks, vs;
                 quantise_vectors<LANES>(kv[j], vv[j], kq, vq, ks, vs);
@@ -310,7 +349,23 @@ __device__ __forceinline__ uint4 dequantise8(uint2 codes, uint8_t scale) {
     return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-template <int D, bool QUANT>
+// 8 E2M1 codes times their scale, as bfloat16 (exact).
+__device__ __forceinline__ uint4 dequantise4(uint32_t codes, uint32_t scale) {
+    const uint32_t f = (scale > S4_MAX ? 0x7E00u : scale << 7) * 0x00010001u;
+    uint32_t h[4], r[4];
+    asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
+        " cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}\n"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(codes));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 x = __half22float2(__hmul2(*reinterpret_cast<const __half2*>(&h[j]), *reinterpret_cast<const __half2*>(&f)));
+        r[j] = pack_bf16x2(x.x, x.y);
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+template <int D, int DTYPE>
 __global__ void __launch_bounds__(CACHE_THREADS) cache_read_kernel(CacheArgs c, int n, const int32_t* __restrict__ start,
                                                                    const int32_t* __restrict__ count, __nv_bfloat16* __restrict__ k_out,
                                                                    __nv_bfloat16* __restrict__ v_out, int* status) {
@@ -323,18 +378,22 @@ __global__ void __launch_bounds__(CACHE_THREADS) cache_read_kernel(CacheArgs c, 
     const long long vectors = (long long)n * c.heads;
     const int lane = threadIdx.x % LANES;
     const long long first = (long long)blockIdx.x * (CACHE_DEPTH * PASS) + threadIdx.x / LANES;
-    uint4 kv[CACHE_DEPTH], vv[CACHE_DEPTH];  // QUANT: codes in x, y and the scale byte in z
+    uint4 kv[CACHE_DEPTH], vv[CACHE_DEPTH];  // codes in x, y and the scale byte in z
 #pragma unroll
     for (int j = 0; j < CACHE_DEPTH; ++j) {
         const long long w = first + j * PASS;
         kv[j] = vv[j] = make_uint4(0, 0, 127, 0);
-        if (!QUANT) kv[j].z = vv[j].z = 0;
+        if (DTYPE != SPEC_E4M3) kv[j].z = vv[j].z = 0;
         if (w >= vectors) continue;
         const int t = (int)(w / c.heads), h = (int)(w - (long long)t * c.heads);
         const long long slot = t < n_here ? cache_slot(c, s, pos0 + t, status) : -1;
         if (slot < 0) continue;
         const long long at = slot + ((long long)h << c.page_shift);
-        if (QUANT) {
+        if (DTYPE == SPEC_E2M1) {
+            const long long i = at * D + lane * 8;
+            kv[j] = make_uint4(*reinterpret_cast<const uint32_t*>((const uint8_t*)c.k + i / 2), 0, c.k_exp[i / GROUP], 0);
+            vv[j] = make_uint4(*reinterpret_cast<const uint32_t*>((const uint8_t*)c.v + i / 2), 0, c.v_exp[i / GROUP], 0);
+        } else if (DTYPE == SPEC_E4M3) {
             const uint2 kq = *reinterpret_cast<const uint2*>((const uint8_t*)c.k + at * D + lane * 8);
             const uint2 vq = *reinterpret_cast<const uint2*>((const uint8_t*)c.v + at * D + lane * 8);
             kv[j] = make_uint4(kq.x, kq.y, c.k_exp[at], 0);
@@ -348,7 +407,10 @@ __global__ void __launch_bounds__(CACHE_THREADS) cache_read_kernel(CacheArgs c, 
     for (int j = 0; j < CACHE_DEPTH; ++j) {
         const long long w = first + j * PASS;
         if (w >= vectors) continue;
-        if (QUANT) {
+        if (DTYPE == SPEC_E2M1) {
+            kv[j] = dequantise4(kv[j].x, kv[j].z);
+            vv[j] = dequantise4(vv[j].x, vv[j].z);
+        } else if (DTYPE == SPEC_E4M3) {
             kv[j] = dequantise8(make_uint2(kv[j].x, kv[j].y), (uint8_t)kv[j].z);
             vv[j] = dequantise8(make_uint2(vv[j].x, vv[j].y), (uint8_t)vv[j].z);
         }
@@ -374,14 +436,15 @@ int launch_cache_write(spec_ctx* ctx, const CacheArgs& c, const void* d_k, long 
     };
     auto by_rope = [&](auto dim, auto quant) {
         constexpr int D = decltype(dim)::value;
-        constexpr bool Q = decltype(quant)::value;
+        constexpr int Q = decltype(quant)::value;
         return rope.rot == 0 ? go(cache_write_kernel<D, Q, ROPE_NONE>) : (rope.interleaved ? go(cache_write_kernel<D, Q, ROPE_PAIRS>) : go(cache_write_kernel<D, Q, ROPE_HALF>));
     };
-    using D64 = std::integral_constant<int, 64>;
-    using D128 = std::integral_constant<int, 128>;
-    cudaError_t e;
-    if (c.quantised) e = c.head_dim == 64 ? by_rope(D64(), std::true_type()) : by_rope(D128(), std::true_type());
-    else e = c.head_dim == 64 ? by_rope(D64(), std::false_type()) : by_rope(D128(), std::false_type());
+    auto by_dim = [&](auto dtype) {
+        return c.head_dim == 64 ? by_rope(std::integral_constant<int, 64>(), dtype) : by_rope(std::integral_constant<int, 128>(), dtype);
+    };
+    const cudaError_t e = c.dtype == SPEC_BF16   ? by_dim(std::integral_constant<int, SPEC_BF16>())
+                          : c.dtype == SPEC_E4M3 ? by_dim(std::integral_constant<int, SPEC_E4M3>())
+                                                 : by_dim(std::integral_constant<int, SPEC_E2M1>());
     ctx->launches += 1;
     return check_cuda(ctx, e, "spec_cache_write launch");
 }
@@ -394,9 +457,13 @@ int launch_cache_read(spec_ctx* ctx, const CacheArgs& c, int S, int n, const int
         return launch_pdl(kernel, grid, dim3(CACHE_THREADS), 0, st, c, n, d_start, d_count, (__nv_bfloat16*)d_k_out, (__nv_bfloat16*)d_v_out,
                           ctx->d_status);
     };
-    cudaError_t e;
-    if (c.quantised) e = c.head_dim == 64 ? go(cache_read_kernel<64, true>) : go(cache_read_kernel<128, true>);
-    else e = c.head_dim == 64 ? go(cache_read_kernel<64, false>) : go(cache_read_kernel<128, false>);
+    auto by_dim = [&](auto dtype) {
+        constexpr int Q = decltype(dtype)::value;
+        return c.head_dim == 64 ? go(cache_read_kernel<64, Q>) : go(cache_read_kernel<128, Q>);
+    };
+    const cudaError_t e = c.dtype == SPEC_BF16   ? by_dim(std::integral_constant<int, SPEC_BF16>())
+                          : c.dtype == SPEC_E4M3 ? by_dim(std::integral_constant<int, SPEC_E4M3>())
+                                                 : by_dim(std::integral_constant<int, SPEC_E2M1>());
     ctx->launches += 1;
     return check_cuda(ctx, e, "spec_cache_read launch");
 }

@@ -6,12 +6,14 @@ namespace ngs {
 
 constexpr int E8_MIN = -120, E8_MAX = 7;  // exponents of a vector's scale
 constexpr int kMaxNodes = 4096;           // nodes of a sequence's draft block
+constexpr int GROUP = 16;                 // elements that share a scale in a 4-bit cache
+constexpr uint32_t S4_MAX = 226;          // the largest scale byte of a 4-bit cache, 10240
 
 struct CacheArgs {
-    void *k, *v;             // [n_pages, heads, page, D] bf16 or E4M3 codes
-    uint8_t *k_exp, *v_exp;  // [n_pages, heads, page] exponent + 127 of the vector's scale
+    void *k, *v;             // [n_pages, heads, page, D] bf16 or E4M3 codes, or [.., D / 2] pairs of E2M1 codes
+    uint8_t *k_exp, *v_exp;  // E4M3: [n_pages, heads, page] exponent + 127 of the vector's scale; E2M1: [.., D / GROUP] scale bytes
     const int32_t* table;    // [S, max_pages]
-    int n_pages, max_pages, page_shift, heads, head_dim, quantised;
+    int n_pages, max_pages, page_shift, heads, head_dim, dtype;
 };
 
 struct RopeArgs {

@@ -108,17 +108,19 @@ struct __align__(16) Filled {
     }
 };
 __device__ const Filled<TILE * 128, 255> nan_page;
-__device__ const Filled<TILE, 127> unit_scales;
+__device__ const Filled<TILE * 128 / GROUP, 127> unit_scales;  // (an E2M1 cache's read as 1.875)
 
-template <int D, bool Q8>
+template <int D, int DTYPE>
 struct Geometry {
+    static constexpr bool Q8 = DTYPE == SPEC_E4M3, Q4 = DTYPE == SPEC_E2M1;
     static constexpr int HALVES = D / 64;  // 128-byte swizzle rows per vector
     static constexpr int TILE_BYTES = TILE * D * 2;
-    static constexpr int SLOTS = Q8 ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 8);  // bf16 tiles in flight
-    static constexpr int STAGES = Q8 ? (D == 128 ? 4 : 6) : 0;                  // E4M3 tiles in flight
-    static constexpr int STAGE_BYTES = TILE * D;
+    static constexpr int SLOTS = Q8 || Q4 ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 8);  // bf16 tiles in flight
+    static constexpr int STAGES = Q4 ? 6 : (Q8 ? (D == 128 ? 4 : 6) : 0);             // tiles of codes in flight
+    static constexpr int CODES = Q4 ? D / 2 : D, SCALES = Q4 ? D / GROUP : 1;         // bytes of a vector
+    static constexpr int STAGE_BYTES = TILE * CODES;
     static constexpr int EXP_AT = 2 * TILE_BYTES + SLOTS * TILE_BYTES + STAGES * STAGE_BYTES;
-    static constexpr int MISC_AT = EXP_AT + STAGES * TILE;
+    static constexpr int MISC_AT = EXP_AT + STAGES * TILE * SCALES;
     static constexpr int SMEM = MISC_AT + (int)sizeof(AttShared);
     static_assert(SMEM <= ATT_SMEM, "shared memory");
 };
@@ -164,7 +166,7 @@ struct Walk {
     int s, h, t, pass, slot;
     long long pos, hi;
 };
-template <bool Q8>
+template <bool CODED>
 __device__ __forceinline__ void advance(const AttParams& p, Walk& w, Segment& g) {
     int rows = 0;
     while (w.pos < w.hi && rows <= 0) {
@@ -183,10 +185,10 @@ __device__ __forceinline__ void advance(const AttParams& p, Walk& w, Segment& g)
                 g.len = len;
                 g.live = live;
                 g.whole = g.t1 - g.t0 == n_tiles;
-                // (a last single row tile beside pairs of the same keys: an E4M3 cache's tiles are converted for it alone, and
+                // (a last single row tile beside pairs of the same keys: tiles of codes are converted for it alone, and
                 // two at a time take longer than one
                 // for both streams; 64 sequences of 144 nodes, 4 heads to a key head, 2048 keys: 657 us so, 761 us split)
-                g.split = rows <= TILE && (!Q8 || qt == 0);
+                g.split = rows <= TILE && (!CODED || qt == 0);
                 g.slot = w.slot;
                 w.slot = 1;
             }
@@ -256,6 +258,11 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
     const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 // Four E4M3 codes times a power of two as bfloat16, two to a word: a code's sign, exponent and mantissa moved into a
 // bfloat16's fields read as its value times 2^-120 (subnormals as subnormals), and `f` holds scale * 2^120.  (The integer
 // pipe is what converting is bound by: it has the shift to the right, the masks and the two joins, 6 instructions; the
@@ -271,6 +278,37 @@ __device__ __forceinline__ void e4m3x4_bf16x4(uint32_t w, uint32_t f, uint32_t& 
 __device__ __forceinline__ uint32_t scale_bf16x2(uint32_t exp) {
     return exp > 127u + E8_MAX ? 0x7FC07FC0u : (exp + 120u) * 0x00800080u;  // beyond the largest: NaN
 }
+// Eight E2M1 codes as bfloat16, elements i and i + 4 in one word: a code's three lower bits moved to the boundary of exponent
+// and mantissa read as its value times 2^-126 (0.5 as a subnormal).  `f` holds scale * 2^106: with a factor of 2^126 a scale of 4 would
+// leave bfloat16, so the tiles of a 4-bit cache hold their values times UNIT4 = 2^-20, exactly, and so do the block's beside them
+// (of which only what is below 2^-106 loses bits).  The order of elements is the one that takes no instructions (10 of the integer
+// pipe for 8 codes): queries and the block's tiles are brought into it where they are loaded, outputs back where they are stored.
+constexpr float UNIT4 = 0x1p-20f;
+__device__ __forceinline__ uint4 e2m1x8_bf16x8(uint32_t w, uint32_t f) {
+    uint32_t a, b, c, d, e;
+    asm("mul.lo.u32 %0, %1, 64;" : "=r"(a) : "r"(w));  // (shifts to the left are multiplications, which go through another pipe)
+    asm("mul.lo.u32 %0, %1, 4096;" : "=r"(b) : "r"(w));
+    asm("mul.lo.u32 %0, %1, 4;" : "=r"(c) : "r"(w));
+    asm("mul.lo.u32 %0, %1, 256;" : "=r"(d) : "r"(w));
+    asm("mul.lo.u32 %0, %1, 16;" : "=r"(e) : "r"(w));
+    constexpr uint32_t MAG = 0x01C001C0u, SIGN = 0x80008000u;
+    return make_uint4(mul_bf16x2((a & MAG) | (b & SIGN), f), mul_bf16x2((c & MAG) | (d & SIGN), f), mul_bf16x2(((w >> 2) & MAG) | (e & SIGN), f),
+                      mul_bf16x2(((w >> 6) & MAG) | (w & SIGN), f));
+}
+__device__ __forceinline__ uint32_t scale4_bf16x2(uint32_t byte) {
+    const float s = __half2float(__ushort_as_half((unsigned short)(byte > S4_MAX ? 0x7E00u : byte << 7))) * 0x1p106f;
+    return pack2(s, s);
+}
+// Eight elements in the order of e2m1x8_bf16x8, and the place that it gives to element j of a row.
+__device__ __forceinline__ uint4 in_code_order(const uint4& v) {
+    return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+}
+template <bool Q4>
+__device__ __forceinline__ constexpr int place(int j) { return Q4 ? (j & ~7) | ((j & 3) << 1) | ((j >> 2) & 1) : j; }
+__device__ __forceinline__ uint4 in_unit4(const uint4& v) {
+    constexpr uint32_t U = 0x35803580u;  // 2^-20, twice
+    return make_uint4(mul_bf16x2(v.x, U), mul_bf16x2(v.y, U), mul_bf16x2(v.z, U), mul_bf16x2(v.w, U));
+}
 __device__ __forceinline__ void st_shared16(uint32_t addr, const uint4& v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -282,11 +320,6 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
 // Where 16-byte chunk `c` of row r lies in a tile: blocks of 64 elements, rows of 128 bytes, chunks swizzled by the row.
 __device__ __forceinline__ uint32_t tile_at(int r, int c) { return (uint32_t)((c >> 3) * (TILE * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
 
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 // Weights 2^(c s - mc) of 32 scores, as bfloat16, and their sum.
 __device__ __forceinline__ float weights32(const uint32_t (&s)[32], float c, float mc, uint32_t (&w)[16]) {
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -336,11 +369,12 @@ __device__ __forceinline__ uint32_t nonfinite_to_zero(uint32_t v, bool& found) {
     return v;
 }
 
-template <int D, bool Q8>
+template <int D, int DTYPE>
 __global__ void __launch_bounds__(ATT_THREADS, 1)
 tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_bk,
                       const __grid_constant__ CUtensorMap tm_bv, const __grid_constant__ AttParams p) {
-    using Geo = Geometry<D, Q8>;
+    using Geo = Geometry<D, DTYPE>;
+    constexpr bool Q4 = Geo::Q4, CODED = Geo::Q8 || Q4;
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = smem_u32(smem);
     if (base & 1023u) {  // (never: the swizzled tiles need it)
@@ -384,7 +418,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         tmem_alloc(smem_u32(&sh.tmem), 512);
         tmem_relinquish();
     }
-    if (warp == TMA_WARP && lane < (Q8 ? 2 : 4))
+    if (warp == TMA_WARP && lane < (CODED ? 2 : 4))
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane == 0 ? &tm_k : (lane == 1 ? &tm_v : (lane == 2 ? &tm_bk : &tm_bv)))) : "memory");
     tc_fence_before();
     __syncthreads();
@@ -439,7 +473,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     if (o >= 0) v[i] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + o + c * 8);
                 }
 #pragma unroll
-                for (int i = 0; i < 16 / RPI; ++i) st_shared16(dst + tile_at(wq * 32 + half * 16 + i * RPI + lane / LPR, c), v[i]);
+                for (int i = 0; i < 16 / RPI; ++i) st_shared16(dst + tile_at(wq * 32 + half * 16 + i * RPI + lane / LPR, c), Q4 ? in_code_order(v[i]) : v[i]);
                 fence_async_smem();
             }
             __syncwarp();
@@ -577,7 +611,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             if ((!split || stream == 0) && warp_on) {
                 const int R = g.qt * 2 * TILE + tile_row, node = R / p.G, gq = R - node * p.G;
                 const bool poisoned = sh.nonfinite[n_seg & 15u] == (int)n_seg + 1;
-                const float inv = g.whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
+                constexpr float UNIT = Q4 ? 1.0f / UNIT4 : 1.0f;
+                const float inv = g.whole ? (l == 0.0f ? 0.0f : UNIT / l) : UNIT;
                 const long long out_row = ((long long)g.s * a.N + node) * a.Hq + g.h * p.G + gq;
                 const long long part = (long long)blockIdx.x * 2 + g.slot;
 #pragma unroll 1
@@ -605,21 +640,22 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
 #pragma unroll
                             for (int j = 0; j < 32; ++j) {
                                 const float y = __bfloat162float(v[j]);
-                                if (!isfinite(y)) x[j] += y;
+                                if (!isfinite(y)) x[place<Q4>(j)] += y;
                             }
                         }
                     }
+                    auto y = [&](int j) { return x[place<Q4>(j)] * inv; };
                     if (g.whole) {  // into the row's place in the query tile, which is done with
                         const uint32_t dst = q_at + stream * Geo::TILE_BYTES;
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
                             st_shared16(dst + tile_at(wq * 32 + lane, 4 * i + j),
-                                        make_uint4(pack2(x[8 * j] * inv, x[8 * j + 1] * inv), pack2(x[8 * j + 2] * inv, x[8 * j + 3] * inv),
-                                                   pack2(x[8 * j + 4] * inv, x[8 * j + 5] * inv), pack2(x[8 * j + 6] * inv, x[8 * j + 7] * inv)));
+                                        make_uint4(pack2(y(8 * j), y(8 * j + 1)), pack2(y(8 * j + 2), y(8 * j + 3)), pack2(y(8 * j + 4), y(8 * j + 5)),
+                                                   pack2(y(8 * j + 6), y(8 * j + 7))));
                     } else if (valid) {  // four columns of neighbouring rows side by side
                         float4* dst = reinterpret_cast<float4*>(p.part_o) + (part * (D / 4) + 8 * i) * p.rows_cap + tile_row;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) dst[(long long)j * p.rows_cap] = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+                        for (int j = 0; j < 8; ++j) dst[(long long)j * p.rows_cap] = make_float4(y(4 * j), y(4 * j + 1), y(4 * j + 2), y(4 * j + 3));
                     }
                 }
                 if (g.whole) {  // rows of the output from there, a 128-byte line (D = 64: half of one) by neighbouring lanes
@@ -668,40 +704,51 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     phase ^= 1u;
                 }
                 const int rows = block ? g.live - (t - g.first) * TILE : g.len - t * TILE;  // may exceed the tile
-                if (!Q8 && !(is_v && (block || rows < TILE))) return true;  // all TMA's
-                if (Q8 && !block) {
+                if (!CODED && !(is_v && (block || rows < TILE))) return true;  // all TMA's
+                if (CODED && !block) {
                     if (!wait(stg_full + 8 * stg, stg_phase)) return false;
                     if (!wait(bar_empty, my_phase ^ 1u)) return false;
-                    const uint32_t src = stg_at + stg * Geo::STAGE_BYTES, ex = exp_at + stg * TILE;
+                    const uint32_t src = stg_at + stg * Geo::STAGE_BYTES, ex = exp_at + stg * (TILE * Geo::SCALES);
                     // A thread has 16 codes of rows 32 (D = 64: 64) apart, a staging row's pieces dealt out so that the 8 lanes
                     // that load or store together meet in no bank: lanes 0-3 the front of row r, 4-7 the back of row r + 1,
                     // the next 8 the other two (the swizzle turns even pieces of one row into odd ones of the next).
                     constexpr int LPR = D / 16, PER = TILE * LPR / LOADERS, STEP = LOADERS / LPR;
                     const int r = D == 64 ? tid / LPR : (tid / 16) * 2 + (((tid >> 3) ^ (tid >> 2)) & 1), c = D == 64 ? tid % LPR : (tid & 7);
-                    const uint32_t from = src + r * D + c * 16, to = dst + tile_at(r, 2 * c);
-                    uint4 v[PER];
+                    const uint32_t from = src + r * Geo::CODES + c * (Q4 ? 8 : 16), to = dst + tile_at(r, 2 * c);
+                    uint4 v[PER];  // (E2M1: x and y)
                     uint32_t e[PER];
 #pragma unroll
                     for (int i = 0; i < PER; ++i) {
-                        v[i] = ld_shared16(from + i * STEP * D);
-                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e[i]) : "r"(ex + r + i * STEP) : "memory");
+                        if (Q4) {
+                            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v[i].x), "=r"(v[i].y) : "r"(from + i * STEP * Geo::CODES) : "memory");
+                            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e[i]) : "r"(ex + (r + i * STEP) * Geo::SCALES + c) : "memory");
+                        } else {
+                            v[i] = ld_shared16(from + i * STEP * Geo::CODES);
+                            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e[i]) : "r"(ex + r + i * STEP) : "memory");
+                        }
                     }
                     if (rows < TILE) {  // (whatever the staging tile held)
 #pragma unroll
                         for (int i = 0; i < PER; ++i)
                             if (r + i * STEP >= rows) {
                                 v[i] = make_uint4(0, 0, 0, 0);
-                                e[i] = 127;
+                                e[i] = 0;
                             }
                     }
 #pragma unroll
                     for (int i = 0; i < PER; ++i) {
-                        const uint32_t f = scale_bf16x2(e[i]);
                         uint4 lo, hi;
-                        e4m3x4_bf16x4(v[i].x, f, lo.x, lo.y);
-                        e4m3x4_bf16x4(v[i].y, f, lo.z, lo.w);
-                        e4m3x4_bf16x4(v[i].z, f, hi.x, hi.y);
-                        e4m3x4_bf16x4(v[i].w, f, hi.z, hi.w);
+                        if (Q4) {
+                            const uint32_t f = scale4_bf16x2(e[i]);
+                            lo = e2m1x8_bf16x8(v[i].x, f);
+                            hi = e2m1x8_bf16x8(v[i].y, f);
+                        } else {
+                            const uint32_t f = scale_bf16x2(e[i]);
+                            e4m3x4_bf16x4(v[i].x, f, lo.x, lo.y);
+                            e4m3x4_bf16x4(v[i].y, f, lo.z, lo.w);
+                            e4m3x4_bf16x4(v[i].z, f, hi.x, hi.y);
+                            e4m3x4_bf16x4(v[i].w, f, hi.z, hi.w);
+                        }
                         st_shared16(to + i * STEP * 128, lo);
                         st_shared16((to ^ 16u) + i * STEP * 128, hi);
                     }
@@ -711,7 +758,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                         stg_phase ^= 1u;
                     }
                 } else {
-                    if (!Q8) {
+                    if (!CODED) {
                         // TMA's as well, but what lies beyond the end must be 0 (a weight of 0 would not keep a NaN out of the
                         // products), and so must values of the block that are not finite.  (A barrier's parity tells one use
                         // of a slot from the next, not from the one after, so these threads, which skip slots, do not wait for
@@ -764,7 +811,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                                 v[i].z = nonfinite_to_zero(v[i].z, found);
                                 v[i].w = nonfinite_to_zero(v[i].w, found);
                             }
-                            st_shared16(dst + tile_at(r, c), v[i]);
+                            st_shared16(dst + tile_at(r, c), Q4 ? in_unit4(in_code_order(v[i])) : v[i]);
                         }
                     }
                     if (found) sh.nonfinite[n_seg & 15u] = (int)n_seg + 1;
@@ -783,7 +830,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             // A lane fetches one page's part of a tile.  Page numbers are read 32 at a time, a window ahead of their use (two
             // registers, by the window's parity: a load is never waited for where it is issued).
             uint32_t slot = 0, phase = 0;
-            constexpr uint32_t RING = Q8 ? Geo::STAGES : Geo::SLOTS;
+            constexpr uint32_t RING = CODED ? Geo::STAGES : Geo::SLOTS;
             const int page = 1 << cache.page_shift, per_tile = TILE >> cache.page_shift;
             const int all_rows = (cache.n_pages * cache.heads) << cache.page_shift;  // a coordinate beyond the cache: reads as 0
             for (;; ++n_seg) {
@@ -799,12 +846,12 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 const bool ok = for_each_tile(g, [&](bool is_v, int t) {
                     const bool block = t >= g.n_prefix;
                     const int rows = block ? TILE : min(g.len - t * TILE, TILE);
-                    const bool mended = !Q8 && is_v && (block || rows < TILE);  // goes through the other threads' hands
-                    const uint32_t bar_full = (Q8 ? stg_full : full) + 8 * slot, bar_empty = (Q8 ? stg_empty : empty) + 8 * slot;
-                    const uint32_t dst = Q8 ? stg_at + slot * Geo::STAGE_BYTES : ring_at + slot * Geo::TILE_BYTES;
-                    const uint32_t ex = exp_at + slot * TILE, bar_go = go + 8 * slot;
+                    const bool mended = !CODED && is_v && (block || rows < TILE);  // goes through the other threads' hands
+                    const uint32_t bar_full = (CODED ? stg_full : full) + 8 * slot, bar_empty = (CODED ? stg_empty : empty) + 8 * slot;
+                    const uint32_t dst = CODED ? stg_at + slot * Geo::STAGE_BYTES : ring_at + slot * Geo::TILE_BYTES;
+                    const uint32_t ex = exp_at + slot * (TILE * Geo::SCALES), bar_go = go + 8 * slot;
                     const uint32_t my_phase = phase;
-                    if (!Q8 || !block) {
+                    if (!CODED || !block) {
                         if (++slot == RING) {
                             slot = 0;
                             phase ^= 1u;
@@ -816,7 +863,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                         if (window & 1) even = fetch(window + 1);
                         else odd = fetch(window + 1);
                     }
-                    if (Q8 && block) return true;
+                    if (CODED && block) return true;
                     const int pages = block ? 0 : (rows + page - 1) >> cache.page_shift;
                     // A page that is not one of the pool's: its keys are made NaN, so that no weights come of the tile before
                     // the softmax warps have looked for its maximum, which is when they hide the positions of missing pages
@@ -832,8 +879,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     __syncwarp();  // (what lane 0's arrival publishes includes the line above)
                     const uint32_t bar = mended ? bar_go : bar_full;
                     if (lane == 0) {
-                        mbar_expect_tx(bar, (uint32_t)(block ? TILE : pages * page) * (Q8 ? D + 1 : 2 * D));
-                        if (!Q8 && !mended) mbar_arrive_n(bar_full, LOADERS - 1);
+                        mbar_expect_tx(bar, (uint32_t)(block ? TILE : pages * page) * (CODED ? Geo::CODES + Geo::SCALES : 2 * D));
+                        if (!CODED && !mended) mbar_arrive_n(bar_full, LOADERS - 1);
                     }
                     __syncwarp();
                     if (block) {
@@ -841,9 +888,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     } else if (lane < pages) {
                         const int row = good ? (pid * cache.heads + g.h) << cache.page_shift : all_rows;
                         const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
-                        if (Q8) {
-                            tma_load_2d(dst + lane * page * D, tm, 0, row, bar);
-                            bulk_load(ex + lane * page, good ? (is_v ? cache.v_exp : cache.k_exp) + row : (is_v ? unit_scales.byte : nan_page.byte), page, bar);
+                        if (CODED) {
+                            tma_load_2d(dst + lane * page * Geo::CODES, tm, 0, row, bar);
+                            bulk_load(ex + lane * page * Geo::SCALES, good ? (is_v ? cache.v_exp : cache.k_exp) + (long long)row * Geo::SCALES : (is_v ? unit_scales.byte : nan_page.byte),
+                                      page * Geo::SCALES, bar);
                         } else {
 #pragma unroll
                             for (int i = 0; i < Geo::HALVES; ++i) {
@@ -1015,7 +1063,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             for (uint32_t k = 0;; ++k) {
                 if (!__all_sync(0xffffffffu, wait(seg_empty + 8 * (k % SEGMENTS), ((k / SEGMENTS) & 1u) ^ 1u))) break;
                 Segment& g = sh.segment[k % SEGMENTS];
-                if (lane == 0) advance<Q8>(p, w, g);
+                if (lane == 0) advance<CODED>(p, w, g);
                 __syncwarp();
                 const int n_pre = g.n_prefix, from = max(g.t0 - n_pre, 0), to = g.t1 - n_pre;
                 if (g.more && to > 0) {
@@ -1176,15 +1224,16 @@ size_t tree_attention_bytes(int num_sms, int S, int N, int Hq, int heads, int he
     return bytes;
 }
 
-// The cache as rows of one vector: [n_pages * heads * page, D], a page and 128 bytes (E4M3: a whole vector) at a time.
+// The cache as rows of one vector: [n_pages * heads * page, D], a page and 128 bytes (codes: a whole vector) at a time.
 static int cache_map(spec_ctx* ctx, CUtensorMap* tm, const void* base, const CacheArgs& c) {
-    const int elem = c.quantised ? 1 : 2;
-    cuuint64_t dims[2] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.n_pages * c.heads << c.page_shift};
-    cuuint64_t strides[1] = {(cuuint64_t)c.head_dim * elem};
-    cuuint32_t box[2] = {(cuuint32_t)(c.quantised ? c.head_dim : 64), 1u << c.page_shift};
+    const bool coded = c.dtype != SPEC_BF16;
+    const int bytes = c.dtype == SPEC_BF16 ? 2 * c.head_dim : (c.dtype == SPEC_E4M3 ? c.head_dim : c.head_dim / 2);  // of a vector
+    cuuint64_t dims[2] = {(cuuint64_t)(coded ? bytes : c.head_dim), (cuuint64_t)c.n_pages * c.heads << c.page_shift};
+    cuuint64_t strides[1] = {(cuuint64_t)bytes};
+    cuuint32_t box[2] = {(cuuint32_t)(coded ? bytes : 64), 1u << c.page_shift};
     cuuint32_t estr[2] = {1u, 1u};
-    CUresult r = ctx->encode(tm, c.quantised ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
-                             strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, c.quantised ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+    CUresult r = ctx->encode(tm, coded ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
+                             strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, coded ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail(ctx, SPEC_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
     return SPEC_OK;
@@ -1204,9 +1253,9 @@ static int block_map(spec_ctx* ctx, CUtensorMap* tm, const void* base, long long
     return SPEC_OK;
 }
 
-template <int D, bool Q8>
+template <int D, int DTYPE>
 static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
-    auto kernel = tree_attention_kernel<D, Q8>;
+    auto kernel = tree_attention_kernel<D, DTYPE>;
     {
         static bool done[64] = {false};
         std::lock_guard<std::mutex> lock(host_mutex());
@@ -1217,7 +1266,7 @@ static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
             if (rc) return rc;
             if (attr.numRegs < LAUNCH_REGS)  // the warpgroups would wait for registers for ever
                 return fail(ctx, SPEC_ERR_UNSUPPORTED, "spec_tree_attention: built with %d registers per thread", attr.numRegs);
-            if ((rc = check_cuda(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Geometry<D, Q8>::SMEM),
+            if ((rc = check_cuda(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Geometry<D, DTYPE>::SMEM),
                                  "spec_tree_attention: cudaFuncSetAttribute")))
                 return rc;
             d = true;
@@ -1228,7 +1277,7 @@ static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
     if (rc || (rc = cache_map(ctx, &tm_v, p.a.cache.v, p.a.cache)) || (rc = block_map(ctx, &tm_bk, p.a.k, p.a.k_tok, p.a.k_head, p.a)) ||
         (rc = block_map(ctx, &tm_bv, p.a.v, p.a.v_tok, p.a.v_head, p.a)))
         return rc;
-    cudaError_t e = launch_pdl(kernel, dim3(p.n_groups * p.side), dim3(ATT_THREADS), (size_t)Geometry<D, Q8>::SMEM, st, tm_k, tm_v, tm_bk, tm_bv, p);
+    cudaError_t e = launch_pdl(kernel, dim3(p.n_groups * p.side), dim3(ATT_THREADS), (size_t)Geometry<D, DTYPE>::SMEM, st, tm_k, tm_v, tm_bk, tm_bv, p);
     if ((rc = check_cuda(ctx, e, "spec_tree_attention launch"))) return rc;
     ++ctx->launches;
     if (p.n_groups == 1) return SPEC_OK;  // nothing is spread
@@ -1247,8 +1296,13 @@ int launch_tree_attention(spec_ctx* ctx, const TreeAttnArgs& a, cudaStream_t st)
     p.part_o = reinterpret_cast<float*>((char*)a.work + (size_t)p.part_o);
     p.part_ml = reinterpret_cast<float2*>((char*)a.work + (size_t)p.part_ml);
     p.wait_limit_ns = ctx->wait_limit_ns;
-    if (a.cache.quantised) return a.cache.head_dim == 64 ? launch<64, true>(ctx, p, st) : launch<128, true>(ctx, p, st);
-    return a.cache.head_dim == 64 ? launch<64, false>(ctx, p, st) : launch<128, false>(ctx, p, st);
+    const bool small = a.cache.head_dim == 64;
+    if (a.cache.dtype == SPEC_E2M1) {
+        p.c /= UNIT4;
+        return small ? launch<64, SPEC_E2M1>(ctx, p, st) : launch<128, SPEC_E2M1>(ctx, p, st);
+    }
+    if (a.cache.dtype == SPEC_E4M3) return small ? launch<64, SPEC_E4M3>(ctx, p, st) : launch<128, SPEC_E4M3>(ctx, p, st);
+    return small ? launch<64, SPEC_BF16>(ctx, p, st) : launch<128, SPEC_BF16>(ctx, p, st);
 }
 
 }  // namespace ngs
