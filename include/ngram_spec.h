@@ -361,6 +361,16 @@ int spec_rope_rows(spec_ctx* ctx, const spec_rope* rope, const void* d_q, int Hq
                    const int32_t* d_pos, int T, void* stream);
 
 /*
+ * The same with a position on each of several axes (time, height and width of images and video, say): pair i is turned by
+ * d_pos[d_axis[i], t] * d_freq[i].  d_axis[rot / 2] holds each pair's axis, in sections, dealt out in turn or in any other order;
+ * NULL: axis 0 for all.  d_pos is [axes, T], 1 <= axes <= SPEC_MAX_AXES.  A pair whose axis is not one of them stands at position 0.
+ */
+enum { SPEC_MAX_AXES = 8 };
+int spec_rope_rows_axes(spec_ctx* ctx, const spec_rope* rope, const uint8_t* d_axis, int axes, const void* d_q, int Hq, long long q_tok,
+                        long long q_head, void* d_q_out, const void* d_k, int Hk, long long k_tok, long long k_head, void* d_k_out,
+                        int head_dim, const int32_t* d_pos, int T, void* stream);
+
+/*
  * Writes keys and values into the cache: for i < d_count[s] (NULL: n), node d_nodes[s, i] (NULL: i) of sequence s goes
  * to position d_start[s] + i.  A node outside [0, N) is skipped (the committed path of a step is padded with -1).
  * rope (or NULL): keys are rotated at the position they are written to, and rounded to bfloat16, first.
@@ -369,6 +379,14 @@ int spec_rope_rows(spec_ctx* ctx, const spec_rope* rope, const void* d_q, int Hq
 int spec_cache_write(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_k, long long k_tok, long long k_head, const void* d_v,
                      long long v_tok, long long v_head, int S, int N, int n, const int32_t* d_nodes, const int32_t* d_start,
                      const int32_t* d_count, const spec_rope* rope, void* stream);
+
+/*
+ * The same with the rotary positions of the block's nodes given, d_pos [axes, S, N], instead of where their keys are written
+ * to: behind images the two differ.  Arguments d_axis and axes as in spec_rope_rows_axes.
+ */
+int spec_cache_write_axes(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_k, long long k_tok, long long k_head, const void* d_v,
+                          long long v_tok, long long v_head, int S, int N, int n, const int32_t* d_nodes, const int32_t* d_start,
+                          const int32_t* d_count, const spec_rope* rope, const uint8_t* d_axis, int axes, const int32_t* d_pos, void* stream);
 
 /* Positions d_start[s] + i, i < d_count[s] (NULL: n), as contiguous bfloat16 [S, n, heads, head_dim] (exact); 0 beyond. */
 int spec_cache_read(spec_ctx* ctx, const spec_kv_cache* cache, int S, int n, const int32_t* d_start, const int32_t* d_count,

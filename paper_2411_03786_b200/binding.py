@@ -91,6 +91,8 @@ def load_library(build: bool = True) -> C.CDLL:
     i, ll, cachep, ropep = C.c_int, C.c_longlong, C.POINTER(_KVCacheStruct), C.POINTER(_RopeStruct)
     rows = [vp, ll, ll]
     lib.spec_rope_rows.argtypes = [vp, ropep, vp, i, ll, ll, vp, vp, i, ll, ll, vp, i, i32p, i, vp]
+    lib.spec_rope_rows_axes.argtypes = [vp, ropep, vp, i, vp, i, ll, ll, vp, vp, i, ll, ll, vp, i, i32p, i, vp]
+    lib.spec_cache_write_axes.argtypes = [vp, cachep, *rows, *rows, i, i, i, i32p, i32p, i32p, ropep, vp, i, i32p, vp]
     lib.spec_cache_write.argtypes = [vp, cachep, *rows, *rows, i, i, i, i32p, i32p, i32p, ropep, vp]
     lib.spec_cache_read.argtypes = [vp, cachep, i, i, i32p, i32p, vp, vp, vp]
     lib.spec_score_bytes.argtypes = [vp, i, i]
@@ -240,13 +242,27 @@ class KVCache:
 
 
 class Rope:
-    """Rotary positions: ``freq[rot / 2]`` float32 radians per position (see ``spec_rope`` in the header)."""
+    """Rotary positions: ``freq[rot / 2]`` float32 radians per position (see ``spec_rope`` in the header).
 
-    def __init__(self, freq: torch.Tensor, interleaved: bool = False, scale: float = 1.0):
+    ``axis[rot / 2]`` uint8 gives each pair the axis whose position it turns by (``spec_rope_rows_axes``): positions then
+    have the axes as their first dimension.
+    """
+
+    def __init__(self, freq: torch.Tensor, interleaved: bool = False, scale: float = 1.0, axis: torch.Tensor | None = None):
         _need(freq.is_cuda and freq.dtype == torch.float32 and freq.dim() == 1 and freq.is_contiguous(), "Rope: freq must be a contiguous float32 CUDA vector")
-        self.freq = freq
+        _need(axis is None or (axis.is_cuda and axis.dtype == torch.uint8 and axis.shape == freq.shape and axis.is_contiguous() and axis.device == freq.device),
+              "Rope: axis must be a contiguous uint8 CUDA vector as long as freq")
+        self.freq, self.axis = freq, axis
+        self._axis = None if axis is None else axis.data_ptr()
         self._struct = _RopeStruct(freq.data_ptr(), 2 * int(freq.shape[0]), int(interleaved), float(scale))
         self._ref = C.byref(self._struct)
+
+    def _positions(self, pos: torch.Tensor, tokens, what: str):
+        """Number of axes and pointer of positions for tokens of a shape."""
+        if self.axis is None:
+            return 1, _i32(pos, what, tokens)
+        axes = pos.shape[0] if pos.dim() else 0
+        return axes, _i32(pos, what, (axes, *tokens))
 
 
 class SpecContext:
@@ -536,7 +552,8 @@ class SpecContext:
     def rope_rows(self, rope: Rope, q: torch.Tensor, k: torch.Tensor | None, pos: torch.Tensor, out=None):
         """Rotates ``q[T, Hq, D]`` and ``k[T, Hk, D]`` (or ``[S, N, heads, D]``; ``k`` may be None) at ``pos`` [T] (or [S, N]).
 
-        Returns contiguous ``(q_out, k_out)``, or writes to ``out``, whose tensors may be ``q`` and ``k`` themselves.
+        With axes (``Rope.axis``) ``pos`` is [axes, T] (or [axes, S, N]).  Returns contiguous ``(q_out, k_out)``, or writes to
+        ``out``, whose tensors may be ``q`` and ``k`` themselves.
         """
         shape = q.shape
         _need(k is None or (k.shape[-1] == shape[-1] and k.shape[:-2] == shape[:-2]), "rope_rows: q and k must have the same tokens and head size")
@@ -549,21 +566,33 @@ class SpecContext:
                     _out(y, x.shape, torch.bfloat16, f"rope_rows: {name}")
         qp, qt, qh = _rows(q, "q")
         kp, kt, kh = (None, 0, 0) if k is None else _rows(k, "k")
-        self._check(self._lib.spec_rope_rows(self._h, rope._ref, qp, shape[-2], qt, qh, out[0].data_ptr(), kp, 0 if k is None else k.shape[-2],
-                                             kt, kh, None if k is None else out[1].data_ptr(), shape[-1], _i32(pos, "pos", shape[:-2]), pos.numel(),
-                                             self._raw_stream()), "spec_rope_rows")
+        rows = (qp, shape[-2], qt, qh, out[0].data_ptr(), kp, 0 if k is None else k.shape[-2], kt, kh, None if k is None else out[1].data_ptr(), shape[-1])
+        axes, at = rope._positions(pos, shape[:-2], "pos")
+        if rope.axis is None:
+            self._check(self._lib.spec_rope_rows(self._h, rope._ref, *rows, at, pos.numel(), self._raw_stream()), "spec_rope_rows")
+        else:
+            self._check(self._lib.spec_rope_rows_axes(self._h, rope._ref, rope._axis, axes, *rows, at, pos.numel() // axes if axes else 0, self._raw_stream()),
+                        "spec_rope_rows_axes")
         return out
 
     def cache_write(self, cache: KVCache, k: torch.Tensor, v: torch.Tensor, start: torch.Tensor, count: torch.Tensor | None = None,
-                    nodes: torch.Tensor | None = None, rope: Rope | None = None):
-        """Writes ``k``, ``v`` ``[S, N, heads, D]`` to positions ``start[s] + i``, ``i < count[s]`` (all N): node ``nodes[s, i]`` or ``i``."""
+                    nodes: torch.Tensor | None = None, rope: Rope | None = None, pos: torch.Tensor | None = None):
+        """Writes ``k``, ``v`` ``[S, N, heads, D]`` to positions ``start[s] + i``, ``i < count[s]`` (all N): node ``nodes[s, i]`` or ``i``.
+
+        ``pos`` [S, N] ([axes, S, N] with axes): the rotary positions of the nodes, where they are not those written to.
+        """
         _need(k.dim() == 4 and k.shape == v.shape, "cache_write: k and v must be [S, N, heads, head_dim]")
         S, N, heads, D = k.shape
         _need(heads == cache.heads and D == cache.head_dim and S == cache.sequences, "cache_write: k and v must have the cache's heads, head_dim and sequences")
         n = N if nodes is None else nodes.shape[1]
-        self._check(self._lib.spec_cache_write(self._h, cache._ref, *_rows(k, "k"), *_rows(v, "v"), S, N, n, _i32(nodes, "nodes", (S, n)),
-                                               _i32(start, "start", (S,)), _i32(count, "count", (S,)), None if rope is None else rope._ref,
-                                               self._raw_stream()), "spec_cache_write")
+        args = (self._h, cache._ref, *_rows(k, "k"), *_rows(v, "v"), S, N, n, _i32(nodes, "nodes", (S, n)), _i32(start, "start", (S,)), _i32(count, "count", (S,)))
+        if pos is None:
+            _need(rope is None or rope.axis is None, "cache_write: a rope with axes needs pos")
+            self._check(self._lib.spec_cache_write(*args, None if rope is None else rope._ref, self._raw_stream()), "spec_cache_write")
+        else:
+            _need(rope is not None, "cache_write: pos without rope")
+            axes, at = rope._positions(pos, (S, N), "pos")
+            self._check(self._lib.spec_cache_write_axes(*args, rope._ref, rope._axis, axes, at, self._raw_stream()), "spec_cache_write_axes")
 
     def cache_read(self, cache: KVCache, start: torch.Tensor, n: int, count: torch.Tensor | None = None, out=None):
         """Positions ``start[s] + i``, ``i < count[s]`` (``n``), as bfloat16 ``(k, v)`` ``[S, n, heads, D]``; zeros beyond."""

@@ -528,8 +528,11 @@ static int check_cache(spec_ctx* ctx, const spec_kv_cache* c, int S, const char*
 static int check_rope(spec_ctx* ctx, const spec_rope* r, int head_dim, const char* who, RopeArgs* out) {
     if (!r->d_freq) return fail(ctx, SPEC_ERR_ARG, "%s: rope frequencies are NULL", who);
     if (r->rot < 16 || r->rot > head_dim || r->rot % 16 != 0) return fail(ctx, SPEC_ERR_ARG, "%s: need 16 <= rot <= head_dim, rot %% 16 == 0", who);
-    *out = RopeArgs{r->d_freq, r->rot, r->interleaved != 0, r->factor};
+    *out = RopeArgs{r->d_freq, r->rot, r->interleaved != 0, r->factor, nullptr, nullptr, 1, 0};
     return SPEC_OK;
+}
+static int check_axes(spec_ctx* ctx, int axes, const char* who) {
+    return axes < 1 || axes > SPEC_MAX_AXES ? fail(ctx, SPEC_ERR_ARG, "%s: need 1 <= axes <= %d", who, (int)SPEC_MAX_AXES) : SPEC_OK;
 }
 // Rows of heads that the kernels read 16 bytes at a time.
 static int check_rows(spec_ctx* ctx, const void* d, long long tok, long long head, const char* who, const char* what) {
@@ -539,31 +542,46 @@ static int check_rows(spec_ctx* ctx, const void* d, long long tok, long long hea
     return SPEC_OK;
 }
 
-int spec_rope_rows(spec_ctx* ctx, const spec_rope* rope, const void* d_q, int Hq, long long q_tok, long long q_head, void* d_q_out,
-                   const void* d_k, int Hk, long long k_tok, long long k_head, void* d_k_out, int head_dim, const int32_t* d_pos, int T,
-                   void* stream) {
-    const char* who = "spec_rope_rows";
+static int rope_rows(spec_ctx* ctx, const char* who, const spec_rope* rope, const uint8_t* d_axis, int axes, const void* d_q, int Hq, long long q_tok,
+                     long long q_head, void* d_q_out, const void* d_k, int Hk, long long k_tok, long long k_head, void* d_k_out, int head_dim,
+                     const int32_t* d_pos, int T, void* stream) {
     if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
     if (!rope) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
     if (head_dim < 16 || head_dim > 512 || head_dim % 16 != 0) return fail(ctx, SPEC_ERR_ARG, "%s: need 16 <= head_dim <= 512, head_dim %% 16 == 0", who);
     if (T < 0 || Hq < 1 || Hk < 0 || Hq > 4096 || Hk > 4096) return fail(ctx, SPEC_ERR_ARG, "%s: need T >= 0, 1 <= Hq <= 4096, 0 <= Hk <= 4096", who);
     RopeArgs r;
     int rc = check_rope(ctx, rope, head_dim, who, &r);
-    if (rc || T == 0) return rc;
+    if (rc || (rc = check_axes(ctx, axes, who)) || T == 0) return rc;
     if (!d_pos) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
     if ((rc = check_rows(ctx, d_q, q_tok, q_head, who, "q")) || (rc = check_rows(ctx, d_q_out, 0, 0, who, "q_out"))) return rc;
     if (Hk && ((rc = check_rows(ctx, d_k, k_tok, k_head, who, "k")) || (rc = check_rows(ctx, d_k_out, 0, 0, who, "k_out")))) return rc;
+    r.axis = d_axis;
+    r.axes = axes;
+    r.pos = d_pos;
+    r.pos_axis = T;
     cudaSetDevice(ctx->device);
-    return launch_rope_rows(ctx, r, d_q, Hq, q_tok, q_head, d_q_out, d_k, Hk, k_tok, k_head, d_k_out, head_dim, d_pos, T, (cudaStream_t)stream);
+    return launch_rope_rows(ctx, r, d_q, Hq, q_tok, q_head, d_q_out, d_k, Hk, k_tok, k_head, d_k_out, head_dim, T, (cudaStream_t)stream);
 }
 
-int spec_cache_write(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_k, long long k_tok, long long k_head, const void* d_v,
-                     long long v_tok, long long v_head, int S, int N, int n, const int32_t* d_nodes, const int32_t* d_start,
-                     const int32_t* d_count, const spec_rope* rope, void* stream) {
-    const char* who = "spec_cache_write";
+int spec_rope_rows(spec_ctx* ctx, const spec_rope* rope, const void* d_q, int Hq, long long q_tok, long long q_head, void* d_q_out,
+                   const void* d_k, int Hk, long long k_tok, long long k_head, void* d_k_out, int head_dim, const int32_t* d_pos, int T,
+                   void* stream) {
+    return rope_rows(ctx, "spec_rope_rows", rope, nullptr, 1, d_q, Hq, q_tok, q_head, d_q_out, d_k, Hk, k_tok, k_head, d_k_out, head_dim, d_pos, T, stream);
+}
+
+int spec_rope_rows_axes(spec_ctx* ctx, const spec_rope* rope, const uint8_t* d_axis, int axes, const void* d_q, int Hq, long long q_tok,
+                        long long q_head, void* d_q_out, const void* d_k, int Hk, long long k_tok, long long k_head, void* d_k_out,
+                        int head_dim, const int32_t* d_pos, int T, void* stream) {
+    return rope_rows(ctx, "spec_rope_rows_axes", rope, d_axis, axes, d_q, Hq, q_tok, q_head, d_q_out, d_k, Hk, k_tok, k_head, d_k_out, head_dim, d_pos, T, stream);
+}
+
+// axes = 0: keys are rotated at the positions that they are written to
+static int cache_write(spec_ctx* ctx, const char* who, const spec_kv_cache* cache, const void* d_k, long long k_tok, long long k_head, const void* d_v,
+                       long long v_tok, long long v_head, int S, int N, int n, const int32_t* d_nodes, const int32_t* d_start, const int32_t* d_count,
+                       const spec_rope* rope, const uint8_t* d_axis, int axes, const int32_t* d_pos, void* stream) {
     if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
     CacheArgs c;
-    RopeArgs r{nullptr, 0, 0, 1.0f};
+    RopeArgs r{nullptr, 0, 0, 1.0f, nullptr, nullptr, 1, 0};
     int rc = check_cache(ctx, cache, S, who, &c);
     if (rc) return rc;
     if (S < 0 || S > 65535 || N < 0 || n < 0 || (!d_nodes && n > N)) return fail(ctx, SPEC_ERR_ARG, "%s: need 0 <= S <= 65535, N >= 0, n >= 0, and n <= N without d_nodes", who);
@@ -571,8 +589,31 @@ int spec_cache_write(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_k,
     if (S == 0 || n == 0 || N == 0) return SPEC_OK;  // (of no nodes every one that is named is skipped)
     if ((rc = check_rows(ctx, d_k, k_tok, k_head, who, "k")) || (rc = check_rows(ctx, d_v, v_tok, v_head, who, "v"))) return rc;
     if (!d_start) return fail(ctx, SPEC_ERR_ARG, "%s: d_start is NULL", who);
+    if (axes) {
+        if (!d_pos) return fail(ctx, SPEC_ERR_ARG, "%s: d_pos is NULL", who);
+        r.axis = d_axis;
+        r.axes = axes;
+        r.pos = d_pos;
+        r.pos_axis = (long long)S * N;
+    }
     cudaSetDevice(ctx->device);
     return launch_cache_write(ctx, c, d_k, k_tok, k_head, d_v, v_tok, v_head, S, N, n, d_nodes, d_start, d_count, r, (cudaStream_t)stream);
+}
+
+int spec_cache_write(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_k, long long k_tok, long long k_head, const void* d_v,
+                     long long v_tok, long long v_head, int S, int N, int n, const int32_t* d_nodes, const int32_t* d_start,
+                     const int32_t* d_count, const spec_rope* rope, void* stream) {
+    return cache_write(ctx, "spec_cache_write", cache, d_k, k_tok, k_head, d_v, v_tok, v_head, S, N, n, d_nodes, d_start, d_count, rope, nullptr, 0, nullptr, stream);
+}
+
+int spec_cache_write_axes(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_k, long long k_tok, long long k_head, const void* d_v,
+                          long long v_tok, long long v_head, int S, int N, int n, const int32_t* d_nodes, const int32_t* d_start,
+                          const int32_t* d_count, const spec_rope* rope, const uint8_t* d_axis, int axes, const int32_t* d_pos, void* stream) {
+    const char* who = "spec_cache_write_axes";
+    if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
+    if (!rope) return fail(ctx, SPEC_ERR_ARG, "%s: rope is NULL", who);
+    const int rc = check_axes(ctx, axes, who);
+    return rc ? rc : cache_write(ctx, who, cache, d_k, k_tok, k_head, d_v, v_tok, v_head, S, N, n, d_nodes, d_start, d_count, rope, d_axis, axes, d_pos, stream);
 }
 
 int spec_cache_read(spec_ctx* ctx, const spec_kv_cache* cache, int S, int n, const int32_t* d_start, const int32_t* d_count,

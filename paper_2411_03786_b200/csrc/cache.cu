@@ -53,6 +53,12 @@ __device__ __forceinline__ float2 rope_cos_sin(int pos, float freq, float factor
     return make_float2(cs * factor, sn * factor);
 }
 
+// The position that pair p of a token turns by.
+__device__ __forceinline__ int rope_position(const RopeArgs& rope, long long token, int p) {
+    const int axis = rope.axis ? rope.axis[p] : 0;
+    return axis < rope.axes ? rope.pos[axis * rope.pos_axis + token] : 0;
+}
+
 // The (cos, sin) table of one token, in the order in which lanes read it: pair p of a run of G pairs that one lane has
 // lies at (p % G) * (half / G) + p / G, so that neighbouring lanes read neighbouring words (in the order of the pairs all
 // lanes of a warp would meet in two banks).
@@ -102,7 +108,7 @@ struct RopeRows {
 // table is made: loading them after it left the kernel waiting twice (32001 tokens, 40 heads of 128: 166 us, so 123).
 constexpr int ROPE_THREADS = 512;
 template <bool INTERLEAVED>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_rows_kernel(RopeRows q, RopeRows k, int D, RopeArgs rope, const int32_t* __restrict__ pos) {
+__global__ void __launch_bounds__(ROPE_THREADS) rope_rows_kernel(RopeRows q, RopeRows k, int D, RopeArgs rope) {
     extern __shared__ float2 table[];
     grid_dependency_wait();
     grid_launch_dependents();
@@ -125,7 +131,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_rows_kernel(RopeRows q, Rop
         a = *reinterpret_cast<const uint4*>(x + e0);
         b = *reinterpret_cast<const uint4*>(x + e1);
     }
-    for (int j = threadIdx.x; j < half; j += blockDim.x) table[table_at(j, 8, half)] = rope_cos_sin(pos[t], rope.freq[j], rope.factor);
+    for (int j = threadIdx.x; j < half; j += blockDim.x) table[table_at(j, 8, half)] = rope_cos_sin(rope_position(rope, t, j), rope.freq[j], rope.factor);
     __syncthreads();
     if (it >= items) return;
     if (rotated) {
@@ -139,8 +145,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_rows_kernel(RopeRows q, Rop
 }
 
 int launch_rope_rows(spec_ctx* ctx, const RopeArgs& rope, const void* d_q, int Hq, long long q_tok, long long q_head, void* d_q_out,
-                     const void* d_k, int Hkv, long long k_tok, long long k_head, void* d_k_out, int D, const int32_t* d_pos, int T,
-                     cudaStream_t st) {
+                     const void* d_k, int Hkv, long long k_tok, long long k_head, void* d_k_out, int D, int T, cudaStream_t st) {
     const RopeRows q{(const __nv_bfloat16*)d_q, (__nv_bfloat16*)d_q_out, q_tok, q_head, Hq};
     const RopeRows k{(const __nv_bfloat16*)d_k, (__nv_bfloat16*)d_k_out, k_tok, k_head, Hkv};
     const int items = (Hq + Hkv) * (D / 16);
@@ -148,7 +153,7 @@ int launch_rope_rows(spec_ctx* ctx, const RopeArgs& rope, const void* d_q, int H
     int slices = (items + ROPE_THREADS - 1) / ROPE_THREADS;
     slices = std::max(slices, std::min((items + 63) / 64, ctx->num_sms / T));
     const int threads = ((items + slices - 1) / slices + 31) / 32 * 32;
-    auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(T, slices), dim3(threads), sizeof(float2) * (rope.rot / 2), st, q, k, D, rope, d_pos); };
+    auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(T, slices), dim3(threads), sizeof(float2) * (rope.rot / 2), st, q, k, D, rope); };
     cudaError_t e = rope.interleaved ? go(rope_rows_kernel<true>) : go(rope_rows_kernel<false>);
     ctx->launches += 1;
     return check_cuda(ctx, e, "spec_rope_rows launch");
@@ -280,7 +285,12 @@ __global__ void __launch_bounds__(CACHE_THREADS, 4) cache_write_kernel(CacheArgs
             }
             for (int i = threadIdx.x; ROPE != ROPE_NONE && i < n_here * half; i += CACHE_THREADS) {
                 const int t = i / half, p = i - t * half;
-                table[t * half + table_at(p, ROPE == ROPE_PAIRS ? 4 : 8, half)] = rope_cos_sin(pos0 + t, rope.freq[p], rope.factor);
+                int at = pos0 + t;
+                if (rope.pos) {
+                    const int node = nodes ? nodes[(long long)s * n + i0 + t] : i0 + t;
+                    at = node >= 0 && node < N ? rope_position(rope, (long long)s * N + node, p) : 0;
+                }
+                table[t * half + table_at(p, ROPE == ROPE_PAIRS ? 4 : 8, half)] = rope_cos_sin(at, rope.freq[p], rope.factor);
             }
             __syncthreads();
         }

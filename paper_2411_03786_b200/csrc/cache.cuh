@@ -20,11 +20,14 @@ struct RopeArgs {
     const float* freq;  // [rot / 2] radians per position
     int rot, interleaved;
     float factor;
+    const uint8_t* axis;  // [rot / 2] axis of each pair, or null: 0
+    const int32_t* pos;   // [axes, tokens], or null: the positions that keys are written to
+    int axes;
+    long long pos_axis;   // from one axis to the next
 };
 
 int launch_rope_rows(spec_ctx* ctx, const RopeArgs& rope, const void* d_q, int Hq, long long q_tok, long long q_head, void* d_q_out,
-                     const void* d_k, int Hkv, long long k_tok, long long k_head, void* d_k_out, int D, const int32_t* d_pos, int T,
-                     cudaStream_t st);
+                     const void* d_k, int Hkv, long long k_tok, long long k_head, void* d_k_out, int D, int T, cudaStream_t st);
 int launch_cache_write(spec_ctx* ctx, const CacheArgs& c, const void* d_k, long long k_tok, long long k_head, const void* d_v,
                        long long v_tok, long long v_head, int S, int N, int n, const int32_t* d_nodes, const int32_t* d_start,
                        const int32_t* d_count, const RopeArgs& rope, cudaStream_t st);
