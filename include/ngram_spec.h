@@ -393,6 +393,42 @@ int spec_cache_read(spec_ctx* ctx, const spec_kv_cache* cache, int S, int n, con
                     void* d_k_out, void* d_v_out, void* stream);
 
 /*
+ * Pages of a cache.  All layers of a model share one table; sequences that begin alike share pages.  d_refs[p] counts the
+ * table entries that name page p - a caller may add holders of its own, such as a prompt that is kept - and 0 means free; entries
+ * outside [0, n_pages) name no page (the calls write -1).  Counts that do not fit the table give pages away twice: start with a table of -1 and zeros.
+ * The decisions are made on the device and are the same every time.  Limits: S <= SPEC_MAX_PAGED, n_pages <= 2^24,
+ * S * max_pages < 2^31, page 16, 32, 64 or 128 tokens, heads * page * head_dim < 2^30.
+ *
+ *   spec_pages_assign   row s becomes the pages that the first d_len[s] positions of (the old) row d_source[s] lie in, and nothing
+ *                       behind them; a source outside [0, S) gives an empty row.  Forks (several rows with one source), changes the
+ *                       order of sequences, drops what was not accepted (d_source[s] = s) and frees, in any mixture.
+ *   spec_pages_reserve  gives every sequence pages of its own for positions [d_start[s], d_start[s] + d_count[s]): where there is none a
+ *                       free one, and in place of a page that has other holders a copy in all `caches`.  The lowest free pages go out, in the order
+ *                       of sequences and positions.  d_ok[s] = 0 and SPEC_STATUS_CAPACITY where a sequence's row is left as it was: its positions do
+ *                       not fit the row, or it, or one before it, needs more pages than are left (else 1).
+ *   spec_pages_compact  moves live pages to the front, in all `caches`, the table and the counts: of L of them those from L on go, in order, to the
+ *                       free ones below L.  d_n_live[0] = L.  Page numbers that the caller keeps elsewhere are not renumbered.
+ *   spec_pages_copy     copies page d_src[i] to page d_dst[i] in all `caches`, i < min(n, d_n[0]) (d_n NULL: n).  No page may be the destination
+ *                       of two, or source and destination of different ones; pairs outside the pool are skipped, with SPEC_STATUS_CAPACITY.
+ * `caches`: n_caches <= SPEC_MAX_LAYERS of them, alike in n_pages and page; heads, head_dim and dtype may differ.  Their tables are not looked at.
+ * None (n_caches = 0) where the caller copies by itself.  d_work: spec_pages_bytes() of scratch, 16-byte aligned, for this call alone.
+ */
+enum { SPEC_MAX_PAGED = 32768, SPEC_MAX_LAYERS = 128 };
+typedef struct spec_pages {
+    int32_t* d_table; /* [S, max_pages] */
+    int32_t* d_refs;  /* [n_pages] */
+    int S, max_pages, n_pages, page;
+} spec_pages;
+size_t spec_pages_bytes(spec_ctx* ctx, const spec_pages* pages);
+int spec_pages_assign(spec_ctx* ctx, const spec_pages* pages, const int32_t* d_source, const int32_t* d_len, void* stream);
+int spec_pages_reserve(spec_ctx* ctx, const spec_pages* pages, const spec_kv_cache* caches, int n_caches, const int32_t* d_start,
+                       const int32_t* d_count, int32_t* d_ok, void* d_work, size_t work_bytes, void* stream);
+int spec_pages_compact(spec_ctx* ctx, const spec_pages* pages, const spec_kv_cache* caches, int n_caches, int32_t* d_n_live, void* d_work,
+                       size_t work_bytes, void* stream);
+int spec_pages_copy(spec_ctx* ctx, const spec_kv_cache* caches, int n_caches, const int32_t* d_src, const int32_t* d_dst, const int32_t* d_n,
+                    int n, void* stream);
+
+/*
  * Ancestors of each node of a draft forest, itself included, as bits: word j/32 bit j%32 of d_mask[s, i, :] says that
  * node i attends to node j; d_mask is [S, N, ceil(N/32)].  d_parent[s, i] < i, or -1 for a root.  A node beyond
  * d_nnodes[s] (NULL: N), or whose path to a root breaks that order, gets an empty mask and depth -1.  N <= 4096.

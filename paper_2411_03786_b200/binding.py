@@ -36,6 +36,10 @@ class _RopeStruct(C.Structure):
     _fields_ = [("d_freq", C.c_void_p), ("rot", C.c_int), ("interleaved", C.c_int), ("factor", C.c_float)]
 
 
+class _PagesStruct(C.Structure):
+    _fields_ = [("d_table", C.c_void_p), ("d_refs", C.c_void_p), ("S", C.c_int), ("max_pages", C.c_int), ("n_pages", C.c_int), ("page", C.c_int)]
+
+
 def declared_symbols() -> list[str]:
     """Function names declared in the public header."""
     text = re.sub(r"/\*.*?\*/", "", open(_HEADER).read(), flags=re.S)
@@ -102,6 +106,13 @@ def load_library(build: bool = True) -> C.CDLL:
     lib.spec_tree_attention_bytes.argtypes = [vp, cachep, i, i, i]
     lib.spec_tree_attention_bytes.restype = C.c_size_t
     lib.spec_tree_attention.argtypes = [vp, cachep, *rows, *rows, *rows, i, i, i, i32p, i32p, i32p, C.c_float, vp, fp, vp, C.c_size_t, vp]
+    pagesp = C.POINTER(_PagesStruct)
+    lib.spec_pages_bytes.argtypes = [vp, pagesp]
+    lib.spec_pages_bytes.restype = C.c_size_t
+    lib.spec_pages_assign.argtypes = [vp, pagesp, i32p, i32p, vp]
+    lib.spec_pages_reserve.argtypes = [vp, pagesp, cachep, i, i32p, i32p, i32p, vp, C.c_size_t, vp]
+    lib.spec_pages_compact.argtypes = [vp, pagesp, cachep, i, i32p, vp, C.c_size_t, vp]
+    lib.spec_pages_copy.argtypes = [vp, cachep, i, i32p, i32p, i32p, i, vp]
     lib.spec_launch_count.argtypes = [vp]
     lib.spec_launch_count.restype = C.c_longlong
     _lib = lib
@@ -239,6 +250,40 @@ class KVCache:
         if bits == 8:
             return cls(new(*shape, head_dim), new(*shape, head_dim), table, new(*shape), new(*shape))
         return cls(new(*shape, head_dim, dtype=torch.bfloat16), new(*shape, head_dim, dtype=torch.bfloat16), table)
+
+
+class PagePool:
+    """The caches of a model's layers, which share one table, and who holds their pages (see ``spec_pages`` in the header).
+
+    ``refs[n_pages]`` int32 counts the table entries that name a page; None: counted from the table as it is now.
+    """
+
+    def __init__(self, caches, refs: torch.Tensor | None = None):
+        caches = list(caches)
+        _need(len(caches) > 0, "PagePool: at least one cache is needed")
+        c = caches[0]
+        for x in caches:
+            _need(x.table.data_ptr() == c.table.data_ptr() and x.table.shape == c.table.shape and x.n_pages == c.n_pages and x.page == c.page,
+                  "PagePool: the caches must share one table and be alike in n_pages and page")
+        if refs is None:
+            held = c.table[(c.table >= 0) & (c.table < c.n_pages)].long()
+            refs = torch.bincount(held, minlength=c.n_pages).int()
+        _need(refs.is_cuda and refs.dtype == torch.int32 and refs.shape == (c.n_pages,) and refs.is_contiguous() and refs.device == c.table.device,
+              "PagePool: refs must be contiguous int32 [n_pages] on the caches' device")
+        self.caches, self.table, self.refs = caches, c.table, refs
+        self.n_pages, self.page, self.sequences = c.n_pages, c.page, c.sequences
+        self._struct = _PagesStruct(c.table.data_ptr(), refs.data_ptr(), c.sequences, int(c.table.shape[1]), c.n_pages, c.page)
+        self._ref = C.byref(self._struct)
+        self._device = refs.device.index or 0
+        self._layers = (_KVCacheStruct * len(caches))(*[x._struct for x in caches])
+        self._work_bytes = 0
+
+    @classmethod
+    def empty(cls, layers: int, n_pages: int, sequences: int, max_pages: int, heads: int, page: int, head_dim: int, bits: int = 16, device="cuda") -> "PagePool":
+        """Caches of ``layers`` layers without a sequence in them."""
+        table = torch.full((sequences, max_pages), -1, dtype=torch.int32, device=device)
+        caches = [KVCache.empty(n_pages, heads, page, head_dim, table, bits=bits) for _ in range(layers)]
+        return cls(caches, torch.zeros(n_pages, dtype=torch.int32, device=device))
 
 
 class Rope:
@@ -607,6 +652,56 @@ class SpecContext:
         self._check(self._lib.spec_cache_read(self._h, cache._ref, S, n, _i32(start, "start", (S,)), _i32(count, "count", (S,)),
                                               out[0].data_ptr(), out[1].data_ptr(), self._raw_stream()), "spec_cache_read")
         return out
+
+    def _pages_work(self, pool: PagePool, work: torch.Tensor | None, what: str):
+        _need(pool._device == self._device, f"{what}: the pool is on another device")
+        if work is not None:
+            return work, *_scratch(work, what)
+        if not pool._work_bytes:
+            pool._work_bytes = self._lib.spec_pages_bytes(self._h, pool._ref)
+        need = max(pool._work_bytes, 16)
+        work = pool.refs.new_empty((need + 3) // 4)
+        return work, work.data_ptr(), need
+
+    def pages_assign(self, pool: PagePool, source: torch.Tensor, lens: torch.Tensor):
+        """Row s of the table becomes the pages of the first ``lens[s]`` positions of row ``source[s]`` (outside the rows: none).
+
+        Forks, reorders, shortens and frees sequences, in any mixture.
+        """
+        S = pool.sequences
+        _need(pool._device == self._device, "pages_assign: the pool is on another device")
+        self._check(self._lib.spec_pages_assign(self._h, pool._ref, _i32(source, "source", (S,)), _i32(lens, "lens", (S,)), self._raw_stream()), "spec_pages_assign")
+
+    def pages_reserve(self, pool: PagePool, start: torch.Tensor, count: torch.Tensor, out: torch.Tensor | None = None, work: torch.Tensor | None = None):
+        """Pages of their own for positions ``start[s] .. start[s] + count[s]`` of every sequence: free ones, or copies of shared ones.
+
+        Returns ``ok[S]`` int32: 0 where there were not enough and a row was left as it was.
+        """
+        S = pool.sequences
+        if out is None:
+            out = start.new_empty((S,))
+        else:
+            _out(out, (S,), torch.int32, "pages_reserve: ok")
+        work, *scratch = self._pages_work(pool, work, "pages_reserve")
+        self._check(self._lib.spec_pages_reserve(self._h, pool._ref, pool._layers, len(pool._layers), _i32(start, "start", (S,)), _i32(count, "count", (S,)),
+                                                 out.data_ptr(), *scratch, self._raw_stream()), "spec_pages_reserve")
+        return out
+
+    def pages_compact(self, pool: PagePool, out: torch.Tensor | None = None, work: torch.Tensor | None = None):
+        """Moves the pages that are held to the front of the pool.  Returns their number, int32 [1] on the device."""
+        if out is None:
+            out = pool.refs.new_empty((1,))
+        else:
+            _out(out, (1,), torch.int32, "pages_compact: n_live")
+        work, *scratch = self._pages_work(pool, work, "pages_compact")
+        self._check(self._lib.spec_pages_compact(self._h, pool._ref, pool._layers, len(pool._layers), out.data_ptr(), *scratch, self._raw_stream()), "spec_pages_compact")
+        return out
+
+    def pages_copy(self, pool: PagePool, src: torch.Tensor, dst: torch.Tensor, n: torch.Tensor | None = None):
+        """Copies page ``src[i]`` to page ``dst[i]`` in all layers (``n`` int32 [1]: only the first ``n`` of them)."""
+        _need(src.dim() == 1 and pool._device == self._device, "pages_copy: src must be [n], on the pool's device")
+        self._check(self._lib.spec_pages_copy(self._h, pool._layers, len(pool._layers), _i32(src, "src", src.shape), _i32(dst, "dst", src.shape), _i32(n, "n", (1,)),
+                                              src.shape[0], self._raw_stream()), "spec_pages_copy")
 
     def tree_mask(self, parent: torch.Tensor, n_nodes: torch.Tensor | None = None):
         """Mask words ``[S, N, ceil(N / 32)]`` and depths ``[S, N]`` (int32) of the forests ``parent[S, N]`` (-1 = root)."""

@@ -631,6 +631,94 @@ int spec_cache_read(spec_ctx* ctx, const spec_kv_cache* cache, int S, int n, con
     return launch_cache_read(ctx, c, S, n, d_start, d_count, d_k_out, d_v_out, (cudaStream_t)stream);
 }
 
+static int check_pages(spec_ctx* ctx, const spec_pages* p, const char* who, PagesArgs* out) {
+    if (!p) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
+    if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128) return fail(ctx, SPEC_ERR_UNSUPPORTED, "%s: page must be 16, 32, 64 or 128 tokens", who);
+    if (p->S < 0 || p->S > SPEC_MAX_PAGED || p->n_pages < 1 || p->n_pages > (1 << 24) || p->max_pages < 1 || (long long)p->max_pages * p->page > (1ll << 30) ||
+        (long long)p->S * p->max_pages >= (1ll << 31))
+        return fail(ctx, SPEC_ERR_ARG, "%s: need 0 <= S <= %d, 1 <= n_pages <= 2^24, max_pages >= 1, max_pages * page <= 2^30 and S * max_pages < 2^31", who, (int)SPEC_MAX_PAGED);
+    if ((p->S > 0 && !p->d_table) || !p->d_refs) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
+    int shift = 4;
+    while ((1 << shift) < p->page) ++shift;
+    *out = PagesArgs{p->d_table, p->d_refs, p->S, p->max_pages, p->n_pages, shift};
+    return SPEC_OK;
+}
+// The caches of a pool's layers; n_pages = 0: as the first has them.
+static int check_layers(spec_ctx* ctx, const spec_kv_cache* caches, int n_caches, int n_pages, int page, const char* who, CacheArgs* out) {
+    if (n_caches < 0 || n_caches > SPEC_MAX_LAYERS || (n_caches > 0 && !caches)) return fail(ctx, SPEC_ERR_ARG, "%s: need 0 <= n_caches <= %d", who, (int)SPEC_MAX_LAYERS);
+    for (int i = 0; i < n_caches; ++i) {
+        const int rc = check_cache(ctx, caches + i, 0, who, out + i);
+        if (rc) return rc;
+        if (caches[i].n_pages != (n_pages ? n_pages : caches[0].n_pages) || caches[i].page != (page ? page : caches[0].page))
+            return fail(ctx, SPEC_ERR_ARG, "%s: the caches must have the same pages", who);
+        if (((long long)out[i].heads << out[i].page_shift) * out[i].head_dim >= (1ll << 30)) return fail(ctx, SPEC_ERR_ARG, "%s: need heads * page * head_dim < 2^30", who);
+    }
+    return SPEC_OK;
+}
+
+size_t spec_pages_bytes(spec_ctx* ctx, const spec_pages* pages) {
+    PagesArgs a;
+    return !ctx || check_pages(ctx, pages, "spec_pages_bytes", &a) ? 0 : pages_bytes(a.S, a.n_pages);
+}
+static int check_pages_work(spec_ctx* ctx, const PagesArgs& a, void* d_work, size_t bytes, const char* who) {
+    if (!d_work || !aligned16(d_work)) return fail(ctx, SPEC_ERR_ARG, "%s: work must be 16-byte aligned", who);
+    const size_t need = pages_bytes(a.S, a.n_pages);
+    return bytes < need ? fail(ctx, SPEC_ERR_ARG, "%s: %zu bytes of scratch given, %zu needed", who, bytes, need) : SPEC_OK;
+}
+
+int spec_pages_assign(spec_ctx* ctx, const spec_pages* pages, const int32_t* d_source, const int32_t* d_len, void* stream) {
+    const char* who = "spec_pages_assign";
+    if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
+    PagesArgs a;
+    const int rc = check_pages(ctx, pages, who, &a);
+    if (rc || a.S == 0) return rc;
+    if (!d_source || !d_len) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
+    cudaSetDevice(ctx->device);
+    return launch_pages_assign(ctx, a, d_source, d_len, (cudaStream_t)stream);
+}
+
+int spec_pages_reserve(spec_ctx* ctx, const spec_pages* pages, const spec_kv_cache* caches, int n_caches, const int32_t* d_start,
+                       const int32_t* d_count, int32_t* d_ok, void* d_work, size_t work_bytes, void* stream) {
+    const char* who = "spec_pages_reserve";
+    if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
+    PagesArgs a;
+    CacheArgs c[SPEC_MAX_LAYERS];
+    int rc = check_pages(ctx, pages, who, &a);
+    if (rc || (rc = check_layers(ctx, caches, n_caches, a.n_pages, pages->page, who, c)) || a.S == 0) return rc;
+    if (!d_start || !d_count || !d_ok) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
+    if ((rc = check_pages_work(ctx, a, d_work, work_bytes, who))) return rc;
+    cudaSetDevice(ctx->device);
+    return launch_pages_reserve(ctx, a, c, n_caches, d_start, d_count, d_ok, d_work, (cudaStream_t)stream);
+}
+
+int spec_pages_compact(spec_ctx* ctx, const spec_pages* pages, const spec_kv_cache* caches, int n_caches, int32_t* d_n_live, void* d_work,
+                       size_t work_bytes, void* stream) {
+    const char* who = "spec_pages_compact";
+    if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
+    PagesArgs a;
+    CacheArgs c[SPEC_MAX_LAYERS];
+    int rc = check_pages(ctx, pages, who, &a);
+    if (rc || (rc = check_layers(ctx, caches, n_caches, a.n_pages, pages->page, who, c))) return rc;
+    if (!d_n_live) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
+    if ((rc = check_pages_work(ctx, a, d_work, work_bytes, who))) return rc;
+    cudaSetDevice(ctx->device);
+    return launch_pages_compact(ctx, a, c, n_caches, d_n_live, d_work, (cudaStream_t)stream);
+}
+
+int spec_pages_copy(spec_ctx* ctx, const spec_kv_cache* caches, int n_caches, const int32_t* d_src, const int32_t* d_dst, const int32_t* d_n, int n,
+                    void* stream) {
+    const char* who = "spec_pages_copy";
+    if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "%s: ctx is NULL", who);
+    CacheArgs c[SPEC_MAX_LAYERS];
+    const int rc = check_layers(ctx, caches, n_caches, 0, 0, who, c);
+    if (rc) return rc;
+    if (n < 0) return fail(ctx, SPEC_ERR_ARG, "%s: need n >= 0", who);
+    if (n == 0 || n_caches == 0) return SPEC_OK;
+    if (!d_src || !d_dst) return fail(ctx, SPEC_ERR_ARG, "%s: NULL pointer", who);
+    cudaSetDevice(ctx->device);
+    return launch_pages_copy(ctx, c, n_caches, d_src, d_dst, d_n, n, (cudaStream_t)stream);
+}
+
 int spec_tree_mask(spec_ctx* ctx, const int32_t* d_parent, int S, int N, const int32_t* d_nnodes, int32_t* d_mask, int32_t* d_depth,
                    void* stream) {
     if (!ctx) return fail(nullptr, SPEC_ERR_ARG, "spec_tree_mask: ctx is NULL");

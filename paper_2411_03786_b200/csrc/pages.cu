@@ -1,0 +1,408 @@
+// Who holds which page of a paged cache: forking, shortening, reordering and freeing (assign), pages of their own for the
+// positions that come next (reserve), live pages to the front (compact), and the copies that these ask for.
+//
+// All layers of a model share one table [S, max_pages]; refs[p] counts the table entries that name page p (a caller may
+// hold further ones), and a page is free at 0.  Everything is decided on the device, without a look from the host, so that a
+// step with these calls can be captured.  What they decide does not depend on the order in which anything runs: the lowest
+// free pages go to the lowest (sequence, index), counts are sums.
+//
+// Bytes bound the copies (each copied page read and written once), latency the rest: a table row of a sequence is some
+// hundred numbers.  What needs a view of all counts is done by one cluster of 8 CTAs, which meet at its hardware barrier a few times
+// instead of being launched again for each step.
+#include <algorithm>
+
+#include "cache.cuh"
+
+namespace ngs {
+
+constexpr int CLUSTER = 8, PLAN_THREADS = 1024, PLAN_PER = 8;  // pages that a thread looks at side by side
+constexpr int ASSIGN_THREADS = 256, ASSIGN_SMEM = 128 * 1024;
+constexpr int COPY_THREADS = 256, PIECE = 2048;  // bytes that a warp copies at a time: four times 16 for each lane
+
+// Scratch of reserve and compact, in ints.
+struct PagesWork {
+    int* head;    // [0] pairs to copy, [1] live pages; [8, 16) and [16, 24) counts of the CTAs
+    int* src;     // [n_pages] pairs to copy
+    int* dst;     // [n_pages]
+    int* list;    // [n_pages] free pages in order (reserve), where a page goes (compact)
+    int* demand;  // [S] pages that a sequence needs, then those needed before it
+};
+constexpr int WORK_HEAD = 64;
+
+static PagesWork pages_work(void* work, int n_pages) {
+    int* w = reinterpret_cast<int*>(work);
+    return PagesWork{w, w + WORK_HEAD, w + WORK_HEAD + n_pages, w + WORK_HEAD + 2 * (size_t)n_pages, w + WORK_HEAD + 3 * (size_t)n_pages};
+}
+size_t pages_bytes(int S, int n_pages) { return (WORK_HEAD + 3 * (size_t)n_pages + S) * sizeof(int); }
+
+__device__ __forceinline__ void cluster_meet() {  // (with what its threads have written to memory)
+    __threadfence();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ int cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return (int)r;
+}
+// Sum over the CTA (all threads get it), and the sum of the threads before this one.
+__device__ __forceinline__ int block_scan(int n, int& before, int* shared) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int upto = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int other = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += other;
+    }
+    __syncthreads();
+    if (lane == 31) shared[warp] = upto;
+    __syncthreads();
+    int w = shared[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int other = __shfl_up_sync(0xffffffffu, w, o);
+        if (lane >= o) w += other;
+    }
+    before = upto - n + (warp ? __shfl_sync(0xffffffffu, w, (warp + 31) & 31) : 0);
+    return __shfl_sync(0xffffffffu, w, 31);
+}
+// The counts that the CTAs left at `at`: their sum, and of those before this CTA.
+__device__ __forceinline__ int cluster_scan(const int* at, int rank, int& before) {
+    int sum = 0;
+    before = 0;
+#pragma unroll
+    for (int i = 0; i < CLUSTER; ++i) {
+        const int n = __ldcg(at + i);
+        if (i < rank) before += n;
+        sum += n;
+    }
+    return sum;
+}
+
+// ------------------------------------------------------------------------------------------ assign
+// A CTA has `cols` columns of all rows: it reads the whole of them, as they are to be, before it writes any, so that rows may
+// change places, and only itself reads or writes them.
+__global__ void __launch_bounds__(ASSIGN_THREADS) pages_assign_kernel(PagesArgs a, int cols, const int32_t* __restrict__ source, const int32_t* __restrict__ len) {
+    extern __shared__ int fresh[];  // [S, cols]
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int c0 = blockIdx.x * cols, n = a.S * cols;
+    for (int i = threadIdx.x; i < n; i += ASSIGN_THREADS) {
+        const int s = i / cols, c = c0 + i - s * cols, from = source[s];
+        int page = -1;
+        if (c < a.max_pages && (unsigned)from < (unsigned)a.S && ((long long)c << a.page_shift) < len[s]) page = a.table[(long long)from * a.max_pages + c];
+        fresh[i] = (unsigned)page < (unsigned)a.n_pages ? page : -1;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += ASSIGN_THREADS) {
+        const int s = i / cols, c = c0 + i - s * cols;
+        if (c >= a.max_pages) continue;
+        int32_t* entry = a.table + (long long)s * a.max_pages + c;
+        const int old = *entry, now = fresh[i];
+        if (old == now) continue;
+        *entry = now;
+        if (now >= 0) atomicAdd(a.refs + now, 1);
+        if ((unsigned)old < (unsigned)a.n_pages) atomicSub(a.refs + old, 1);
+    }
+}
+
+int launch_pages_assign(spec_ctx* ctx, const PagesArgs& a, const int32_t* d_source, const int32_t* d_len, cudaStream_t st) {
+    int cols = 8;  // a sector of a row, fewer where that many rows do not fit
+    while (cols > 1 && (long long)a.S * cols * 4 > ASSIGN_SMEM) cols /= 2;
+    const size_t smem = (size_t)a.S * cols * 4;
+    {
+        static bool done[64] = {false};
+        std::lock_guard<std::mutex> lock(host_mutex());
+        bool& d = done[ctx->device & 63];
+        if (!d) {
+            int rc = check_cuda(ctx, cudaFuncSetAttribute(pages_assign_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ASSIGN_SMEM), "spec_pages_assign: cudaFuncSetAttribute");
+            if (rc) return rc;
+            d = true;
+        }
+    }
+    cudaError_t e = launch_pdl(pages_assign_kernel, dim3((a.max_pages + cols - 1) / cols), dim3(ASSIGN_THREADS), smem, st, a, cols, d_source, d_len);
+    ++ctx->launches;
+    return check_cuda(ctx, e, "spec_pages_assign launch");
+}
+
+// ------------------------------------------------------------------------------------------ reserve
+// The entries of a sequence's row that its next positions lie in; n = 0: none, or not possible.
+struct Span {
+    int first, n;
+    bool ok;
+};
+__device__ __forceinline__ Span span_of(const PagesArgs& a, int start, int count) {
+    const bool ok = start >= 0 && count >= 0 && (long long)start + count <= ((long long)a.max_pages << a.page_shift);
+    const int first = start >> a.page_shift;
+    return Span{first, ok && count > 0 ? (int)(((long long)start + count - 1) >> a.page_shift) - first + 1 : 0, ok};
+}
+__device__ __forceinline__ bool needs_page(const PagesArgs& a, int page) {  // there is none, or others hold it too
+    return (unsigned)page >= (unsigned)a.n_pages || __ldcg(a.refs + page) != 1;
+}
+
+__global__ void __launch_bounds__(PLAN_THREADS) pages_reserve_kernel(PagesArgs a, PagesWork w, const int32_t* __restrict__ start, const int32_t* __restrict__ count,
+                                                                   int32_t* __restrict__ ok, int* status) {
+    __shared__ int shared[32];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int rank = cluster_rank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (rank == 0 && threadIdx.x == 0) w.head[0] = 0;
+    // ---- pages that each sequence needs: a warp per sequence, consecutive sequences to a CTA
+    const int per = (a.S + CLUSTER - 1) / CLUSTER, s0 = min(rank * per, a.S), s1 = min(s0 + per, a.S);
+    for (int s = s0 + warp; s < s1; s += PLAN_THREADS / 32) {
+        const Span sp = span_of(a, start[s], count[s]);
+        const int32_t* row = a.table + (long long)s * a.max_pages + sp.first;
+        int n = 0;
+        for (int i = lane; i < sp.n; i += 32) n += needs_page(a, row[i]);
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (lane == 0) w.demand[s] = sp.ok ? n : -1;
+    }
+    __syncthreads();
+    // ---- and free pages of this CTA's part of the pool
+    int demand = 0, unused, n_free = 0;
+    for (int s = s0 + threadIdx.x; s < s1; s += PLAN_THREADS) demand += max(w.demand[s], 0);
+    demand = block_scan(demand, unused, shared);
+    const int per_pool = (a.n_pages + CLUSTER - 1) / CLUSTER, p0 = min(rank * per_pool, a.n_pages), p1 = min(p0 + per_pool, a.n_pages);
+    for (int p = p0 + threadIdx.x; p < p1; p += PLAN_THREADS) n_free += a.refs[p] == 0;
+    n_free = block_scan(n_free, unused, shared);
+    if (threadIdx.x == 0) {
+        w.head[8 + rank] = demand;
+        w.head[16 + rank] = n_free;
+    }
+    cluster_meet();
+    int base, free_base;
+    const int wanted = cluster_scan(w.head + 8, rank, base), total_free = cluster_scan(w.head + 16, rank, free_base);
+    // ---- who gets his pages: those that come before the first that needs more than is left
+    for (int b = s0; b < s1; b += PLAN_THREADS) {
+        const int s = b + threadIdx.x, n = s < s1 ? w.demand[s] : 0;
+        int before;
+        const int sum = block_scan(max(n, 0), before, shared);
+        before += base;
+        if (s < s1) {
+            const bool good = n == 0 || (n > 0 && before + n <= total_free);
+            ok[s] = good;
+            w.demand[s] = good ? before : -1;
+            if (!good) atomicOr(status, SPEC_STATUS_CAPACITY);
+        }
+        base += sum;
+    }
+    // ---- the free pages in order, as many as are wanted
+    for (int b = p0; b < p1 && free_base < wanted; b += PLAN_THREADS * PLAN_PER) {
+        const int p = b + threadIdx.x * PLAN_PER;
+        uint32_t free = 0;
+#pragma unroll
+        for (int j = 0; j < PLAN_PER; ++j)
+            if (p + j < p1 && a.refs[p + j] == 0) free |= 1u << j;
+        int before;
+        const int sum = block_scan(__popc(free), before, shared);
+        before += free_base;
+#pragma unroll
+        for (int j = 0; j < PLAN_PER; ++j)
+            if ((free >> j) & 1u) w.list[before++] = p + j;
+        free_base += sum;
+    }
+    cluster_meet();
+    // ---- hand them out.  (Counts of pages that lose a holder stay until all have looked at them.)
+    for (int s = s0 + warp; s < s1; s += PLAN_THREADS / 32) {
+        const Span sp = span_of(a, start[s], count[s]);
+        int at = w.demand[s];
+        if (at < 0) continue;
+        int32_t* row = a.table + (long long)s * a.max_pages + sp.first;
+        for (int i0 = 0; i0 < sp.n; i0 += 32) {
+            const int i = i0 + lane, old = i < sp.n ? row[i] : 0;
+            const bool need = i < sp.n && needs_page(a, old);
+            const unsigned who = __ballot_sync(0xffffffffu, need), below = who & ((1u << lane) - 1u);
+            if (need) {
+                const int page = __ldcg(w.list + at + __popc(below));
+                row[i] = page;
+                a.refs[page] = 1;
+                if ((unsigned)old < (unsigned)a.n_pages) {
+                    const int k = atomicAdd(w.head, 1);
+                    w.src[k] = old;
+                    w.dst[k] = page;
+                }
+            }
+            at += __popc(who);
+        }
+    }
+    cluster_meet();
+    const int n_pairs = __ldcg(w.head);
+    for (int k = rank * PLAN_THREADS + threadIdx.x; k < n_pairs; k += CLUSTER * PLAN_THREADS) atomicSub(a.refs + __ldcg(w.src + k), 1);
+}
+
+// ------------------------------------------------------------------------------------------ compact
+// With L live pages, those numbered from L on go, in their order, to the free ones below L: there are as many of each, no page
+// is both, and so the copies can run side by side.
+__global__ void __launch_bounds__(PLAN_THREADS) pages_compact_kernel(PagesArgs a, PagesWork w, int32_t* __restrict__ n_live) {
+    __shared__ int shared[32];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int rank = cluster_rank(), per_pool = (a.n_pages + CLUSTER - 1) / CLUSTER, p0 = min(rank * per_pool, a.n_pages), p1 = min(p0 + per_pool, a.n_pages);
+    int n = 0, unused, live_base, below_base;
+    for (int p = p0 + threadIdx.x; p < p1; p += PLAN_THREADS) n += a.refs[p] > 0;
+    n = block_scan(n, unused, shared);
+    if (threadIdx.x == 0) w.head[8 + rank] = n;
+    cluster_meet();
+    const int live = cluster_scan(w.head + 8, rank, live_base);
+    n = 0;
+    for (int p = p0 + threadIdx.x; p < min(p1, live); p += PLAN_THREADS) n += a.refs[p] > 0;
+    n = block_scan(n, unused, shared);
+    if (threadIdx.x == 0) w.head[16 + rank] = n;
+    cluster_meet();
+    const int stay = cluster_scan(w.head + 16, rank, below_base);  // live pages below L
+    for (int b = p0; b < p1; b += PLAN_THREADS * PLAN_PER) {
+        const int p = b + threadIdx.x * PLAN_PER;
+        uint32_t held = 0;
+#pragma unroll
+        for (int j = 0; j < PLAN_PER; ++j)
+            if (p + j < p1 && a.refs[p + j] > 0) held |= 1u << j;
+        int before;
+        const int sum = block_scan(__popc(held), before, shared);
+        before += live_base;  // live pages below p
+#pragma unroll
+        for (int j = 0; j < PLAN_PER; ++j) {
+            if (p + j >= p1) continue;
+            const bool is_live = (held >> j) & 1u;
+            if (p + j >= live) {
+                w.list[p + j] = p + j;
+                if (is_live) w.src[before - stay] = p + j;
+            } else if (!is_live) {
+                w.dst[p + j - before] = p + j;
+            }
+            before += is_live;
+        }
+        live_base += sum;
+    }
+    cluster_meet();
+    const int n_pairs = live - stay;
+    for (int k = rank * PLAN_THREADS + threadIdx.x; k < n_pairs; k += CLUSTER * PLAN_THREADS) {
+        const int src = __ldcg(w.src + k), dst = __ldcg(w.dst + k);
+        w.list[src] = dst;
+        a.refs[dst] = __ldcg(a.refs + src);
+        a.refs[src] = 0;
+    }
+    if (rank == 0 && threadIdx.x == 0) {
+        w.head[0] = n_pairs;
+        w.head[1] = live;
+        *n_live = live;
+    }
+}
+
+// ------------------------------------------------------------------------------------------ copies
+// The tensors of a pool's layers: pages of `bytes` each, whose pieces are numbered through from `first`.
+template <int MAX>
+struct Tensors {
+    char* base[MAX];
+    uint32_t bytes[MAX];
+    int first[MAX + 1];
+    int n;
+};
+// A warp copies a piece of a page of a tensor, 4 x 16 bytes for each lane; consecutive warps have consecutive pieces.  After a compaction
+// the entries of the table are renumbered along with it.
+template <int MAX>
+__global__ void __launch_bounds__(COPY_THREADS) pages_copy_kernel(const __grid_constant__ Tensors<MAX> t, int n_pages, const int32_t* __restrict__ src,
+                                                                 const int32_t* __restrict__ dst, const int32_t* __restrict__ n_at, int n_max, PagesArgs a,
+                                                                 const int* __restrict__ now, const int* __restrict__ live_at, int* status) {
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int lane = threadIdx.x & 31, warps = gridDim.x * (COPY_THREADS / 32), warp = blockIdx.x * (COPY_THREADS / 32) + (threadIdx.x >> 5);
+    if (now) {
+        const int live = *live_at;
+        const long long entries = (long long)a.S * a.max_pages;
+        for (long long i = (long long)blockIdx.x * COPY_THREADS + threadIdx.x; i < entries; i += (long long)gridDim.x * COPY_THREADS) {
+            const int page = a.table[i];
+            if (page >= live && page < a.n_pages) a.table[i] = now[page];
+        }
+    }
+    const int n = n_at ? min(*n_at, n_max) : n_max, pieces = t.first[t.n];
+    if (pieces == 0) return;
+    int pair = warp / pieces, piece = warp - pair * pieces;
+    const int step = warps / pieces, turn = warps - step * pieces;
+    while (pair < n) {
+        const int from = src[pair], to = dst[pair];
+        const bool good = (unsigned)from < (unsigned)n_pages && (unsigned)to < (unsigned)n_pages;
+        if (!good && piece == 0 && lane == 0) atomicOr(status, SPEC_STATUS_CAPACITY);
+        if (good && from != to) {
+            int lo = 0, hi = t.n;  // the tensor that the piece lies in
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (t.first[mid] <= piece) lo = mid;
+                else hi = mid;
+            }
+            const uint32_t bytes = t.bytes[lo], at = (uint32_t)(piece - t.first[lo]) * PIECE + lane * 16;
+            const char* x = t.base[lo] + (long long)from * bytes;
+            char* y = t.base[lo] + (long long)to * bytes;
+            uint4 v[PIECE / 512];
+#pragma unroll
+            for (int j = 0; j < PIECE / 512; ++j)
+                if (at + j * 512 < bytes) v[j] = *reinterpret_cast<const uint4*>(x + at + j * 512);
+#pragma unroll
+            for (int j = 0; j < PIECE / 512; ++j)
+                if (at + j * 512 < bytes) *reinterpret_cast<uint4*>(y + at + j * 512) = v[j];
+        }
+        pair += step;
+        piece += turn;
+        if (piece >= pieces) {
+            piece -= pieces;
+            ++pair;
+        }
+    }
+}
+
+template <int MAX>
+static int copy_pages(spec_ctx* ctx, const CacheArgs* caches, int n_caches, int n_pages, const int32_t* d_src, const int32_t* d_dst, const int32_t* d_n, int n_max,
+                      const PagesArgs& a, const int* now, const int* live, cudaStream_t st) {
+    Tensors<MAX> t;
+    t.n = 0;
+    t.first[0] = 0;
+    auto add = [&](void* base, long long bytes) {
+        t.base[t.n] = (char*)base;
+        t.bytes[t.n] = (uint32_t)bytes;
+        t.first[t.n + 1] = t.first[t.n] + (int)((bytes + PIECE - 1) / PIECE);
+        ++t.n;
+    };
+    for (int i = 0; i < n_caches; ++i) {
+        const CacheArgs& c = caches[i];
+        const long long vectors = (long long)c.heads << c.page_shift, codes = c.dtype == SPEC_BF16 ? 2 * c.head_dim : (c.dtype == SPEC_E4M3 ? c.head_dim : c.head_dim / 2);
+        add(c.k, vectors * codes);
+        add(c.v, vectors * codes);
+        if (c.dtype == SPEC_BF16) continue;
+        const long long scales = vectors * (c.dtype == SPEC_E4M3 ? 1 : c.head_dim / GROUP);
+        add(c.k_exp, scales);
+        add(c.v_exp, scales);
+    }
+    // (as many warps as fit: eight CTAs of 256 threads to an SM; fewer where there cannot be as many pieces)
+    const long long items = std::max((long long)n_max * t.first[t.n], now ? ((long long)a.S * a.max_pages + 31) / 32 : 0ll), per_cta = COPY_THREADS / 32;
+    const int grid = (int)std::min<long long>(8ll * ctx->num_sms, std::max<long long>(1, (items + per_cta - 1) / per_cta));
+    cudaError_t e = launch_pdl(pages_copy_kernel<MAX>, dim3(grid), dim3(COPY_THREADS), 0, st, t, n_pages, d_src, d_dst, d_n, n_max, a, now, live, ctx->d_status);
+    ++ctx->launches;
+    return check_cuda(ctx, e, "spec_pages copy launch");
+}
+// (the tensors travel as a parameter of the launch: two sizes, for a few layers and for as many as are allowed)
+static int copy_pages(spec_ctx* ctx, const CacheArgs* caches, int n_caches, int n_pages, const int32_t* d_src, const int32_t* d_dst, const int32_t* d_n, int n_max,
+                      const PagesArgs& a, const int* now, const int* live, cudaStream_t st) {
+    return n_caches <= 16 ? copy_pages<64>(ctx, caches, n_caches, n_pages, d_src, d_dst, d_n, n_max, a, now, live, st)
+                          : copy_pages<4 * SPEC_MAX_LAYERS>(ctx, caches, n_caches, n_pages, d_src, d_dst, d_n, n_max, a, now, live, st);
+}
+
+int launch_pages_copy(spec_ctx* ctx, const CacheArgs* caches, int n_caches, const int32_t* d_src, const int32_t* d_dst, const int32_t* d_n, int n_max, cudaStream_t st) {
+    return copy_pages(ctx, caches, n_caches, caches[0].n_pages, d_src, d_dst, d_n, n_max, PagesArgs{}, nullptr, nullptr, st);
+}
+
+int launch_pages_reserve(spec_ctx* ctx, const PagesArgs& a, const CacheArgs* caches, int n_caches, const int32_t* d_start, const int32_t* d_count, int32_t* d_ok,
+                         void* d_work, cudaStream_t st) {
+    const PagesWork w = pages_work(d_work, a.n_pages);
+    cudaError_t e = launch_pdl_cluster(pages_reserve_kernel, dim3(CLUSTER), dim3(PLAN_THREADS), 0, st, CLUSTER, a, w, d_start, d_count, d_ok, ctx->d_status);
+    ++ctx->launches;
+    int rc = check_cuda(ctx, e, "spec_pages_reserve launch");
+    return rc || n_caches == 0 ? rc : copy_pages(ctx, caches, n_caches, a.n_pages, w.src, w.dst, w.head, a.n_pages, a, nullptr, nullptr, st);
+}
+
+int launch_pages_compact(spec_ctx* ctx, const PagesArgs& a, const CacheArgs* caches, int n_caches, int32_t* d_n_live, void* d_work, cudaStream_t st) {
+    const PagesWork w = pages_work(d_work, a.n_pages);
+    cudaError_t e = launch_pdl_cluster(pages_compact_kernel, dim3(CLUSTER), dim3(PLAN_THREADS), 0, st, CLUSTER, a, w, d_n_live);
+    ++ctx->launches;
+    const int rc = check_cuda(ctx, e, "spec_pages_compact launch");
+    return rc ? rc : copy_pages(ctx, caches, n_caches, a.n_pages, w.src, w.dst, w.head, a.n_pages, a, w.list, w.head + 1, st);
+}
+
+}  // namespace ngs
