@@ -730,7 +730,7 @@ class SpecContext:
             if out[1] is not None:
                 _out(out[1], q.shape[:3], torch.float32, "tree_attention: lse")
         if work is None:
-            key = (S, N, Hq, cache.heads, D)
+            key = (S, N, Hq, cache.heads, D, cache._struct.dtype)
             need = self._work_bytes.get(key)
             if need is None:
                 need = self._lib.spec_tree_attention_bytes(self._h, cache._ref, S, N, Hq)

@@ -49,6 +49,7 @@
 
 #include "cache.cuh"
 #include "tc100.cuh"
+#include "tree_attention.cuh"
 
 namespace ngs {
 
@@ -63,17 +64,6 @@ static_assert(128 * (4 * REGS_SOFTMAX + 2 * REGS_LOADER + REGS_CONTROL) <= ATT_T
 constexpr int START = 4;  // tiles that the beginning and end of a segment take as long as (2 or 8 instead: no better)
 constexpr float RESCALE = 256.0f;  // what 32 weights may add up to before their reference is moved
 
-struct AttParams {
-    TreeAttnArgs a;
-    int G, n_qtiles, side, n_groups, passes;  // side: row-tile pairs that run side by side
-    int rows_cap;                             // rows of a partial result
-    float c;                                  // scale * log2(e)
-    struct JoinTask* tasks;                   // [grid]
-    float2* part_ml;                          // [grid * 2, rows_cap]
-    float* part_o;                            // [grid * 2, D / 4, rows_cap, 4]
-    unsigned long long wait_limit_ns;
-};
-
 // A run of key tiles [t0, t1) of one (s, h) against one row-tile pair.
 struct Segment {
     int s, h, qt, t0, t1, n_prefix, len, live, rows;
@@ -82,13 +72,6 @@ struct Segment {
     int slot;   // partial result: 0 = the CTA's range starts here, 1 = it ends here
     int more;   // 0: there was none left
     int first;  // tile t >= n_prefix is the block's tile t - first
-};
-// An (s, h) and row-tile pair that several CTAs walked: its partial rows are joined.  Recorded by the second of them.
-struct __align__(16) JoinTask {
-    int s, h, qt, rows;
-    int n;      // parts; 0: nothing to join
-    int first;  // slot of the first CTA's part
-    int pad[2];
 };
 struct AttShared {
     uint64_t full[8], empty[8], go[8], stg_full[6], stg_empty[6], s_full[2], p_full[2], o_full, q_full, xch, seg_full[SEGMENTS], seg_empty[SEGMENTS];
@@ -139,27 +122,6 @@ __device__ __forceinline__ int sequence_tiles(const TreeAttnArgs& a, int s, int&
 }
 
 __device__ __forceinline__ int places(int n_tiles) { return n_tiles ? n_tiles + START : 0; }
-
-// Quotient of numbers that nearly always fit in 32 bits (a 64-bit division is a long subroutine).
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
-}
-// The work is cut where it costs the same: every (s, h) counts as START places more than it has tiles, for what it takes to
-// begin and end a segment (its places first), and the places [0, total) are cut into equal consecutive ranges: the first
-// `rem` groups have base + 1 places, the others base.  With fewer places than groups, as many groups as places have one.
-struct Ranges {
-    long long total, n, base, rem;
-    __device__ __forceinline__ Ranges(const AttParams& p, long long total_) : total(total_), n(min((long long)p.n_groups, total_)), base(0), rem(0) {
-        if (n) {
-            base = quotient(total, n);
-            rem = total - base * n;
-        }
-    }
-    __device__ __forceinline__ long long begin(long long g) const { return g * base + min(g, rem); }
-    __device__ __forceinline__ long long group_of(long long x) const {
-        return x < rem * (base + 1) ? quotient(x, base + 1) : rem + quotient(x - rem * (base + 1), base);
-    }
-};
 
 // The planning warp's place in the CTA's range.
 struct Walk {
@@ -1025,7 +987,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             }
             const long long per_pass = (sum + __shfl_sync(0xffffffffu, first_upto, 31)) * cache.heads, total = per_pass * p.passes;
-            const Ranges ranges(p, total);
+            const Ranges ranges(p.n_groups, total);
             const long long group = min((long long)(blockIdx.x / p.side), ranges.n);
             Walk w;
             w.pos = ranges.begin(group);
@@ -1088,10 +1050,11 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 if (!more) break;
             }
             if (lane == 0) {
-                JoinTask task = {s, h, first_pass * p.side + (int)(blockIdx.x % p.side), 0, 0, 0, {0, 0}};
-                if (inside && u0 + START >= ranges.begin(group - 1) && task.qt < p.n_qtiles) {
+                const int qt = first_pass * p.side + (int)(blockIdx.x % p.side);
+                JoinTask task = {s, h, qt * 2 * TILE, 0, 0, 0, {0, 0}};
+                if (inside && u0 + START >= ranges.begin(group - 1) && qt < p.n_qtiles) {
                     const int n = places(sequence_tiles(a, s, len, live, np));
-                    task.rows = min(2 * TILE, live * p.G - task.qt * 2 * TILE);
+                    task.rows = min(2 * TILE, live * p.G - task.row0);
                     task.n = task.rows > 0 ? (int)(ranges.group_of(u0 + n - 1) - group) + 2 : 0;
                     task.first = u0 > ranges.begin(group - 1);  // that range begins with another (s, h)
                 }
@@ -1148,7 +1111,7 @@ __global__ void __launch_bounds__(2 * D) join_kernel(const __grid_constant__ Att
     if (n == 0 || rows <= 0) return;
     const int bits = rows > 16 ? 5 : (rows > 8 ? 4 : (rows > 4 ? 3 : 2)), lanes = 1 << bits, sharers = 32 >> bits;  // lanes: for distinct rows
     const int r = r0 + min(lane & (lanes - 1), rows - 1), mine = lane >> bits;
-    const int R = task.qt * 2 * TILE + r, node = R / p.G, gq = R - node * p.G;
+    const int R = task.row0 + r, node = R / p.G, gq = R - node * p.G;
     const long long out_row = ((long long)task.s * a.N + node) * a.Hq + task.h * p.G + gq;
     uint4* out = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + out_row * D + 16 * cols);
     const long long at0 = 2ll * (cta - p.side) + task.first, at1 = 2ll * cta;
@@ -1217,7 +1180,17 @@ static void plan(int num_sms, int S, int N, int Hq, int heads, int head_dim, Att
     bytes = tasks + parts * (head_dim * 4 + 8);
 }
 
-size_t tree_attention_bytes(int num_sms, int S, int N, int Hq, int heads, int head_dim) {
+int launch_join(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
+    if (p.n_groups == 1) return SPEC_OK;  // nothing is spread
+    const dim3 grid((p.n_groups - 1) * p.side, (p.rows_cap + 31) / 32);
+    const int D = p.a.cache.head_dim;
+    const cudaError_t e = D == 64 ? launch_pdl(join_kernel<64>, grid, dim3(2 * D), 0, st, p) : launch_pdl(join_kernel<128>, grid, dim3(2 * D), 0, st, p);
+    ++ctx->launches;
+    return check_cuda(ctx, e, "spec_tree_attention join launch");
+}
+
+size_t tree_attention_bytes(int num_sms, int S, int N, int Hq, int heads, int head_dim, int dtype) {
+    if (dtype == SPEC_E2M1 && few_rows(N, Hq, heads)) return few_rows_bytes(num_sms, N, Hq, heads, head_dim);
     AttParams p;
     size_t bytes;
     plan(num_sms, S, N, Hq, heads, head_dim, p, bytes);
@@ -1280,13 +1253,11 @@ static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
     cudaError_t e = launch_pdl(kernel, dim3(p.n_groups * p.side), dim3(ATT_THREADS), (size_t)Geometry<D, DTYPE>::SMEM, st, tm_k, tm_v, tm_bk, tm_bv, p);
     if ((rc = check_cuda(ctx, e, "spec_tree_attention launch"))) return rc;
     ++ctx->launches;
-    if (p.n_groups == 1) return SPEC_OK;  // nothing is spread
-    e = launch_pdl(join_kernel<D>, dim3((p.n_groups - 1) * p.side, (p.rows_cap + 31) / 32), dim3(2 * D), 0, st, p);
-    ++ctx->launches;
-    return check_cuda(ctx, e, "spec_tree_attention join launch");
+    return launch_join(ctx, p, st);
 }
 
 int launch_tree_attention(spec_ctx* ctx, const TreeAttnArgs& a, cudaStream_t st) {
+    if (a.cache.dtype == SPEC_E2M1 && few_rows(a.N, a.Hq, a.cache.heads)) return launch_few_rows(ctx, a, st);
     AttParams p;
     size_t bytes;
     plan(ctx->num_sms, a.S, a.N, a.Hq, a.cache.heads, a.cache.head_dim, p, bytes);

@@ -1,0 +1,55 @@
+// What the two forms of tree attention share: how work is cut into ranges, and how the parts of rows that several CTAs
+// walked are joined.
+#pragma once
+#include "cache.cuh"
+
+namespace ngs {
+
+struct AttParams {
+    TreeAttnArgs a;
+    int G, n_qtiles, side, n_groups, passes;  // side: row-tile pairs that run side by side
+    int rows_cap;                             // rows of a partial result
+    float c;                                  // scale * log2(e)
+    struct JoinTask* tasks;                   // [grid]
+    float2* part_ml;                          // [grid * 2, rows_cap]
+    float* part_o;                            // [grid * 2, D / 4, rows_cap, 4]
+    unsigned long long wait_limit_ns;
+};
+
+// An (s, h) and row tiles that several CTAs walked: their partial rows are joined.  Recorded by the second of them.
+struct __align__(16) JoinTask {
+    int s, h, row0, rows;  // rows [row0, row0 + rows)
+    int n;      // parts; 0: nothing to join
+    int first;  // slot of the first CTA's part
+    int pad[2];
+};
+
+// Quotient of numbers that nearly always fit in 32 bits (a 64-bit division is a long subroutine).
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+// The work is cut where it costs the same: every (s, h) counts as some places more than it has tiles, for what it takes to
+// begin and end a segment (these places first), and the places [0, total) are cut into equal consecutive ranges: the first
+// `rem` groups have base + 1 places, the others base.  With fewer places than groups, as many groups as places have one.
+struct Ranges {
+    long long total, n, base, rem;
+    __device__ __forceinline__ Ranges(int n_groups, long long total_) : total(total_), n(min((long long)n_groups, total_)), base(0), rem(0) {
+        if (n) {
+            base = quotient(total, n);
+            rem = total - base * n;
+        }
+    }
+    __device__ __forceinline__ long long begin(long long g) const { return g * base + min(g, rem); }
+    __device__ __forceinline__ long long group_of(long long x) const {
+        return x < rem * (base + 1) ? quotient(x, base + 1) : rem + quotient(x - rem * (base + 1), base);
+    }
+};
+
+int launch_join(spec_ctx* ctx, const AttParams& p, cudaStream_t st);
+
+// tree_attention_few.cu: few rows for each key head over a 4-bit cache
+bool few_rows(int N, int Hq, int heads);
+size_t few_rows_bytes(int num_sms, int N, int Hq, int heads, int head_dim);
+int launch_few_rows(spec_ctx* ctx, const TreeAttnArgs& a, cudaStream_t st);
+
+}  // namespace ngs

@@ -1,0 +1,657 @@
+// Tree attention over a 4-bit cache for few rows to a key head: plain decoding, and small blocks of drafted nodes.
+//
+// The mathematics is that of tree_attention.cu.  There, tiles of 128 keys are turned into bfloat16 in shared memory for
+// products of 128 rows; with 4 or 8 rows hardly any of that work is needed, and the time to turn a tile over is what is
+// measured.  Here a warp takes 16 keys at a time and turns their codes into half precision in registers, straight into the
+// operands of products of 16 keys with 8 rows (mma.sync: S^T = K Q^T, O^T += V^T P^T; a 128-row product of the other kind would be empty but
+// for those rows).  Nothing but codes passes through shared memory: 2304 bytes for 16 keys and values of 128.
+//
+//   order of elements   a contraction does not mind it: lane (g, t) = (lane / 4, lane % 4) has the 32 codes of key g that begin
+//                       at 32 t (16 bytes), and of the values the 16 of dimension 16 g and on of four keys (8 bytes each).
+//   half precision      code * scale has 6 significant bits and is exact in it.  Queries are bfloat16 (8 bits): a row is scaled by a power of two so that
+//                       its largest element lies in [2^14, 2^15), and elements down to 2^-24 of that stay exact, smaller ones lose bits of
+//                       no more than 2^-39 of the largest.
+//   weights             2^(s - reference) in fp32, rounded to half precision (2^-11 of each, where bfloat16 has 2^-8); their sum is
+//                       taken before.  The reference is 6 below a score that was the row's largest when it was taken, and is moved when a
+//                       weight exceeds 2^15: weights keep 11 bits down to 2^-14 (2^-20 of the largest then), and an absolute 2^-25 below.
+//   transposing P       the product leaves lane (g, t) two rows of key g; the next one takes two keys of row g: movmatrix.
+//   the block           a warp for each row, on the CUDA cores in fp32: few rows have few nodes, and what a row does not attend to is
+//                       not even read.
+//
+// Work is cut as in tree_attention.cu, with 16 keys as the unit; the warps of a CTA take every eighth of its keys, each with
+// a reference, sum and output of its own, which are joined in shared memory at the end of an (s, h).  Copies (cp.async) run STAGES - 1
+// units ahead.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "tc100.cuh"
+#include "tree_attention.cuh"
+
+namespace ngs {
+
+constexpr int UNIT = 16;           // keys that a warp takes at a time
+constexpr int FEW_START = 20;      // units that the beginning and end of a segment take as long as
+constexpr float BIAS = 6.0f;       // a fresh reference lies that far below the largest score, in powers of two
+constexpr float WEIGHT_MAX = 32768.0f;
+constexpr float NO_SCORE = -3e38f;  // reference of a row without one: the first score exceeds any limit from there
+
+template <int D_, int NT_>
+struct Few {
+    static constexpr int D = D_, NT = NT_, ROWS = 8 * NT;           // rows that a CTA handles
+    static constexpr int WARPS = NT == 1 ? 8 : 12, CTAS = NT == 1 ? 2 : 1;  // CTAs of an SM: 128 or 168 registers per thread
+    static constexpr int THREADS = 32 * WARPS;
+    static constexpr int CODES = D / 2, SCALES = D / GROUP;         // bytes of a vector
+    static constexpr int K_AT = 0, V_AT = UNIT * CODES, KS_AT = 2 * UNIT * CODES, VS_AT = KS_AT + UNIT * SCALES, STAGE = VS_AT + UNIT * SCALES;
+    static constexpr int STAGES = 4;
+    static constexpr int ROW = D + 4;                               // floats of a row that waits to be joined (conflict-free)
+    static constexpr int RING = WARPS * STAGES * STAGE, JOIN = (WARPS + 1) * ROWS * ROW * 4;
+    static constexpr int SMEM = RING > JOIN ? RING : JOIN;
+    static_assert(CTAS * (SMEM + 8192) <= 227 * 1024, "shared memory");
+};
+
+struct FewSegment {
+    int s, h, row0, rows;  // rows [row0, row0 + rows) of the (s, h)
+    int t0, t1, n_units;   // units of 16 positions; unit n_units is the block
+    int len, live, whole, slot, more;
+};
+
+__device__ __forceinline__ int few_units(const TreeAttnArgs& a, int s, int& len, int& live) {  // of the context; -1: no live node
+    len = a.len[s];
+    live = a.n_nodes ? min(max(a.n_nodes[s], 0), a.N) : a.N;
+    if (len < 0 || (long long)len > ((long long)a.cache.max_pages << a.cache.page_shift)) len = live = 0;
+    return live == 0 ? -1 : (len + UNIT - 1) / UNIT;
+}
+__device__ __forceinline__ int few_places(int units) { return units < 0 ? 0 : units + 1 + FEW_START; }
+
+struct FewWalk {
+    int s, h, t, slot;  // h: key head and row tile, key head first
+    long long pos, hi;
+};
+template <int ROWS>
+__device__ __forceinline__ void few_advance(const AttParams& p, FewWalk& w, FewSegment& g) {
+    int rows = 0;
+    while (w.pos < w.hi && rows <= 0) {
+        int len, live;
+        const int units = few_units(p.a, w.s, len, live), n = few_places(units);
+        if (w.t < n) {
+            const int take = (int)min((long long)(n - w.t), w.hi - w.pos);
+            g.t0 = max(w.t - FEW_START, 0);
+            g.t1 = w.t + take - FEW_START;
+            if (g.t1 > g.t0) {
+                g.h = w.h / p.n_qtiles;
+                g.row0 = (w.h - g.h * p.n_qtiles) * ROWS;
+                rows = min(ROWS, live * p.G - g.row0);
+                g.s = w.s;
+                g.n_units = units;
+                g.len = len;
+                g.live = live;
+                g.whole = g.t1 - g.t0 == units + 1;
+                g.slot = w.slot;
+                w.slot = 1;
+            }
+            w.pos += take;
+            w.t += take;
+        }
+        if (w.t >= n) {
+            w.t = 0;
+            if (n == 0 || ++w.h == p.a.cache.heads * p.n_qtiles) {
+                w.h = 0;
+                ++w.s;
+                if (w.s == p.a.S) break;
+            }
+        }
+    }
+    g.rows = rows;
+    g.more = rows > 0;
+}
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {  // (zeros if it is not)
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Four bytes of two codes each as half precision.
+__device__ __forceinline__ void e2m1x8_f16x8(uint32_t w, uint32_t (&h)[4]) {
+    asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
+        " cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}\n"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(w));
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// A scale byte as half precision; beyond the largest: NaN.
+__device__ __forceinline__ uint32_t scale_f16(uint32_t byte) { return byte > S4_MAX ? 0x7E00u : byte << 7; }
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+template <int BYTES>
+__device__ __forceinline__ void ld_words(uint32_t addr, uint32_t (&w)[BYTES / 4]) {
+    if constexpr (BYTES == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
+    if constexpr (BYTES == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr) : "memory");
+    if constexpr (BYTES == 4) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t ld_byte(uint32_t addr) {
+    uint32_t b;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(b) : "r"(addr) : "memory");
+    return b;
+}
+
+template <class F>
+__global__ void __launch_bounds__(F::THREADS, F::CTAS) few_rows_kernel(const __grid_constant__ AttParams p) {
+    constexpr int D = F::D, NT = F::NT, ROWS = F::ROWS, WARPS = F::WARPS, KC = D / 4, VC = D / 8;  // codes of a lane: of a key, of a value
+    constexpr int TILES = D / 16;  // products of 16 along the head
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ FewSegment segments[2];
+    __shared__ float2 parts[WARPS + 1][ROWS];  // reference and sum of each warp's part of a row; the last: the block's
+    const TreeAttnArgs& a = p.a;
+    const CacheArgs& cache = a.cache;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    grid_dependency_wait();
+    grid_launch_dependents();
+
+    // ---- this CTA's range
+    FewWalk w;  // (of thread 0)
+    if (warp == 0) {
+        int len, live;
+        long long sum = 0;
+        const int all = cache.heads * p.n_qtiles;
+        const int n_first = lane < a.S ? few_places(few_units(a, lane, len, live)) : 0;
+        auto scan = [&](int n) {  // inclusive
+            long long upto = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long other = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += other;
+            }
+            return upto;
+        };
+        for (int s = lane + 32; s < a.S; s += 32) sum += few_places(few_units(a, s, len, live));
+        const long long first_upto = scan(n_first);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const long long total = (sum + __shfl_sync(0xffffffffu, first_upto, 31)) * all;
+        // (a unit for each warp at least: shorter ranges only leave more parts to join)
+        const Ranges ranges((int)min((long long)p.n_groups, max(total / WARPS, 1ll)), total);
+        const long long group = min((long long)blockIdx.x, ranges.n);
+        w.pos = ranges.begin(group);
+        w.hi = group < ranges.n ? ranges.begin(group + 1) : w.pos;
+        w.s = w.h = w.t = w.slot = 0;
+        int mine = 0;
+        long long before = 0;
+        for (int s0 = 0; s0 < a.S; s0 += 32) {
+            const int s = s0 + lane;
+            const int n = s0 == 0 ? n_first : (s < a.S ? few_places(few_units(a, s, len, live)) : 0);
+            const long long upto = before + (s0 == 0 ? first_upto : scan(n)), from = (upto - n) * all;
+            if (n > 0 && w.pos >= from && w.pos < upto * all) {
+                mine = 1;
+                w.s = s;
+                w.h = (int)quotient(w.pos - from, n);
+                w.t = (int)(w.pos - from - (long long)w.h * n);
+            }
+            before = __shfl_sync(0xffffffffu, upto, 31);
+            if (before * all > w.pos) break;
+        }
+        const unsigned who = __ballot_sync(0xffffffffu, mine);
+        const int src = who ? __ffs(who) - 1 : 0;
+        w.s = __shfl_sync(0xffffffffu, w.s, src);
+        w.h = __shfl_sync(0xffffffffu, w.h, src);
+        w.t = __shfl_sync(0xffffffffu, w.t, src);
+        if (lane == 0) {
+            JoinTask task = {w.s, w.h / p.n_qtiles, (w.h % p.n_qtiles) * ROWS, 0, 0, 0, {0, 0}};
+            const long long u0 = w.pos - w.t;  // the first place of the (s, h)
+            if (w.pos < w.hi && w.t > FEW_START && u0 + FEW_START >= ranges.begin(group - 1)) {
+                const int n = few_places(few_units(a, w.s, len, live));
+                task.rows = min(ROWS, live * p.G - task.row0);
+                task.n = task.rows > 0 ? (int)(ranges.group_of(u0 + n - 1) - group) + 2 : 0;
+                task.first = u0 > ranges.begin(group - 1);
+            }
+            p.tasks[blockIdx.x] = task;
+            few_advance<ROWS>(p, w, segments[0]);
+        }
+    }
+    __syncthreads();
+
+    const uint32_t ring = smem_u32(smem) + warp * (F::STAGES * F::STAGE);
+    float* const join = reinterpret_cast<float*>(smem);  // [WARPS + 1, ROWS, ROW], over the rings when they are done with
+    // key rows of a product: lane group g has key key_of(g) (and the same of the second eight), so that a value's two neighbours, rows 2 t and
+    // 2 t + 1, are keys t and 7 - t: neither keys nor values meet in banks
+    const int key = (g & 1) ? 7 - (g >> 1) : g >> 1;
+
+    for (int n_seg = 0;; ++n_seg) {
+        const FewSegment seg = segments[n_seg & 1];
+        if (!seg.more) break;
+        const int end = min(seg.t1, seg.n_units), first = seg.t0 + warp;
+        const int n_mine = first < end ? (end - first + WARPS - 1) / WARPS : 0;
+        const int32_t* table = cache.table + (long long)seg.s * cache.max_pages;
+        const int unit_shift = cache.page_shift - 4, in_page = (1 << cache.page_shift) - 1;
+        auto page_of = [&](int k) { return k < n_mine ? table[(first + k * WARPS) >> unit_shift] : 0; };
+        int pages = page_of(lane), pages_next = page_of(32 + lane);
+        uint32_t bad = 0;  // units in flight whose page is not one of the pool's
+        auto issue = [&](int k) {
+            if (k < n_mine) {
+                if ((k & 31) == 0 && k > 0) {
+                    pages = pages_next;
+                    pages_next = page_of(k + 32 + lane);
+                }
+                const int page = __shfl_sync(0xffffffffu, pages, k & 31);
+                const bool good = (unsigned)page < (unsigned)cache.n_pages;
+                const uint32_t bit = 1u << (k % F::STAGES);
+                bad = good ? bad & ~bit : bad | bit;
+                if (!good && lane == 0) atomicOr(a.status, SPEC_STATUS_CAPACITY);
+                const long long row = (((long long)(good ? page : 0) * cache.heads + seg.h) << cache.page_shift) + (((first + k * WARPS) * UNIT) & in_page);
+                const uint32_t dst = ring + (k % F::STAGES) * F::STAGE;
+                const char *kc = (const char*)cache.k + row * F::CODES, *vc = (const char*)cache.v + row * F::CODES;
+#pragma unroll
+                for (int i = lane; i < UNIT * F::CODES / 16; i += 32) {
+                    // (values: two of four rows' pieces change places, for the banks)
+                    const int swap = D == 128 ? ((i >> 3) & 1) << 1 : 0;
+                    copy16(dst + F::K_AT + i * 16, kc + i * 16, good);
+                    copy16(dst + F::V_AT + (i ^ swap) * 16, vc + i * 16, good);
+                }
+                constexpr int SP = UNIT * F::SCALES / 16;  // pieces of the scales
+                if (lane < 2 * SP) {
+                    const char* sc = lane < SP ? (const char*)cache.k_exp + row * F::SCALES + lane * 16 : (const char*)cache.v_exp + row * F::SCALES + (lane - SP) * 16;
+                    copy16(dst + F::KS_AT + lane * 16, sc, good);
+                }
+            }
+            copies_commit();
+        };
+#pragma unroll
+        for (int k = 0; k < F::STAGES - 1; ++k) issue(k);
+        if (threadIdx.x == 0) few_advance<ROWS>(p, w, segments[(n_seg + 1) & 1]);  // (read after the next barriers)
+
+        // ---- queries: row 8 j + g, elements [KC t, KC t + KC), half precision times a power of two; c: score to powers of two
+        uint32_t q[NT][TILES][2];
+        float c[NT][2];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int r = 8 * j + g, R = seg.row0 + r, node = R / p.G, gq = R - node * p.G;
+            uint4 x[KC / 8];
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < KC / 8; ++i) {
+                x[i] = make_uint4(0, 0, 0, 0);
+                if (r < seg.rows)
+                    x[i] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + ((long long)seg.s * a.N + node) * a.q_tok + (long long)(seg.h * p.G + gq) * a.q_head +
+                                                           KC * t + 8 * i);
+                top = __vmaxu2(top, __vmaxu2(__vmaxu2(x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu), __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu)));
+            }
+            top = max(top & 0xFFFFu, top >> 16);
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int e = min(141 - (int)(top >> 7), 126);  // 2^e brings the largest to [2^14, 2^15)
+            const float f = __uint_as_float((uint32_t)(e + 127) << 23);
+#pragma unroll
+            for (int i = 0; i < KC / 8; ++i) {
+                const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) q[j][2 * i + k / 2][k & 1] = pack_f16x2(__uint_as_float(v[k] << 16) * f, __uint_as_float(v[k] & 0xFFFF0000u) * f);
+            }
+            const float cr = p.c * __uint_as_float((uint32_t)(127 - e) << 23);
+            c[j][0] = __shfl_sync(0xffffffffu, cr, 8 * t);
+            c[j][1] = __shfl_sync(0xffffffffu, cr, 8 * t + 4);
+        }
+
+        // ---- the block: a warp for each row; lane: D / 32 columns
+        constexpr int BC = D / 32, PER = (ROWS + WARPS - 1) / WARPS;
+        const bool block = seg.t1 > seg.n_units;
+        float bo[PER][BC], bm[PER], bl[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            bm[j] = NO_SCORE;
+            bl[j] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < BC; ++i) bo[j][i] = 0.0f;
+            const int r = warp + j * WARPS;
+            if (!block || r >= seg.rows) continue;
+            const int R = seg.row0 + r, node = R / p.G, gq = R - node * p.G;
+            auto columns = [&](const void* x, float (&y)[BC]) {
+                if constexpr (BC == 4) {
+                    const uint2 v = *reinterpret_cast<const uint2*>((const __nv_bfloat16*)x + 4 * lane);
+                    y[0] = __uint_as_float(v.x << 16), y[1] = __uint_as_float(v.x & 0xFFFF0000u);
+                    y[2] = __uint_as_float(v.y << 16), y[3] = __uint_as_float(v.y & 0xFFFF0000u);
+                } else {
+                    const uint32_t v = *reinterpret_cast<const uint32_t*>((const __nv_bfloat16*)x + 2 * lane);
+                    y[0] = __uint_as_float(v << 16), y[1] = __uint_as_float(v & 0xFFFF0000u);
+                }
+            };
+            float qr[BC];
+            columns((const __nv_bfloat16*)a.q + ((long long)seg.s * a.N + node) * a.q_tok + (long long)(seg.h * p.G + gq) * a.q_head, qr);
+            const int words = (a.N + 31) / 32;
+            for (int b = 0; b < words; ++b) {
+                uint32_t bits = (uint32_t)a.mask[((long long)seg.s * a.N + node) * words + b];
+                const int left = seg.live - 32 * b;
+                if (left < 32) bits &= left <= 0 ? 0u : (1u << left) - 1u;
+                for (; bits; bits &= bits - 1) {
+                    const long long tok = (long long)seg.s * a.N + 32 * b + __ffs(bits) - 1;
+                    float kk[BC], vv[BC], x = 0.0f;
+                    columns((const __nv_bfloat16*)a.k + tok * a.k_tok + (long long)seg.h * a.k_head, kk);
+                    columns((const __nv_bfloat16*)a.v + tok * a.v_tok + (long long)seg.h * a.v_head, vv);
+#pragma unroll
+                    for (int i = 0; i < BC; ++i) x = fmaf(qr[i], kk[i], x);
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+                    x *= p.c;
+                    const float m = fmaxf(bm[j], x), f = exp2_approx(bm[j] - m), y = exp2_approx(x - m);
+                    bm[j] = m;
+                    bl[j] = bl[j] * f + y;
+#pragma unroll
+                    for (int i = 0; i < BC; ++i) bo[j][i] = bo[j][i] * f + y * vv[i];
+                }
+            }
+        }
+
+        // ---- the context, 16 keys at a time
+        float o[NT][TILES][4], m[NT][2], l[NT][2];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            m[j][0] = m[j][1] = NO_SCORE;
+            l[j][0] = l[j][1] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) o[j][i][0] = o[j][i][1] = o[j][i][2] = o[j][i][3] = 0.0f;
+        }
+#pragma unroll 1
+        for (int k = 0; k < n_mine; ++k) {
+            const bool missing = (bad >> (k % F::STAGES)) & 1u;
+            copies_wait<F::STAGES - 2>();
+            __syncwarp();  // the unit is there for all lanes, and all have read the one before, which the next copies overwrite
+            issue(k + F::STAGES - 1);
+            const uint32_t at = ring + (k % F::STAGES) * F::STAGE;
+            const int left = seg.len - (first + k * WARPS) * UNIT;  // keys that are there; may exceed the unit
+            // ---- scores
+            float s[NT][4];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.0f;
+            {
+                uint32_t ka[KC / 8], kb[KC / 8];
+                ld_words<KC / 2>(at + F::K_AT + key * F::CODES + t * (KC / 2), ka);
+                ld_words<KC / 2>(at + F::K_AT + (key + 8) * F::CODES + t * (KC / 2), kb);
+                uint32_t fa[KC / GROUP], fb[KC / GROUP];
+#pragma unroll
+                for (int i = 0; i < KC / GROUP; ++i) {
+                    fa[i] = scale_f16(ld_byte(at + F::KS_AT + key * F::SCALES + t * (KC / GROUP) + i)) * 0x00010001u;
+                    fb[i] = scale_f16(ld_byte(at + F::KS_AT + (key + 8) * F::SCALES + t * (KC / GROUP) + i)) * 0x00010001u;
+                }
+#pragma unroll
+                for (int i = 0; i < KC / 8; ++i) {  // 8 codes: two products
+                    uint32_t ha[4], hb[4];
+                    e2m1x8_f16x8(ka[i], ha);
+                    e2m1x8_f16x8(kb[i], hb);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const uint32_t op[4] = {mul_f16x2(ha[2 * x], fa[i / 2]), mul_f16x2(hb[2 * x], fb[i / 2]), mul_f16x2(ha[2 * x + 1], fa[i / 2]),
+                                                mul_f16x2(hb[2 * x + 1], fb[i / 2])};
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) mma(s[j], op, q[j][2 * i + x][0], q[j][2 * i + x][1]);
+                    }
+                }
+            }
+            // ---- weights
+            uint32_t pt[NT][2];
+            const bool hide = missing || left < UNIT;
+            bool grown = false;
+            float e[NT][4];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[j][i] *= c[j][i & 1];
+                    if (hide && (missing || key + (i & 2) * 4 >= left)) s[j][i] = -INFINITY;
+                    e[j][i] = exp2_approx(s[j][i] - m[j][i & 1]);
+                    grown |= e[j][i] > WEIGHT_MAX;
+                }
+            }
+            if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float top = fmaxf(s[j][i], s[j][i + 2]);
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16)) - BIAS;
+                        const float now = fmaxf(m[j][i], top), f = exp2_approx(m[j][i] - now);
+                        m[j][i] = now;
+                        l[j][i] *= f;
+#pragma unroll
+                        for (int d = 0; d < TILES; ++d) {
+                            o[j][d][i] *= f;
+                            o[j][d][i + 2] *= f;
+                        }
+                        e[j][i] = exp2_approx(s[j][i] - now);
+                        e[j][i + 2] = exp2_approx(s[j][i + 2] - now);
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                l[j][0] += e[j][0] + e[j][2];
+                l[j][1] += e[j][1] + e[j][3];
+                pt[j][0] = transposed(pack_f16x2(e[j][0], e[j][1]));
+                pt[j][1] = transposed(pack_f16x2(e[j][2], e[j][3]));
+            }
+            // ---- outputs: keys t and 7 - t of both eights
+            {
+                const int ka = t, kb = 7 - t;
+                uint32_t va[VC / 8], vb[VC / 8], vc[VC / 8], vd[VC / 8];
+                auto value = [&](int kk, uint32_t (&x)[VC / 8]) {
+                    const uint32_t piece = D == 128 ? (uint32_t)(((g >> 1) ^ (((kk >> 1) & 1) << 1)) * 16 + (g & 1) * 8) : (uint32_t)(g * 4);
+                    ld_words<VC / 2>(at + F::V_AT + kk * F::CODES + piece, x);
+                };
+                value(ka, va);
+                value(kb, vb);
+                value(ka + 8, vc);
+                value(kb + 8, vd);
+                auto scale = [&](int kk) {  // (0 where there is no key: what lies there may be anything)
+                    const uint32_t b = ld_byte(at + F::VS_AT + kk * F::SCALES + g * VC / GROUP);
+                    return left < UNIT && kk >= left ? 0u : scale_f16(b);
+                };
+                const uint32_t fab = scale(ka) | (scale(kb) << 16), fcd = scale(ka + 8) | (scale(kb + 8) << 16);
+#pragma unroll
+                for (int i = 0; i < VC / 8; ++i) {
+                    // the codes of two keys for one dimension in one byte: even dimensions, then odd ones
+                    constexpr uint32_t LOW = 0x0F0F0F0Fu;
+                    uint32_t ab0[4], ab1[4], cd0[4], cd1[4];
+                    e2m1x8_f16x8((va[i] & LOW) | ((vb[i] << 4) & ~LOW), ab0);
+                    e2m1x8_f16x8(((va[i] >> 4) & LOW) | (vb[i] & ~LOW), ab1);
+                    e2m1x8_f16x8((vc[i] & LOW) | ((vd[i] << 4) & ~LOW), cd0);
+                    e2m1x8_f16x8(((vc[i] >> 4) & LOW) | (vd[i] & ~LOW), cd1);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const uint32_t op[4] = {mul_f16x2(ab0[x], fab), mul_f16x2(ab1[x], fab), mul_f16x2(cd0[x], fcd), mul_f16x2(cd1[x], fcd)};
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) mma(o[j][4 * i + x], op, pt[j][0], pt[j][1]);
+                    }
+                }
+            }
+        }
+        copies_wait<0>();
+
+        // ---- join the warps' parts
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float x = l[j][i];
+                x += __shfl_xor_sync(0xffffffffu, x, 4);
+                x += __shfl_xor_sync(0xffffffffu, x, 8);
+                x += __shfl_xor_sync(0xffffffffu, x, 16);
+                if (g == 0) parts[warp][8 * j + 2 * t + i] = make_float2(m[j][i], x);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (lane == 0 && warp + j * WARPS < ROWS) parts[WARPS][warp + j * WARPS] = make_float2(bm[j], bl[j]);
+        __syncthreads();
+        auto reference = [&](int r) {
+            float top = NO_SCORE;
+            for (int i = 0; i <= WARPS; ++i) top = fmaxf(top, parts[i][r].x);
+            return top;
+        };
+        // (a part's element pair d, d + 1 with d = VC g + 2 i lies at 16 i + 2 g of its row: lanes side by side)
+        if (n_mine > 0) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int r = 8 * j + 2 * t + i;
+                    if (r >= seg.rows) continue;
+                    const float f = exp2_approx(m[j][i] - reference(r));
+                    float* dst = join + (warp * ROWS + r) * F::ROW + 2 * g;
+#pragma unroll
+                    for (int d = 0; d < TILES; ++d) *reinterpret_cast<float2*>(dst + 16 * d) = make_float2(o[j][d][i] * f, o[j][d][i + 2] * f);
+                }
+            }
+        }
+        if (block) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                const int r = warp + j * WARPS;
+                if (r >= seg.rows) continue;
+                const float f = exp2_approx(bm[j] - reference(r));
+                float* dst = join + (WARPS * ROWS + r) * F::ROW;
+#pragma unroll
+                for (int i = 0; i < BC; i += 2) {
+                    const int d = BC * lane + i;
+                    *reinterpret_cast<float2*>(dst + (d % VC) * 8 + (d / VC) * 2) = make_float2(bo[j][i] * f, bo[j][i + 1] * f);
+                }
+            }
+        }
+        __syncthreads();
+        const int busy = min(max(end - seg.t0, 0), WARPS);  // warps that had a unit: the first ones
+        for (int i = threadIdx.x; i < seg.rows * (D / 4); i += F::THREADS) {
+            const int r = i / (D / 4), d = 4 * (i - r * (D / 4));
+            const float top = reference(r);
+            float4 x = make_float4(0, 0, 0, 0);
+            float sum = 0.0f;
+            const float* src = join + r * F::ROW + (d % VC) * 8 + (d / VC) * 2;
+            auto add = [&](int part) {
+                const float2 u = *reinterpret_cast<const float2*>(src + part * (ROWS * F::ROW)), v = *reinterpret_cast<const float2*>(src + part * (ROWS * F::ROW) + 16);
+                x.x += u.x;
+                x.y += u.y;
+                x.z += v.x;
+                x.w += v.y;
+                const float2 ml = parts[part][r];
+                sum += ml.y * exp2_approx(ml.x - top);
+            };
+            for (int part = 0; part < busy; ++part) add(part);
+            if (block) add(WARPS);
+            const int R = seg.row0 + r, node = R / p.G, gq = R - node * p.G;
+            if (seg.whole) {
+                const long long row = ((long long)seg.s * a.N + node) * a.Hq + seg.h * p.G + gq;
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                const __nv_bfloat162 lo = __floats2bfloat162_rn(x.x * inv, x.y * inv), hi = __floats2bfloat162_rn(x.z * inv, x.w * inv);
+                *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + row * D + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+                if (a.lse && d == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
+            } else {
+                const long long part = (long long)blockIdx.x * 2 + seg.slot;
+                reinterpret_cast<float4*>(p.part_o)[(part * (D / 4) + d / 4) * p.rows_cap + r] = x;
+                if (d == 0) p.part_ml[part * p.rows_cap + r] = make_float2(sum == 0.0f ? -INFINITY : top, sum);
+            }
+        }
+        __syncthreads();
+    }
+
+    // ---- nodes that are not live
+    const long long n_nodes = (long long)a.S * a.N;
+    for (long long i0 = 32ll * (blockIdx.x * WARPS + warp); i0 < n_nodes; i0 += 32ll * WARPS * gridDim.x) {
+        const long long i = i0 + lane;
+        bool blank = false;
+        if (i < n_nodes) {
+            const int s = (int)quotient(i, a.N), node = (int)(i - (long long)s * a.N);
+            int len, live;
+            few_units(a, s, len, live);
+            blank = node >= live;
+            if (node == 0 && (a.len[s] < 0 || (long long)a.len[s] > ((long long)cache.max_pages << cache.page_shift))) atomicOr(a.status, SPEC_STATUS_CAPACITY);
+        }
+        for (unsigned left = __ballot_sync(0xffffffffu, blank); left; left &= left - 1) {
+            const long long at = (i0 + __ffs(left) - 1) * a.Hq;
+            uint4* out = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + at * D);
+            for (int j = lane; j < a.Hq * (D / 8); j += 32) out[j] = make_uint4(0, 0, 0, 0);
+            if (a.lse)
+                for (int j = lane; j < a.Hq; j += 32) a.lse[at + j] = -INFINITY;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ host
+constexpr int FEW_ROWS = 32;
+bool few_rows(int N, int Hq, int heads) { return (long long)N * (Hq / heads) <= FEW_ROWS; }
+
+static void few_plan(int num_sms, int N, int Hq, int heads, int head_dim, AttParams& p, size_t& bytes) {
+    p.G = Hq / heads;
+    const int rows = N * p.G, tile = rows <= 8 ? 8 : 16;
+    p.n_qtiles = (rows + tile - 1) / tile;
+    p.side = p.passes = 1;
+    p.n_groups = num_sms * (rows <= 8 ? 2 : 1);
+    p.rows_cap = std::min(tile, rows);
+    const size_t parts = (size_t)p.n_groups * 2 * p.rows_cap, tasks = (size_t)p.n_groups * sizeof(JoinTask);
+    p.tasks = nullptr;
+    p.part_o = reinterpret_cast<float*>(tasks);
+    p.part_ml = reinterpret_cast<float2*>(tasks + parts * head_dim * 4);
+    bytes = tasks + parts * (head_dim * 4 + 8);
+}
+size_t few_rows_bytes(int num_sms, int N, int Hq, int heads, int head_dim) {
+    AttParams p;
+    size_t bytes;
+    few_plan(num_sms, N, Hq, heads, head_dim, p, bytes);
+    return bytes;
+}
+
+template <class F>
+static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
+    auto kernel = few_rows_kernel<F>;
+    {
+        static bool done[64] = {false};
+        std::lock_guard<std::mutex> lock(host_mutex());
+        bool& d = done[ctx->device & 63];
+        if (!d) {
+            const int rc = check_cuda(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM), "spec_tree_attention: cudaFuncSetAttribute");
+            if (rc) return rc;
+            d = true;
+        }
+    }
+    const cudaError_t e = launch_pdl(kernel, dim3(p.n_groups), dim3(F::THREADS), (size_t)F::SMEM, st, p);
+    const int rc = check_cuda(ctx, e, "spec_tree_attention launch");
+    if (rc) return rc;
+    ++ctx->launches;
+    AttParams j = p;
+    j.c = 1.0f;  // (references are in powers of two here)
+    return launch_join(ctx, j, st);
+}
+
+int launch_few_rows(spec_ctx* ctx, const TreeAttnArgs& a, cudaStream_t st) {
+    AttParams p;
+    size_t bytes;
+    few_plan(ctx->num_sms, a.N, a.Hq, a.cache.heads, a.cache.head_dim, p, bytes);
+    p.a = a;
+    p.c = a.scale * LOG2E;
+    p.tasks = reinterpret_cast<JoinTask*>(a.work);
+    p.part_o = reinterpret_cast<float*>((char*)a.work + (size_t)p.part_o);
+    p.part_ml = reinterpret_cast<float2*>((char*)a.work + (size_t)p.part_ml);
+    p.wait_limit_ns = ctx->wait_limit_ns;
+    const bool one = a.N * p.G <= 8;
+    if (a.cache.head_dim == 64) return one ? launch<Few<64, 1>>(ctx, p, st) : launch<Few<64, 2>>(ctx, p, st);
+    return one ? launch<Few<128, 1>>(ctx, p, st) : launch<Few<128, 2>>(ctx, p, st);
+}
+
+}  // namespace ngs
