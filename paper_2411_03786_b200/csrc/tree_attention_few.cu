@@ -20,12 +20,13 @@
 //
 // Work is cut as in tree_attention.cu, with 16 keys as the unit; the warps of a CTA take every eighth of its keys, each with
 // a reference, sum and output of its own, which are joined in shared memory at the end of an (s, h).  Copies (cp.async) run STAGES - 1
-// units ahead.
+// steps ahead.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "tc100.cuh"
 #include "tree_attention.cuh"
@@ -45,11 +46,12 @@ struct Few {
     static constexpr int THREADS = 32 * WARPS;
     static constexpr int CODES = D / 2, SCALES = D / GROUP;         // bytes of a vector
     static constexpr int K_AT = 0, V_AT = UNIT * CODES, KS_AT = 2 * UNIT * CODES, VS_AT = KS_AT + UNIT * SCALES, STAGE = VS_AT + UNIT * SCALES;
-    static constexpr int STAGES = 4;
+    static constexpr int STEP = 2;                                  // units that a warp works on at a time
+    static constexpr int STAGES = NT == 1 ? 3 : 2;                  // steps in shared memory
     static constexpr int ROW = D + 4;                               // floats of a row that waits to be joined (conflict-free)
-    static constexpr int RING = WARPS * STAGES * STAGE, JOIN = (WARPS + 1) * ROWS * ROW * 4;
+    static constexpr int RING = WARPS * STAGES * STEP * STAGE, JOIN = (WARPS + 1) * ROWS * ROW * 4;
     static constexpr int SMEM = RING > JOIN ? RING : JOIN;
-    static_assert(CTAS * (SMEM + 8192) <= 227 * 1024, "shared memory");
+    static_assert(CTAS * (SMEM + 3072) <= 228 * 1024, "shared memory");
 };
 
 struct FewSegment {
@@ -108,8 +110,9 @@ __device__ __forceinline__ void few_advance(const AttParams& p, FewWalk& w, FewS
     g.more = rows > 0;
 }
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {  // (zeros if it is not)
-    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+template <int AT>
+__device__ __forceinline__ void copy16(uint32_t dst, const char* src, int from) {
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0 + %2], [%1], 16;" ::"r"(dst), "l"(src + from), "n"(AT) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -126,13 +129,19 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
+__device__ __forceinline__ uint32_t mul_one(int which, uint32_t a, uint32_t b) {  // by the lower or the upper half of b
+    const __half2 f = *reinterpret_cast<const __half2*>(&b);
+    const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), which ? __high2half2(f) : __low2half2(f));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// A scale byte as half precision; beyond the largest: NaN.
-__device__ __forceinline__ uint32_t scale_f16(uint32_t byte) { return byte > S4_MAX ? 0x7E00u : byte << 7; }
+// Two scales in half precision, of which those of bytes beyond the largest become NaN; that some are is seen in the largest of many.
+__device__ __forceinline__ uint32_t beyond(uint32_t f) { return (f + (0x8000u - ((S4_MAX + 1) << 7)) * 0x00010001u) & 0x80008000u; }
+__device__ __forceinline__ void to_nan(uint32_t& f) { f |= (beyond(f) >> 15) * 0x7E00u; }
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -143,15 +152,22 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-template <int BYTES>
+template <int BYTES, int AT>
 __device__ __forceinline__ void ld_words(uint32_t addr, uint32_t (&w)[BYTES / 4]) {
-    if constexpr (BYTES == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
-    if constexpr (BYTES == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr) : "memory");
-    if constexpr (BYTES == 4) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(addr) : "memory");
+    if constexpr (BYTES == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4 + %5];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr), "n"(AT) : "memory");
+    if constexpr (BYTES == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2 + %3];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr), "n"(AT) : "memory");
+    if constexpr (BYTES == 4) asm volatile("ld.shared.b32 %0, [%1 + %2];" : "=r"(w[0]) : "r"(addr), "n"(AT) : "memory");
 }
+template <int AT>
 __device__ __forceinline__ uint32_t ld_byte(uint32_t addr) {
     uint32_t b;
-    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(b) : "r"(addr) : "memory");
+    asm volatile("ld.shared.u8 %0, [%1 + %2];" : "=r"(b) : "r"(addr), "n"(AT) : "memory");
+    return b;
+}
+template <int AT>
+__device__ __forceinline__ uint32_t ld_half(uint32_t addr) {
+    uint32_t b;
+    asm volatile("ld.shared.u16 %0, [%1 + %2];" : "=r"(b) : "r"(addr), "n"(AT) : "memory");
     return b;
 }
 
@@ -230,7 +246,7 @@ __global__ void __launch_bounds__(F::THREADS, F::CTAS) few_rows_kernel(const __g
     }
     __syncthreads();
 
-    const uint32_t ring = smem_u32(smem) + warp * (F::STAGES * F::STAGE);
+    const uint32_t ring = smem_u32(smem) + warp * (F::STAGES * F::STEP * F::STAGE);
     float* const join = reinterpret_cast<float*>(smem);  // [WARPS + 1, ROWS, ROW], over the rings when they are done with
     // key rows of a product: lane group g has key key_of(g) (and the same of the second eight), so that a value's two neighbours, rows 2 t and
     // 2 t + 1, are keys t and 7 - t: neither keys nor values meet in banks
@@ -243,40 +259,66 @@ __global__ void __launch_bounds__(F::THREADS, F::CTAS) few_rows_kernel(const __g
         const int n_mine = first < end ? (end - first + WARPS - 1) / WARPS : 0;
         const int32_t* table = cache.table + (long long)seg.s * cache.max_pages;
         const int unit_shift = cache.page_shift - 4, in_page = (1 << cache.page_shift) - 1;
-        auto page_of = [&](int k) { return k < n_mine ? table[(first + k * WARPS) >> unit_shift] : 0; };
-        int pages = page_of(lane), pages_next = page_of(32 + lane);
-        uint32_t bad = 0;  // units in flight whose page is not one of the pool's
-        auto issue = [&](int k) {
-            if (k < n_mine) {
-                if ((k & 31) == 0 && k > 0) {
-                    pages = pages_next;
-                    pages_next = page_of(k + 32 + lane);
-                }
-                const int page = __shfl_sync(0xffffffffu, pages, k & 31);
-                const bool good = (unsigned)page < (unsigned)cache.n_pages;
-                const uint32_t bit = 1u << (k % F::STAGES);
-                bad = good ? bad & ~bit : bad | bit;
-                if (!good && lane == 0) atomicOr(a.status, SPEC_STATUS_CAPACITY);
-                const long long row = (((long long)(good ? page : 0) * cache.heads + seg.h) << cache.page_shift) + (((first + k * WARPS) * UNIT) & in_page);
-                const uint32_t dst = ring + (k % F::STAGES) * F::STAGE;
-                const char *kc = (const char*)cache.k + row * F::CODES, *vc = (const char*)cache.v + row * F::CODES;
+        // where unit k of this warp lies, counted in vectors: lanes have those of 32 units.  Negative: to be hidden in part (-1 - where it lies:
+        // the context ends there) or, in no page of the pool, as a whole (MISSING: vectors 0 to 15 are read in its place)
+        constexpr int MISSING = (int)0x80000000;
+        auto row_of = [&](int k) {
+            if (k >= n_mine) return 0;
+            const int unit = first + k * WARPS, page = table[unit >> unit_shift];
+            const int row = ((page * cache.heads + seg.h) << cache.page_shift) + ((unit * UNIT) & in_page);  // (below 2^31)
+            return (unsigned)page >= (unsigned)cache.n_pages ? MISSING : (unit * UNIT + UNIT > seg.len ? -1 - row : row);
+        };
+        int rows_at = row_of(lane), rows_next = row_of(32 + lane);
+        uint32_t odd = 0, gone = 0;  // units in flight that are to be hidden in part or as a whole: a bit for each place
+        constexpr int SP = UNIT * F::SCALES / 16;  // pieces of 16 bytes of a unit's scales
+        const char *k_from = (const char*)cache.k + lane * 16, *v_from = (const char*)cache.v + lane * 16;
+        const char* s_from = (const char*)(lane < SP ? cache.k_exp : cache.v_exp) + (lane % SP) * 16;
+        const bool has_scales = lane < 2 * SP;
+        int k_next = 0;
+        uint32_t dst = ring + lane * 16, place = 0;  // of the step that is copied next
+        auto issue = [&]() {  // (past the last unit nothing is copied, and what lies there is hidden)
 #pragma unroll
-                for (int i = lane; i < UNIT * F::CODES / 16; i += 32) {
-                    // (values: two of four rows' pieces change places, for the banks)
-                    const int swap = D == 128 ? ((i >> 3) & 1) << 1 : 0;
-                    copy16(dst + F::K_AT + i * 16, kc + i * 16, good);
-                    copy16(dst + F::V_AT + (i ^ swap) * 16, vc + i * 16, good);
-                }
-                constexpr int SP = UNIT * F::SCALES / 16;  // pieces of the scales
-                if (lane < 2 * SP) {
-                    const char* sc = lane < SP ? (const char*)cache.k_exp + row * F::SCALES + lane * 16 : (const char*)cache.v_exp + row * F::SCALES + (lane - SP) * 16;
-                    copy16(dst + F::KS_AT + lane * 16, sc, good);
+            for (int i = 0; i < F::STEP; ++i) {
+                if (k_next < n_mine) {
+                    int row = __shfl_sync(0xffffffffu, rows_at, k_next & 31);
+                    if (row < 0) {
+                        odd |= 1u << (place + i);
+                        if (row == MISSING) {
+                            gone |= 1u << (place + i);
+                            if (lane == 0) atomicOr(a.status, SPEC_STATUS_CAPACITY);
+                            row = -1;
+                        }
+                        row = -1 - row;
+                    }
+                    const char *kc = k_from + (long long)row * F::CODES, *vc = v_from + (long long)row * F::CODES, *sc = s_from + (long long)row * F::SCALES;
+                    const uint32_t to = dst + i * F::STAGE;
+                    copy16<F::K_AT>(to, kc, 0);
+                    copy16<F::V_AT>(to, vc, 0);
+                    if (F::V_AT > 512) {
+                        copy16<F::K_AT + 512>(to, kc, 512);
+                        copy16<F::V_AT + 512>(to, vc, 512);
+                    }
+                    if (has_scales) copy16<F::KS_AT>(to, sc, 0);
+                    ++k_next;
+                    if ((k_next & 31) == 0) {
+                        rows_at = rows_next;
+                        rows_next = row_of(k_next + 32 + lane);
+                    }
+                } else {
+                    gone |= 1u << (place + i);
+                    odd |= 1u << (place + i);
                 }
             }
             copies_commit();
+            dst += F::STEP * F::STAGE;
+            place += F::STEP;
+            if (place == F::STAGES * F::STEP) {
+                place = 0;
+                dst = ring + lane * 16;
+            }
         };
 #pragma unroll
-        for (int k = 0; k < F::STAGES - 1; ++k) issue(k);
+        for (int k = 0; k < F::STAGES - 1; ++k) issue();
         if (threadIdx.x == 0) few_advance<ROWS>(p, w, segments[(n_seg + 1) & 1]);  // (read after the next barriers)
 
         // ---- queries: row 8 j + g, elements [KC t, KC t + KC), half precision times a power of two; c: score to powers of two
@@ -306,7 +348,8 @@ __global__ void __launch_bounds__(F::THREADS, F::CTAS) few_rows_kernel(const __g
 #pragma unroll
                 for (int k = 0; k < 4; ++k) q[j][2 * i + k / 2][k & 1] = pack_f16x2(__uint_as_float(v[k] << 16) * f, __uint_as_float(v[k] & 0xFFFF0000u) * f);
             }
-            const float cr = p.c * __uint_as_float((uint32_t)(127 - e) << 23);
+            // (never 0 or infinite, as for a row of zeros: hidden scores are -infinity, and others may be 0)
+            const float cr = fminf(fmaxf(p.c * __uint_as_float((uint32_t)(127 - e) << 23), 0x1p-126f), 0x1p127f);
             c[j][0] = __shfl_sync(0xffffffffu, cr, 8 * t);
             c[j][1] = __shfl_sync(0xffffffffu, cr, 8 * t + 4);
         }
@@ -369,28 +412,71 @@ __global__ void __launch_bounds__(F::THREADS, F::CTAS) few_rows_kernel(const __g
 #pragma unroll
             for (int i = 0; i < TILES; ++i) o[j][i][0] = o[j][i][1] = o[j][i][2] = o[j][i][3] = 0.0f;
         }
+        uint32_t here = 0;  // place of the step that is worked on
 #pragma unroll 1
-        for (int k = 0; k < n_mine; ++k) {
-            const bool missing = (bad >> (k % F::STAGES)) & 1u;
-            copies_wait<F::STAGES - 2>();
-            __syncwarp();  // the unit is there for all lanes, and all have read the one before, which the next copies overwrite
-            issue(k + F::STAGES - 1);
-            const uint32_t at = ring + (k % F::STAGES) * F::STAGE;
-            const int left = seg.len - (first + k * WARPS) * UNIT;  // keys that are there; may exceed the unit
-            // ---- scores
-            float s[NT][4];
+        for (int k = 0; k < n_mine; k += F::STEP) {
+            int left[F::STEP];  // keys that are there
 #pragma unroll
-            for (int j = 0; j < NT; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.0f;
-            {
-                uint32_t ka[KC / 8], kb[KC / 8];
-                ld_words<KC / 2>(at + F::K_AT + key * F::CODES + t * (KC / 2), ka);
-                ld_words<KC / 2>(at + F::K_AT + (key + 8) * F::CODES + t * (KC / 2), kb);
-                uint32_t fa[KC / GROUP], fb[KC / GROUP];
+            for (int u = 0; u < F::STEP; ++u) left[u] = UNIT;
+            const bool hide = (odd >> here) & ((1u << F::STEP) - 1u);
+            if (hide) {
 #pragma unroll
-                for (int i = 0; i < KC / GROUP; ++i) {
-                    fa[i] = scale_f16(ld_byte(at + F::KS_AT + key * F::SCALES + t * (KC / GROUP) + i)) * 0x00010001u;
-                    fb[i] = scale_f16(ld_byte(at + F::KS_AT + (key + 8) * F::SCALES + t * (KC / GROUP) + i)) * 0x00010001u;
+                for (int u = 0; u < F::STEP; ++u) {
+                    const uint32_t bit = 1u << (here + u);
+                    left[u] = (gone & bit) ? 0 : min(seg.len - (first + (k + u) * WARPS) * UNIT, UNIT);
+                    odd &= ~bit;
+                    gone &= ~bit;
                 }
+            }
+            copies_wait<F::STAGES - 2>();
+            __syncwarp();  // the step is there for all lanes, and all have read the one before, which the next copies overwrite
+            issue();
+            const uint32_t at = ring + here * F::STAGE;
+            here = here + F::STEP == F::STAGES * F::STEP ? 0 : here + F::STEP;
+            // ---- scales, two to a word: of a key's two groups (head size 64: of its one), and of a group of two values
+            uint32_t fa[F::STEP], fb[F::STEP], fv[F::STEP][2];
+            {
+                const uint32_t ks = at + key * F::SCALES + t * (KC / GROUP), va = at + g * VC / GROUP + t * F::SCALES, vb = at + g * VC / GROUP + (7 - t) * F::SCALES;
+                uint32_t most = 0;
+                auto load = [&](auto unit) {
+                    constexpr int u = decltype(unit)::value, K0 = u * F::STAGE + F::KS_AT, V0 = u * F::STAGE + F::VS_AT;
+                    if constexpr (KC / GROUP == 2) {
+                        fa[u] = __byte_perm(ld_half<K0>(ks), 0, 0x4140) * 0x80u;
+                        fb[u] = __byte_perm(ld_half<K0 + 8 * F::SCALES>(ks), 0, 0x4140) * 0x80u;
+                    } else {
+                        fa[u] = ld_byte<K0>(ks) * 0x80u;
+                        fb[u] = ld_byte<K0 + 8 * F::SCALES>(ks) * 0x80u;
+                    }
+                    fv[u][0] = ld_byte<V0>(va) * 0x80u + ld_byte<V0>(vb) * 0x800000u;
+                    fv[u][1] = ld_byte<V0 + 8 * F::SCALES>(va) * 0x80u + ld_byte<V0 + 8 * F::SCALES>(vb) * 0x800000u;
+                    if (hide) {  // (0 where there is no key: what lies there may be anything)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) fv[u][i] &= (t + 8 * i < left[u] ? 0xFFFFu : 0u) | (7 - t + 8 * i < left[u] ? 0xFFFF0000u : 0u);
+                    }
+                    most = __vmaxu2(most, __vmaxu2(__vmaxu2(fa[u], fb[u]), __vmaxu2(fv[u][0], fv[u][1])));
+                };
+                load(std::integral_constant<int, 0>());
+                load(std::integral_constant<int, 1>());
+                if (beyond(most)) {
+#pragma unroll
+                    for (int u = 0; u < F::STEP; ++u) {
+                        to_nan(fa[u]);
+                        to_nan(fb[u]);
+                        to_nan(fv[u][0]);
+                        to_nan(fv[u][1]);
+                    }
+                }
+            }
+            // ---- scores
+            float s[F::STEP][NT][4];
+            auto scores = [&](auto unit) {
+                constexpr int u = decltype(unit)::value;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) s[u][j][0] = s[u][j][1] = s[u][j][2] = s[u][j][3] = 0.0f;
+                uint32_t ka[KC / 8], kb[KC / 8];
+                const uint32_t from = at + key * F::CODES + t * (KC / 2);
+                ld_words<KC / 2, u * F::STAGE + F::K_AT>(from, ka);
+                ld_words<KC / 2, u * F::STAGE + F::K_AT + 8 * F::CODES>(from, kb);
 #pragma unroll
                 for (int i = 0; i < KC / 8; ++i) {  // 8 codes: two products
                     uint32_t ha[4], hb[4];
@@ -398,34 +484,41 @@ __global__ void __launch_bounds__(F::THREADS, F::CTAS) few_rows_kernel(const __g
                     e2m1x8_f16x8(kb[i], hb);
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const uint32_t op[4] = {mul_f16x2(ha[2 * x], fa[i / 2]), mul_f16x2(hb[2 * x], fb[i / 2]), mul_f16x2(ha[2 * x + 1], fa[i / 2]),
-                                                mul_f16x2(hb[2 * x + 1], fb[i / 2])};
+                        const uint32_t op[4] = {mul_one(i / 2, ha[2 * x], fa[u]), mul_one(i / 2, hb[2 * x], fb[u]), mul_one(i / 2, ha[2 * x + 1], fa[u]),
+                                                mul_one(i / 2, hb[2 * x + 1], fb[u])};
 #pragma unroll
-                        for (int j = 0; j < NT; ++j) mma(s[j], op, q[j][2 * i + x][0], q[j][2 * i + x][1]);
+                        for (int j = 0; j < NT; ++j) mma(s[u][j], op, q[j][2 * i + x][0], q[j][2 * i + x][1]);
                     }
                 }
-            }
+            };
+            scores(std::integral_constant<int, 0>());
+            scores(std::integral_constant<int, 1>());
             // ---- weights
-            uint32_t pt[NT][2];
-            const bool hide = missing || left < UNIT;
-            bool grown = false;
-            float e[NT][4];
+            if (hide) {
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
+                for (int u = 0; u < F::STEP; ++u)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[j][i] *= c[j][i & 1];
-                    if (hide && (missing || key + (i & 2) * 4 >= left)) s[j][i] = -INFINITY;
-                    e[j][i] = exp2_approx(s[j][i] - m[j][i & 1]);
-                    grown |= e[j][i] > WEIGHT_MAX;
-                }
+                    for (int j = 0; j < NT; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (key + (i & 2) * 4 >= left[u]) s[u][j][i] = -INFINITY;
             }
-            if (__any_sync(0xffffffffu, grown)) {
+            float e[F::STEP][NT][4], most = 0.0f;
+#pragma unroll
+            for (int u = 0; u < F::STEP; ++u)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        e[u][j][i] = exp2_approx(fmaf(s[u][j][i], c[j][i & 1], -m[j][i & 1]));
+                        most = fmaxf(most, e[u][j][i]);
+                    }
+            if (__any_sync(0xffffffffu, most > WEIGHT_MAX)) {
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        float top = fmaxf(s[j][i], s[j][i + 2]);
+                        float top = fmaxf(fmaxf(s[0][j][i], s[0][j][i + 2]), fmaxf(s[1][j][i], s[1][j][i + 2])) * c[j][i];
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16)) - BIAS;
@@ -437,35 +530,31 @@ __global__ void __launch_bounds__(F::THREADS, F::CTAS) few_rows_kernel(const __g
                             o[j][d][i] *= f;
                             o[j][d][i + 2] *= f;
                         }
-                        e[j][i] = exp2_approx(s[j][i] - now);
-                        e[j][i + 2] = exp2_approx(s[j][i + 2] - now);
+#pragma unroll
+                        for (int u = 0; u < F::STEP; ++u) {
+                            e[u][j][i] = exp2_approx(fmaf(s[u][j][i], c[j][i], -now));
+                            e[u][j][i + 2] = exp2_approx(fmaf(s[u][j][i + 2], c[j][i], -now));
+                        }
                     }
                 }
             }
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                l[j][0] += e[j][0] + e[j][2];
-                l[j][1] += e[j][1] + e[j][3];
-                pt[j][0] = transposed(pack_f16x2(e[j][0], e[j][1]));
-                pt[j][1] = transposed(pack_f16x2(e[j][2], e[j][3]));
-            }
             // ---- outputs: keys t and 7 - t of both eights
-            {
-                const int ka = t, kb = 7 - t;
+            auto outputs = [&](auto unit) {
+                constexpr int u = decltype(unit)::value, V0 = u * F::STAGE + F::V_AT;
+                uint32_t pt[NT][2];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    l[j][0] += e[u][j][0] + e[u][j][2];
+                    l[j][1] += e[u][j][1] + e[u][j][3];
+                    pt[j][0] = transposed(pack_f16x2(e[u][j][0], e[u][j][1]));
+                    pt[j][1] = transposed(pack_f16x2(e[u][j][2], e[u][j][3]));
+                }
                 uint32_t va[VC / 8], vb[VC / 8], vc[VC / 8], vd[VC / 8];
-                auto value = [&](int kk, uint32_t (&x)[VC / 8]) {
-                    const uint32_t piece = D == 128 ? (uint32_t)(((g >> 1) ^ (((kk >> 1) & 1) << 1)) * 16 + (g & 1) * 8) : (uint32_t)(g * 4);
-                    ld_words<VC / 2>(at + F::V_AT + kk * F::CODES + piece, x);
-                };
-                value(ka, va);
-                value(kb, vb);
-                value(ka + 8, vc);
-                value(kb + 8, vd);
-                auto scale = [&](int kk) {  // (0 where there is no key: what lies there may be anything)
-                    const uint32_t b = ld_byte(at + F::VS_AT + kk * F::SCALES + g * VC / GROUP);
-                    return left < UNIT && kk >= left ? 0u : scale_f16(b);
-                };
-                const uint32_t fab = scale(ka) | (scale(kb) << 16), fcd = scale(ka + 8) | (scale(kb + 8) << 16);
+                const uint32_t a0 = at + t * F::CODES + g * (VC / 2), b0 = at + (7 - t) * F::CODES + g * (VC / 2);
+                ld_words<VC / 2, V0>(a0, va);
+                ld_words<VC / 2, V0>(b0, vb);
+                ld_words<VC / 2, V0 + 8 * F::CODES>(a0, vc);
+                ld_words<VC / 2, V0 + 8 * F::CODES>(b0, vd);
 #pragma unroll
                 for (int i = 0; i < VC / 8; ++i) {
                     // the codes of two keys for one dimension in one byte: even dimensions, then odd ones
@@ -477,12 +566,14 @@ __global__ void __launch_bounds__(F::THREADS, F::CTAS) few_rows_kernel(const __g
                     e2m1x8_f16x8(((vc[i] >> 4) & LOW) | (vd[i] & ~LOW), cd1);
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        const uint32_t op[4] = {mul_f16x2(ab0[x], fab), mul_f16x2(ab1[x], fab), mul_f16x2(cd0[x], fcd), mul_f16x2(cd1[x], fcd)};
+                        const uint32_t op[4] = {mul_f16x2(ab0[x], fv[u][0]), mul_f16x2(ab1[x], fv[u][0]), mul_f16x2(cd0[x], fv[u][1]), mul_f16x2(cd1[x], fv[u][1])};
 #pragma unroll
                         for (int j = 0; j < NT; ++j) mma(o[j][4 * i + x], op, pt[j][0], pt[j][1]);
                     }
                 }
-            }
+            };
+            outputs(std::integral_constant<int, 0>());
+            outputs(std::integral_constant<int, 1>());
         }
         copies_wait<0>();
 
