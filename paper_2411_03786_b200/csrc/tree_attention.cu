@@ -282,17 +282,36 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
 // Where 16-byte chunk `c` of row r lies in a tile: blocks of 64 elements, rows of 128 bytes, chunks swizzled by the row.
 __device__ __forceinline__ uint32_t tile_at(int r, int c) { return (uint32_t)((c >> 3) * (TILE * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
 
+// Two fp32 operations in one instruction (the issue slots are what the softmax warps share with the loaders).
+struct __align__(8) Pair {
+    float x, y;
+};
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair d;
+    asm("{\n .reg .b64 p, q, r;\n mov.b64 p, {%2, %3};\n mov.b64 q, {%4, %5};\n mov.b64 r, {%6, %7};\n fma.rn.f32x2 p, p, q, r;\n mov.b64 {%0, %1}, p;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    Pair d;
+    asm("{\n .reg .b64 p, q;\n mov.b64 p, {%2, %3};\n mov.b64 q, {%4, %5};\n add.rn.f32x2 p, p, q;\n mov.b64 {%0, %1}, p;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
 // Weights 2^(c s - mc) of 32 scores, as bfloat16, and their sum.
 __device__ __forceinline__ float weights32(const uint32_t (&s)[32], float c, float mc, uint32_t (&w)[16]) {
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    Pair sum[2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-        const float x = exp2_approx(fmaf(__uint_as_float(s[2 * j]), c, -mc)), y = exp2_approx(fmaf(__uint_as_float(s[2 * j + 1]), c, -mc));
-        sum[(2 * j) & 3] += x;
-        sum[(2 * j + 1) & 3] += y;
-        w[j] = pack2(x, y);
+        Pair e = fma2({__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1])}, {c, c}, {-mc, -mc});
+        e.x = exp2_approx(e.x);
+        e.y = exp2_approx(e.y);
+        sum[j & 1] = add2(sum[j & 1], e);
+        w[j] = pack2(e.x, e.y);
     }
-    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    return (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
 }
 __device__ __forceinline__ float max32(const uint32_t (&s)[32]) {
     float m[4];
