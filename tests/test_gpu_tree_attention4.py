@@ -24,6 +24,15 @@ def i32(x):
     return torch.tensor(x, dtype=torch.int32).cuda()
 
 
+def with_small_weights(ref, held_v, v):
+    """Weights for the cached values are held in half precision with the largest at 2^6 or more: below 2^-14 they are off by up to
+    2^-25, which is 2^-31 of the largest weight, which is at most 1 of their sum.  So an output is off by up to 2^-31 of the sum of all |v|, which
+    counts where the values that matter are 0.  `check_attention` allows 2^-8 of the magnitude."""
+    S, _, Hq, _ = ref[0].shape
+    total = held_v.abs().sum(1) + v.double().cpu().abs().sum(1)  # [S, heads, D]
+    return ref[0], ref[1], ref[2] + 2.0 ** (8 - 31) * total.repeat_interleave(Hq // v.shape[2], 1)[:, None]
+
+
 def run(ctx, S, N, Hq, Hkv, D, lens, page, kind="tree", seed=0, strided=False, live=None, scale=None, gain=1.0, bound=SCORE):
     cache, hk, hv = e4.make_cache(S, max(max(lens), 1), Hkv, D, page, seed, gain=gain)
     q, k, v = block(S, N, Hq, Hkv, D, seed + 1, strided)
@@ -199,7 +208,7 @@ def test_extreme_scores(ctx, N):
     mask = au.ancestors(parents(S, N, "chain", 0))
     got = ctx.tree_attention(cache, q, k, v, au.pack(mask).cuda(), i32([L]), with_lse=True)
     # scores near 2000: fp32 leaves 2^-24 * 64 * 2000 of them at most
-    au.check_attention(got, au.attention(q, k, v, hk, hv, mask, [L], D ** -0.5), 2.0 ** -7)
+    au.check_attention(got, with_small_weights(au.attention(q, k, v, hk, hv, mask, [L], D ** -0.5), hv, v), 2.0 ** -7)
 
 
 @pytest.mark.parametrize("N", [2, 40])
