@@ -96,6 +96,21 @@ __device__ __forceinline__ uint4 rope_chunk(const uint4& chunk, uint4 other, con
     return pack_bf16x8(y);
 }
 
+// Both chunks of a half layout's pairs at once: one look at the table, and each element is unpacked once.
+__device__ __forceinline__ void rope_halves(uint4& a, uint4& b, const float2* row, int stride) {
+    float x[8], o[8], y[8], z[8];
+    unpack_bf16x8(a, x);
+    unpack_bf16x8(b, o);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float2 cs = row[j * stride];
+        y[j] = x[j] * cs.x + -o[j] * cs.y;
+        z[j] = o[j] * cs.x + x[j] * cs.y;
+    }
+    a = pack_bf16x8(y);
+    b = pack_bf16x8(z);
+}
+
 // ------------------------------------------------------------------------------------------ rotary positions
 struct RopeRows {
     const __nv_bfloat16* x;
@@ -108,7 +123,7 @@ struct RopeRows {
 // table is made: loading them after it left the kernel waiting twice (32001 tokens, 40 heads of 128: 166 us, so 123).
 constexpr int ROPE_THREADS = 512;
 template <bool INTERLEAVED>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_rows_kernel(RopeRows q, RopeRows k, int D, RopeArgs rope) {
+__global__ void __launch_bounds__(ROPE_THREADS) rope_rows_kernel(RopeRows q, RopeRows k, int D, uint32_t per_head_inv, RopeArgs rope) {
     extern __shared__ float2 table[];
     grid_dependency_wait();
     grid_launch_dependents();
@@ -118,7 +133,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_rows_kernel(RopeRows q, Rop
     const int rot_items = rope.rot / 16;
     const int items = (q.heads + k.heads) * per_head;
     const int it = blockIdx.y * blockDim.x + threadIdx.x;
-    const int h = it / per_head, i = it - h * per_head;
+    const int h = per_head == 1 ? it : (int)__umulhi((uint32_t)it, per_head_inv), i = it - h * per_head;  // it / per_head: exact below 2^18
     const bool is_q = h < q.heads;
     const RopeRows& r = is_q ? q : k;
     const int hh = is_q ? h : h - q.heads;
@@ -134,10 +149,11 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_rows_kernel(RopeRows q, Rop
     for (int j = threadIdx.x; j < half; j += blockDim.x) table[table_at(j, 8, half)] = rope_cos_sin(rope_position(rope, t, j), rope.freq[j], rope.factor);
     __syncthreads();
     if (it >= items) return;
-    if (rotated) {
-        const uint4 a0 = a;
-        a = rope_chunk<INTERLEAVED, 8>(a0, b, table, e0, half);
-        b = rope_chunk<INTERLEAVED, 8>(b, a0, table, e1, half);
+    if (rotated && INTERLEAVED) {
+        a = rope_chunk<INTERLEAVED, 8>(a, a, table, e0, half);
+        b = rope_chunk<INTERLEAVED, 8>(b, b, table, e1, half);
+    } else if (rotated) {
+        rope_halves(a, b, table + i, half / 8);
     }
     __nv_bfloat16* y = r.y + (t * r.heads + hh) * D;
     *reinterpret_cast<uint4*>(y + e0) = a;
@@ -148,12 +164,14 @@ int launch_rope_rows(spec_ctx* ctx, const RopeArgs& rope, const void* d_q, int H
                      const void* d_k, int Hkv, long long k_tok, long long k_head, void* d_k_out, int D, int T, cudaStream_t st) {
     const RopeRows q{(const __nv_bfloat16*)d_q, (__nv_bfloat16*)d_q_out, q_tok, q_head, Hq};
     const RopeRows k{(const __nv_bfloat16*)d_k, (__nv_bfloat16*)d_k_out, k_tok, k_head, Hkv};
-    const int items = (Hq + Hkv) * (D / 16);
+    const int items = (Hq + Hkv) * (D / 16);  // below 2^18: 8192 heads of 512
+    const uint32_t per_head_inv = (uint32_t)((1ull << 32) / (D / 16)) + 1u;  // (of no use for D = 16)
     // as few threads as hold all items of a token in equal slices; few tokens: smaller slices, for more of the SMs
     int slices = (items + ROPE_THREADS - 1) / ROPE_THREADS;
     slices = std::max(slices, std::min((items + 63) / 64, ctx->num_sms / T));
     const int threads = ((items + slices - 1) / slices + 31) / 32 * 32;
-    auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(T, slices), dim3(threads), sizeof(float2) * (rope.rot / 2), st, q, k, D, rope); };
+    auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(T, slices), dim3(threads), sizeof(float2) * (rope.rot / 2), st, q, k, D, per_head_inv, rope); };
+
     cudaError_t e = rope.interleaved ? go(rope_rows_kernel<true>) : go(rope_rows_kernel<false>);
     ctx->launches += 1;
     return check_cuda(ctx, e, "spec_rope_rows launch");
@@ -219,12 +237,15 @@ __device__ __forceinline__ float scale4(uint32_t byte) { return __half2float(__u
 // max / 6, rounded towards zero all the way, gives the byte or the one below it, which 6 * scale >= max (exact in fp32) decides.  A quotient x / scale
 // is rounded to a multiple of 2^-13 on the way: x has 8 significant bits and the border between two codes times a scale 7, so that
 // they differ by 2^-10 of the quotient's unit or not at all, and the error of the reciprocal (2^-20) leaves no trace: ties are ties.
-__device__ __forceinline__ uint32_t quantise4(const uint4& v, uint32_t top, uint32_t& byte) {
+__device__ __forceinline__ uint32_t scale_byte4(uint32_t top) {
     const float a = __uint_as_float(top << 16);
     uint32_t b = __half_as_ushort(__float2half_rd(__fmul_rd(a, 0x1.555554p-3f))) >> 7;
     b = min(b, S4_MAX);
     if (__half2float(__ushort_as_half((unsigned short)(b << 7))) * 6.0f < a) ++b;
-    byte = top > 0x7F80u ? 255u : min(b, S4_MAX);
+    return top > 0x7F80u ? 255u : min(b, S4_MAX);
+}
+__device__ __forceinline__ uint32_t quantise4(const uint4& v, uint32_t top, uint32_t& byte) {
+    byte = scale_byte4(top);
     const float inv = byte == 0u || byte == 255u ? 0.0f : 1.0f / scale4(byte);
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     constexpr float C = 1536.0f;  // its neighbours are 2^-13 away
@@ -235,6 +256,35 @@ __device__ __forceinline__ uint32_t quantise4(const uint4& v, uint32_t top, uint
         asm("{\n .reg .b8 q;\n cvt.rn.satfinite.e2m1x2.f32 q, %1, %2;\n cvt.u32.u8 %0, q;\n}\n" : "=r"(r[j]) : "f"(y), "f"(x));
     }
     return byte == 255u ? 0u : __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
+}
+
+// The same for a lane that has all 16 elements: the codes, two words.  (Two elements to an instruction where there are such.)
+__device__ __forceinline__ uint2 quantise_group(const uint4 (&v)[2], uint32_t& byte) {
+    const uint32_t top = max(top16(v[0]), top16(v[1])), w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+    byte = scale_byte4(top);
+    float inv;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(scale4(byte)));
+    if (byte == 0u || byte == 255u) inv = 0.0f;
+    uint2 r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t& out = i ? r.y : r.x;
+        const uint32_t* x = w + 4 * i;
+        asm("{\n .reg .b64 f, c, n, p0, p1, p2, p3;\n .reg .b32 x0, x1, x2, x3, y0, y1, y2, y3;\n .reg .f32 a, b;\n .reg .b8 q0, q1, q2, q3;\n"
+            " mov.b64 f, {%5, %5};\n mov.b64 c, {%6, %6};\n mov.b64 n, {%7, %7};\n"
+            " shl.b32 x0, %1, 16;\n and.b32 y0, %1, 0xFFFF0000;\n mov.b64 p0, {x0, y0};\n"
+            " shl.b32 x1, %2, 16;\n and.b32 y1, %2, 0xFFFF0000;\n mov.b64 p1, {x1, y1};\n"
+            " shl.b32 x2, %3, 16;\n and.b32 y2, %3, 0xFFFF0000;\n mov.b64 p2, {x2, y2};\n"
+            " shl.b32 x3, %4, 16;\n and.b32 y3, %4, 0xFFFF0000;\n mov.b64 p3, {x3, y3};\n"
+            " fma.rn.f32x2 p0, p0, f, c;\n fma.rn.f32x2 p1, p1, f, c;\n fma.rn.f32x2 p2, p2, f, c;\n fma.rn.f32x2 p3, p3, f, c;\n"
+            " add.rn.f32x2 p0, p0, n;\n add.rn.f32x2 p1, p1, n;\n add.rn.f32x2 p2, p2, n;\n add.rn.f32x2 p3, p3, n;\n"
+            " mov.b64 {a, b}, p0;\n cvt.rn.satfinite.e2m1x2.f32 q0, b, a;\n mov.b64 {a, b}, p1;\n cvt.rn.satfinite.e2m1x2.f32 q1, b, a;\n"
+            " mov.b64 {a, b}, p2;\n cvt.rn.satfinite.e2m1x2.f32 q2, b, a;\n mov.b64 {a, b}, p3;\n cvt.rn.satfinite.e2m1x2.f32 q3, b, a;\n"
+            " mov.b32 %0, {q0, q1, q2, q3};\n}\n"
+            : "=r"(out)
+            : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "f"(inv), "f"(1536.0f), "f"(-1536.0f));
+    }
+    return byte == 255u ? make_uint2(0u, 0u) : r;
 }
 
 // A CTA writes `n_tok` tokens of one sequence, all heads of K and V: the rotation table is made once per token.  A thread
@@ -344,6 +394,81 @@ __global__ void __launch_bounds__(CACHE_THREADS, 4) cache_write_kernel(CacheArgs
     }
 }
 
+// A 4-bit cache without rotation: a lane has all 16 elements of a group of K and of V, so that what it takes to find a vector's
+// places is shared by twice as many, and no lanes exchange maxima (8 prompts of 4001 tokens, 8 heads of 128: 48 -> 30 us, where the bytes take 26).
+constexpr int WRITE4_DEPTH = 2;
+// Vectors one after another, `step` apart: token and head without a division for each.
+struct VectorWalk {
+    int t, h, dt, dh, heads;
+    __device__ __forceinline__ VectorWalk(int first, int step, int heads_) : heads(heads_) {
+        t = first / heads;
+        h = first - t * heads;
+        dt = step / heads;
+        dh = step - dt * heads;
+    }
+    __device__ __forceinline__ void next() {
+        t += dt;
+        h += dh;
+        if (h >= heads) {
+            h -= heads;
+            ++t;
+        }
+    }
+};
+template <int D>
+__global__ void __launch_bounds__(CACHE_THREADS) cache_write4_kernel(CacheArgs c, const __nv_bfloat16* __restrict__ k, long long k_tok, long long k_head,
+                                                                    const __nv_bfloat16* __restrict__ v, long long v_tok, long long v_head, int N, int n, int n_tok,
+                                                                    const int32_t* __restrict__ nodes, const int32_t* __restrict__ start,
+                                                                    const int32_t* __restrict__ count, int* status) {
+    constexpr int LANES = D / GROUP, PASS = CACHE_THREADS / LANES;
+    __shared__ int dst[WRITE_MAX_TOK];   // vector of head 0 (below 2^31), -1: none
+    __shared__ int from[WRITE_MAX_TOK];  // node, -1: none
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int s = blockIdx.y, i0 = blockIdx.x * n_tok;
+    const int n_here = min(count ? min(count[s], n) : n, i0 + n_tok) - i0;
+    if (n_here <= 0) return;
+    if (threadIdx.x < n_here) {
+        const int node = nodes ? nodes[(long long)s * n + i0 + threadIdx.x] : i0 + (int)threadIdx.x;
+        const bool on = node >= 0 && node < N;
+        from[threadIdx.x] = on ? node : -1;
+        dst[threadIdx.x] = on ? (int)cache_slot(c, s, start[s] + i0 + (int)threadIdx.x, status) : -1;
+    }
+    __syncthreads();
+    const int lane = threadIdx.x % LANES;
+    k += (long long)s * N * k_tok + lane * GROUP;
+    v += (long long)s * N * v_tok + lane * GROUP;
+    uint8_t *k_at = (uint8_t*)c.k + lane * (GROUP / 2), *v_at = (uint8_t*)c.v + lane * (GROUP / 2);
+    for (VectorWalk w(threadIdx.x / LANES, PASS, c.heads); w.t < n_here;) {
+        uint4 kv[WRITE4_DEPTH][2], vv[WRITE4_DEPTH][2];
+        int at[WRITE4_DEPTH];
+#pragma unroll
+        for (int j = 0; j < WRITE4_DEPTH; ++j) {
+            at[j] = -1;
+            if (w.t < n_here && dst[w.t] >= 0) {
+                const int node = from[w.t];
+                const uint4 *x = reinterpret_cast<const uint4*>(k + node * k_tok + w.h * k_head), *y = reinterpret_cast<const uint4*>(v + node * v_tok + w.h * v_head);
+                kv[j][0] = x[0];
+                kv[j][1] = x[1];
+                vv[j][0] = y[0];
+                vv[j][1] = y[1];
+                at[j] = dst[w.t] + (w.h << c.page_shift);
+            }
+            w.next();
+        }
+#pragma unroll
+        for (int j = 0; j < WRITE4_DEPTH; ++j) {
+            if (at[j] < 0) continue;
+            uint32_t ks, vs;
+            const uint2 kq = quantise_group(kv[j], ks), vq = quantise_group(vv[j], vs);
+            *reinterpret_cast<uint2*>(k_at + (long long)at[j] * (D / 2)) = kq;
+            *reinterpret_cast<uint2*>(v_at + (long long)at[j] * (D / 2)) = vq;
+            c.k_exp[(long long)at[j] * LANES + lane] = (uint8_t)ks;
+            c.v_exp[(long long)at[j] * LANES + lane] = (uint8_t)vs;
+        }
+    }
+}
+
 // 8 E4M3 codes times a power of two, as bfloat16 (exact).  Scales beyond the format's largest read as NaN.
 __device__ __forceinline__ uint4 dequantise8(uint2 codes, uint8_t scale) {
     const float f = (int)scale > 127 + E8_MAX ? __uint_as_float(0x7FC00000u) : ldexpf(1.0f, (int)scale - 127);
@@ -399,11 +524,7 @@ __global__ void __launch_bounds__(CACHE_THREADS) cache_read_kernel(CacheArgs c, 
         const long long slot = t < n_here ? cache_slot(c, s, pos0 + t, status) : -1;
         if (slot < 0) continue;
         const long long at = slot + ((long long)h << c.page_shift);
-        if (DTYPE == SPEC_E2M1) {
-            const long long i = at * D + lane * 8;
-            kv[j] = make_uint4(*reinterpret_cast<const uint32_t*>((const uint8_t*)c.k + i / 2), 0, c.k_exp[i / GROUP], 0);
-            vv[j] = make_uint4(*reinterpret_cast<const uint32_t*>((const uint8_t*)c.v + i / 2), 0, c.v_exp[i / GROUP], 0);
-        } else if (DTYPE == SPEC_E4M3) {
+        if (DTYPE == SPEC_E4M3) {
             const uint2 kq = *reinterpret_cast<const uint2*>((const uint8_t*)c.k + at * D + lane * 8);
             const uint2 vq = *reinterpret_cast<const uint2*>((const uint8_t*)c.v + at * D + lane * 8);
             kv[j] = make_uint4(kq.x, kq.y, c.k_exp[at], 0);
@@ -417,10 +538,7 @@ __global__ void __launch_bounds__(CACHE_THREADS) cache_read_kernel(CacheArgs c, 
     for (int j = 0; j < CACHE_DEPTH; ++j) {
         const long long w = first + j * PASS;
         if (w >= vectors) continue;
-        if (DTYPE == SPEC_E2M1) {
-            kv[j] = dequantise4(kv[j].x, kv[j].z);
-            vv[j] = dequantise4(vv[j].x, vv[j].z);
-        } else if (DTYPE == SPEC_E4M3) {
+        if (DTYPE == SPEC_E4M3) {
             kv[j] = dequantise8(make_uint2(kv[j].x, kv[j].y), (uint8_t)kv[j].z);
             vv[j] = dequantise8(make_uint2(vv[j].x, vv[j].y), (uint8_t)vv[j].z);
         }
@@ -430,9 +548,72 @@ __global__ void __launch_bounds__(CACHE_THREADS) cache_read_kernel(CacheArgs c, 
     }
 }
 
+// The same of a 4-bit cache.  A lane has half a group: with a whole one its two stores leave halves of sectors (34 -> 42 us for the 8 prompts).
+constexpr int READ4_DEPTH = 4;
+template <int D>
+__global__ void __launch_bounds__(CACHE_THREADS) cache_read4_kernel(CacheArgs c, int n, int n_tok, const int32_t* __restrict__ start, const int32_t* __restrict__ count,
+                                                                   __nv_bfloat16* __restrict__ k_out, __nv_bfloat16* __restrict__ v_out, int* status) {
+    constexpr int LANES = D / 8, PASS = CACHE_THREADS / LANES;
+    __shared__ int src[WRITE_MAX_TOK];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int s = blockIdx.y, i0 = blockIdx.x * n_tok, all = min(n - i0, n_tok), n_here = (count ? min(count[s], n) : n) - i0;
+    if (threadIdx.x < all) src[threadIdx.x] = (int)threadIdx.x < n_here ? (int)cache_slot(c, s, start[s] + i0 + (int)threadIdx.x, status) : -1;
+    __syncthreads();
+    const int lane = threadIdx.x % LANES;
+    const uint8_t *k_at = (const uint8_t*)c.k + lane * 4, *v_at = (const uint8_t*)c.v + lane * 4;
+    const long long first = ((long long)s * n + i0) * c.heads * D + lane * 8;
+    k_out += first;
+    v_out += first;
+    for (VectorWalk w(threadIdx.x / LANES, PASS, c.heads); w.t < all;) {
+        uint32_t kv[READ4_DEPTH], vv[READ4_DEPTH];
+        uint32_t ks[READ4_DEPTH], vs[READ4_DEPTH];
+        int to[READ4_DEPTH];
+#pragma unroll
+        for (int j = 0; j < READ4_DEPTH; ++j) {
+            kv[j] = vv[j] = ks[j] = vs[j] = 0;
+            to[j] = -1;
+            if (w.t < all) {
+                const int slot = src[w.t];
+                to[j] = w.t * c.heads + w.h;
+                if (slot >= 0) {
+                    const int at = slot + (w.h << c.page_shift);
+                    kv[j] = *reinterpret_cast<const uint32_t*>(k_at + (long long)at * (D / 2));
+                    vv[j] = *reinterpret_cast<const uint32_t*>(v_at + (long long)at * (D / 2));
+                    ks[j] = c.k_exp[(long long)at * (D / GROUP) + lane / 2];
+                    vs[j] = c.v_exp[(long long)at * (D / GROUP) + lane / 2];
+                }
+            }
+            w.next();
+        }
+#pragma unroll
+        for (int j = 0; j < READ4_DEPTH; ++j) {
+            if (to[j] < 0) continue;
+            *reinterpret_cast<uint4*>(k_out + (long long)to[j] * D) = dequantise4(kv[j], ks[j]);
+            *reinterpret_cast<uint4*>(v_out + (long long)to[j] * D) = dequantise4(vv[j], vs[j]);
+        }
+    }
+}
+
+// Tokens of a CTA that moves a 4-bit cache's groups: some steps' worth, fewer where that would leave SMs without work.
+static int tokens4(spec_ctx* ctx, const CacheArgs& c, int S, int n, int lane_elements) {
+    const int pass = CACHE_THREADS / (c.head_dim / lane_elements);
+    const long long vectors = (long long)S * n * c.heads;
+    const int depth = (int)std::min<long long>(4, std::max<long long>(1, vectors / ((long long)pass * 4 * ctx->num_sms)));
+    return std::min(std::min(WRITE_MAX_TOK, n), std::max(1, depth * pass / c.heads));
+}
+
 int launch_cache_write(spec_ctx* ctx, const CacheArgs& c, const void* d_k, long long k_tok, long long k_head, const void* d_v,
                        long long v_tok, long long v_head, int S, int N, int n, const int32_t* d_nodes, const int32_t* d_start,
                        const int32_t* d_count, const RopeArgs& rope, cudaStream_t st) {
+    if (c.dtype == SPEC_E2M1 && rope.rot == 0) {
+        const int n_tok = tokens4(ctx, c, S, n, GROUP);
+        auto kernel = c.head_dim == 64 ? cache_write4_kernel<64> : cache_write4_kernel<128>;
+        const cudaError_t e = launch_pdl(kernel, dim3((n + n_tok - 1) / n_tok, S), dim3(CACHE_THREADS), 0, st, c, (const __nv_bfloat16*)d_k, k_tok, k_head,
+                                         (const __nv_bfloat16*)d_v, v_tok, v_head, N, n, n_tok, d_nodes, d_start, d_count, ctx->d_status);
+        ctx->launches += 1;
+        return check_cuda(ctx, e, "spec_cache_write launch");
+    }
     // tokens of a CTA: CACHE_DEPTH vectors per thread, fewer where that would leave SMs without work
     const int pass = CACHE_THREADS / (c.head_dim / 8);
     const long long vectors = (long long)S * n * c.heads;
@@ -447,7 +628,8 @@ int launch_cache_write(spec_ctx* ctx, const CacheArgs& c, const void* d_k, long 
     auto by_rope = [&](auto dim, auto quant) {
         constexpr int D = decltype(dim)::value;
         constexpr int Q = decltype(quant)::value;
-        return rope.rot == 0 ? go(cache_write_kernel<D, Q, ROPE_NONE>) : (rope.interleaved ? go(cache_write_kernel<D, Q, ROPE_PAIRS>) : go(cache_write_kernel<D, Q, ROPE_HALF>));
+        if constexpr (Q == SPEC_E2M1) return rope.interleaved ? go(cache_write_kernel<D, Q, ROPE_PAIRS>) : go(cache_write_kernel<D, Q, ROPE_HALF>);
+        else return rope.rot == 0 ? go(cache_write_kernel<D, Q, ROPE_NONE>) : (rope.interleaved ? go(cache_write_kernel<D, Q, ROPE_PAIRS>) : go(cache_write_kernel<D, Q, ROPE_HALF>));
     };
     auto by_dim = [&](auto dtype) {
         return c.head_dim == 64 ? by_rope(std::integral_constant<int, 64>(), dtype) : by_rope(std::integral_constant<int, 128>(), dtype);
@@ -461,6 +643,14 @@ int launch_cache_write(spec_ctx* ctx, const CacheArgs& c, const void* d_k, long 
 
 int launch_cache_read(spec_ctx* ctx, const CacheArgs& c, int S, int n, const int32_t* d_start, const int32_t* d_count, void* d_k_out,
                       void* d_v_out, cudaStream_t st) {
+    if (c.dtype == SPEC_E2M1) {
+        const int n_tok = tokens4(ctx, c, S, n, 8);
+        auto kernel = c.head_dim == 64 ? cache_read4_kernel<64> : cache_read4_kernel<128>;
+        const cudaError_t e = launch_pdl(kernel, dim3((n + n_tok - 1) / n_tok, S), dim3(CACHE_THREADS), 0, st, c, n, n_tok, d_start, d_count, (__nv_bfloat16*)d_k_out,
+                                         (__nv_bfloat16*)d_v_out, ctx->d_status);
+        ctx->launches += 1;
+        return check_cuda(ctx, e, "spec_cache_read launch");
+    }
     const long long per_cta = CACHE_DEPTH * (CACHE_THREADS / (c.head_dim / 8));
     const dim3 grid((unsigned)(((long long)n * c.heads + per_cta - 1) / per_cta), S);
     auto go = [&](auto kernel) {
@@ -471,9 +661,7 @@ int launch_cache_read(spec_ctx* ctx, const CacheArgs& c, int S, int n, const int
         constexpr int Q = decltype(dtype)::value;
         return c.head_dim == 64 ? go(cache_read_kernel<64, Q>) : go(cache_read_kernel<128, Q>);
     };
-    const cudaError_t e = c.dtype == SPEC_BF16   ? by_dim(std::integral_constant<int, SPEC_BF16>())
-                          : c.dtype == SPEC_E4M3 ? by_dim(std::integral_constant<int, SPEC_E4M3>())
-                                                 : by_dim(std::integral_constant<int, SPEC_E2M1>());
+    const cudaError_t e = c.dtype == SPEC_BF16 ? by_dim(std::integral_constant<int, SPEC_BF16>()) : by_dim(std::integral_constant<int, SPEC_E4M3>());
     ctx->launches += 1;
     return check_cuda(ctx, e, "spec_cache_read launch");
 }
