@@ -1209,7 +1209,7 @@ int launch_join(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
 }
 
 size_t tree_attention_bytes(int num_sms, int S, int N, int Hq, int heads, int head_dim, int dtype) {
-    if (dtype == SPEC_E2M1 && few_rows(N, Hq, heads)) return few_rows_bytes(num_sms, N, Hq, heads, head_dim);
+    if (dtype == SPEC_E2M1 && few_rows(N, Hq, heads, head_dim)) return few_rows_bytes(num_sms, N, Hq, heads, head_dim);
     AttParams p;
     size_t bytes;
     plan(num_sms, S, N, Hq, heads, head_dim, p, bytes);
@@ -1276,7 +1276,7 @@ static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
 }
 
 int launch_tree_attention(spec_ctx* ctx, const TreeAttnArgs& a, cudaStream_t st) {
-    if (a.cache.dtype == SPEC_E2M1 && few_rows(a.N, a.Hq, a.cache.heads)) return launch_few_rows(ctx, a, st);
+    if (a.cache.dtype == SPEC_E2M1 && few_rows(a.N, a.Hq, a.cache.heads, a.cache.head_dim)) return launch_few_rows(ctx, a, st);
     AttParams p;
     size_t bytes;
     plan(ctx->num_sms, a.S, a.N, a.Hq, a.cache.heads, a.cache.head_dim, p, bytes);

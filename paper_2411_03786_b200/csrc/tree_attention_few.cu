@@ -42,12 +42,13 @@ constexpr float NO_SCORE = -3e38f;  // reference of a row without one: the first
 template <int D_, int NT_>
 struct Few {
     static constexpr int D = D_, NT = NT_, ROWS = 8 * NT;           // rows that a CTA handles
-    static constexpr int WARPS = NT == 1 ? 8 : 12, CTAS = NT == 1 ? 2 : 1;  // CTAs of an SM: 128 or 168 registers per thread
+    // CTAs of an SM, and as many warps as have the registers that a row tile takes (16 rows of 128 with 12 warps: 90 us, with 8: 84)
+    static constexpr int WARPS = NT == 2 && D == 64 ? 12 : 8, CTAS = NT == 1 ? 2 : 1;
     static constexpr int THREADS = 32 * WARPS;
     static constexpr int CODES = D / 2, SCALES = D / GROUP;         // bytes of a vector
     static constexpr int K_AT = 0, V_AT = UNIT * CODES, KS_AT = 2 * UNIT * CODES, VS_AT = KS_AT + UNIT * SCALES, STAGE = VS_AT + UNIT * SCALES;
     static constexpr int STEP = 2;                                  // units that a warp works on at a time
-    static constexpr int STAGES = NT == 1 ? 3 : 2;                  // steps in shared memory
+    static constexpr int STAGES = NT == 1 ? 3 : 4;                  // steps in shared memory
     static constexpr int ROW = D + 4;                               // floats of a row that waits to be joined (conflict-free)
     static constexpr int RING = WARPS * STAGES * STEP * STAGE, JOIN = (WARPS + 1) * ROWS * ROW * 4;
     static constexpr int SMEM = RING > JOIN ? RING : JOIN;
@@ -685,8 +686,11 @@ __global__ void __launch_bounds__(F::THREADS, F::CTAS) few_rows_kernel(const __g
 }
 
 // ------------------------------------------------------------------------------------------ host
-constexpr int FEW_ROWS = 32;
-bool few_rows(int N, int Hq, int heads) { return (long long)N * (Hq / heads) <= FEW_ROWS; }
+// Up to which this form is faster: its time goes with the row tiles, the other's hardly with rows at all.  64 sequences of 2048 keys, 8 key heads,
+// head size 128: 8 rows 50 us against 135, 16 rows 84 against 137, 24 rows 170 against 138; head size 64: 28 rows 99 against 102, 56 rows
+// 191 against 104.
+constexpr int FEW_ROWS = 16;
+bool few_rows(int N, int Hq, int heads, int head_dim) { return (long long)N * (Hq / heads) <= (head_dim == 64 ? 2 * FEW_ROWS : FEW_ROWS); }
 
 static void few_plan(int num_sms, int N, int Hq, int heads, int head_dim, AttParams& p, size_t& bytes) {
     p.G = Hq / heads;
