@@ -1,6 +1,6 @@
 """Speculative decoding of a small transformer: drafting, the model call on the block of draft rows, acceptance.
 
-    python examples/speculative_transformer.py [--cache e4m3] [--steps 40]
+    python examples/speculative_transformer.py [--cache e4m3 | e2m1] [--steps 40]
 
 A step drafts B rows of w tokens from the sequence's own history and the model's bigrams, runs the model on the block of
 B * (w + 1) nodes behind the cached context (``rope_rows``, ``tree_attention``), takes the arg max of every node,
@@ -30,6 +30,11 @@ class Model:
         self.freq = (10000.0 ** (-torch.arange(0, D, 2, dtype=torch.float64) / D)).float().cuda()
         self.rope = ngs.Rope(self.freq)
         self.ctx = ngs.SpecContext(self.embed, self.unembed)
+
+    def pool(self, S, tokens, page=16, bits=4):
+        """Caches whose pages are handed out while the sequences grow: room for all of them, and for half a sequence more."""
+        per = -(-tokens // page)
+        return ngs.PagePool.empty(len(self.layers), S * per + per // 2, S, per, self.Hkv, page, self.D, bits=bits)
 
     def caches(self, S, tokens, page=16, quantised=False):
         per = -(-tokens // page)
@@ -94,15 +99,19 @@ class Model:
         return torch.nn.functional.rms_norm(x, x.shape[-1:]) @ self.unembed.float().T
 
 
-def decode(model, prompt, steps, B=6, w=4, quantised=False):
+def decode(model, prompt, steps, B=6, w=4, quantised=False, bits=None):
     """`steps` speculative steps after prompt [S, L].  Returns the histories [S, cap], their lengths, the log probabilities
-    of the committed tokens, and tokens per step."""
+    of the committed tokens, and tokens per step.  With `bits` (16, 8 or 4) the caches' pages come from a pool, as they are needed."""
     ctx, (S, L) = model.ctx, prompt.shape
     cap = (L + steps * (w + 1) + 3) // 4 * 4
     hist = torch.zeros(S, cap, dtype=torch.int32, device="cuda")
     hist[:, :L] = prompt
     lens = torch.full((S,), L, dtype=torch.int32, device="cuda")
-    caches = model.caches(S, cap, quantised=quantised)
+    pool = None if bits is None else model.pool(S, cap, bits=bits)
+    caches = model.caches(S, cap, quantised=quantised) if pool is None else pool.caches
+    if pool is not None:
+        ctx.pages_reserve(pool, torch.zeros_like(lens), lens - 1)
+    span = torch.full_like(lens, w + 1)
     ctx.build_model_ngram_tables(8, w_ext=w)
     model.read_prompt(caches, prompt[:, :-1].contiguous())
     N = B * (w + 1)
@@ -121,6 +130,8 @@ def decode(model, prompt, steps, B=6, w=4, quantised=False):
         # the accepted path: column 0 and the accepted drafts of the best row
         step = torch.arange(w + 1, device="cuda")
         nodes = torch.where(step <= accepted[:, None], best[:, None] * (w + 1) + step, -1).int()
+        if pool is not None:
+            ctx.pages_reserve(pool, cached, torch.minimum(accepted + 1, span))
         for cache, (k, v) in zip(caches, kv):
             ctx.cache_write(cache, k, v, cached, count=accepted + 1, nodes=nodes)
         at = (torch.arange(S, device="cuda")[:, None] * N + nodes.clamp(min=0)).view(-1)
@@ -131,13 +142,13 @@ def decode(model, prompt, steps, B=6, w=4, quantised=False):
 
 def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
-    ap.add_argument("--cache", choices=("bf16", "e4m3"), default="bf16")
+    ap.add_argument("--cache", choices=("bf16", "e4m3", "e2m1"), default="bf16")
     ap.add_argument("--steps", type=int, default=40)
     a = ap.parse_args()
     torch.manual_seed(0)
     model = Model()
     prompt = torch.randint(0, model.V, (4, 24), device="cuda").int().repeat(1, 3)  # something to find again
-    hist, lens, logp, rate = decode(model, prompt, a.steps, quantised=a.cache == "e4m3")
+    hist, lens, logp, rate = decode(model, prompt, a.steps, quantised=a.cache == "e4m3", bits=4 if a.cache == "e2m1" else None)
     print(f"{rate:.2f} tokens per model call, mean log probability {logp[logp < 0].mean().item():.2f}")
     for s in range(hist.shape[0]):
         print(hist[s, prompt.shape[1]: min(int(lens[s]), prompt.shape[1] + 16)].tolist(), "...")

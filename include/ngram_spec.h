@@ -411,7 +411,8 @@ int spec_cache_read(spec_ctx* ctx, const spec_kv_cache* cache, int S, int n, con
  *   spec_pages_copy     copies page d_src[i] to page d_dst[i] in all `caches`, i < min(n, d_n[0]) (d_n NULL: n).  No page may be the destination
  *                       of two, or source and destination of different ones; pairs outside the pool are skipped, with SPEC_STATUS_CAPACITY.
  * `caches`: n_caches <= SPEC_MAX_LAYERS of them, alike in n_pages and page; heads, head_dim and dtype may differ.  Their tables are not looked at.
- * None (n_caches = 0) where the caller copies by itself.  d_work: spec_pages_bytes() of scratch, 16-byte aligned, for this call alone.
+ * None (n_caches = 0) where the caller copies by itself.  d_work: spec_pages_bytes() (of any ctx, NULL too) of scratch, 16-byte aligned,
+ * for this call alone.
  */
 enum { SPEC_MAX_PAGED = 32768, SPEC_MAX_LAYERS = 128 };
 typedef struct spec_pages {
@@ -448,7 +449,9 @@ int spec_tree_mask(spec_ctx* ctx, const int32_t* d_parent, int S, int N, const i
  *   d_out [S, N, Hq, head_dim] bfloat16, d_lse [S, N, Hq] float32 or NULL, contiguous.
  *   d_work: spec_tree_attention_bytes() of scratch, 16-byte aligned, for this call alone; needs no initial value.
  * Products are bf16 x bf16 with fp32 accumulation; statistics are fp32; the weights exp(s - max) are rounded to
- * bfloat16 for their product with the values.  Results do not depend on the order in which blocks of work finish.  Outputs
+ * bfloat16 for their product with the values.  (Over a SPEC_E2M1 cache with few rows to a key head, N * Hq / heads up to 16, or 32 with a head_dim of 64, the
+ * products with what is cached are of half precision, in which codes times scales, and queries times a power of two, are exact; weights keep 11 bits down to
+ * 2^-20 of a row's largest and are off by 2^-31 of it at most below.)  Results do not depend on the order in which blocks of work finish.  Outputs
  * and scratch may not overlap what the call reads.
  */
 size_t spec_tree_attention_bytes(spec_ctx* ctx, const spec_kv_cache* cache, int S, int N, int Hq);

@@ -255,7 +255,8 @@ class KVCache:
 class PagePool:
     """The caches of a model's layers, which share one table, and who holds their pages (see ``spec_pages`` in the header).
 
-    ``refs[n_pages]`` int32 counts the table entries that name a page; None: counted from the table as it is now.
+    ``refs[n_pages]`` int32 counts the table entries that name a page; None: counted from the table as it is now.  Calls on one
+    pool have to be ordered, on one stream or by events: they change its table, and share its scratch.
     """
 
     def __init__(self, caches, refs: torch.Tensor | None = None):
@@ -276,7 +277,8 @@ class PagePool:
         self._ref = C.byref(self._struct)
         self._device = refs.device.index or 0
         self._layers = (_KVCacheStruct * len(caches))(*[x._struct for x in caches])
-        self._work_bytes = 0
+        # (scratch of its own: calls on one pool change one table, and have to follow one another anyway)
+        self._work = refs.new_empty((load_library().spec_pages_bytes(None, self._ref) + 16) // 4)
 
     @classmethod
     def empty(cls, layers: int, n_pages: int, sequences: int, max_pages: int, heads: int, page: int, head_dim: int, bits: int = 16, device="cuda") -> "PagePool":
@@ -655,13 +657,7 @@ class SpecContext:
 
     def _pages_work(self, pool: PagePool, work: torch.Tensor | None, what: str):
         _need(pool._device == self._device, f"{what}: the pool is on another device")
-        if work is not None:
-            return work, *_scratch(work, what)
-        if not pool._work_bytes:
-            pool._work_bytes = self._lib.spec_pages_bytes(self._h, pool._ref)
-        need = max(pool._work_bytes, 16)
-        work = pool.refs.new_empty((need + 3) // 4)
-        return work, work.data_ptr(), need
+        return _scratch(pool._work if work is None else work, what)
 
     def pages_assign(self, pool: PagePool, source: torch.Tensor, lens: torch.Tensor):
         """Row s of the table becomes the pages of the first ``lens[s]`` positions of row ``source[s]`` (outside the rows: none).
@@ -682,7 +678,7 @@ class SpecContext:
             out = start.new_empty((S,))
         else:
             _out(out, (S,), torch.int32, "pages_reserve: ok")
-        work, *scratch = self._pages_work(pool, work, "pages_reserve")
+        scratch = self._pages_work(pool, work, "pages_reserve")
         self._check(self._lib.spec_pages_reserve(self._h, pool._ref, pool._layers, len(pool._layers), _i32(start, "start", (S,)), _i32(count, "count", (S,)),
                                                  out.data_ptr(), *scratch, self._raw_stream()), "spec_pages_reserve")
         return out
@@ -693,7 +689,7 @@ class SpecContext:
             out = pool.refs.new_empty((1,))
         else:
             _out(out, (1,), torch.int32, "pages_compact: n_live")
-        work, *scratch = self._pages_work(pool, work, "pages_compact")
+        scratch = self._pages_work(pool, work, "pages_compact")
         self._check(self._lib.spec_pages_compact(self._h, pool._ref, pool._layers, len(pool._layers), out.data_ptr(), *scratch, self._raw_stream()), "spec_pages_compact")
         return out
 

@@ -658,7 +658,7 @@ static int check_layers(spec_ctx* ctx, const spec_kv_cache* caches, int n_caches
 
 size_t spec_pages_bytes(spec_ctx* ctx, const spec_pages* pages) {
     PagesArgs a;
-    return !ctx || check_pages(ctx, pages, "spec_pages_bytes", &a) ? 0 : pages_bytes(a.S, a.n_pages);
+    return check_pages(ctx, pages, "spec_pages_bytes", &a) ? 0 : pages_bytes(a.S, a.n_pages);
 }
 static int check_pages_work(spec_ctx* ctx, const PagesArgs& a, void* d_work, size_t bytes, const char* who) {
     if (!d_work || !aligned16(d_work)) return fail(ctx, SPEC_ERR_ARG, "%s: work must be 16-byte aligned", who);
