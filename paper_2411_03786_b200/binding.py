@@ -231,6 +231,7 @@ class KVCache:
         if four:
             self.head_dim *= 2
         self.sequences = int(table.shape[0])
+        self._device = k.device.index or 0
         ptr = lambda t: None if t is None else t.data_ptr()
         self._struct = _KVCacheStruct(ptr(k), ptr(v), ptr(k_scale if four else k_exp), ptr(v_scale if four else v_exp), ptr(table),
                                       SPEC_E2M1 if four else (SPEC_E4M3 if codes else SPEC_BF16),
@@ -630,6 +631,7 @@ class SpecContext:
         """
         _need(k.dim() == 4 and k.shape == v.shape, "cache_write: k and v must be [S, N, heads, head_dim]")
         S, N, heads, D = k.shape
+        _need(cache._device == self._device, "cache_write: the cache is on another device")
         _need(heads == cache.heads and D == cache.head_dim and S == cache.sequences, "cache_write: k and v must have the cache's heads, head_dim and sequences")
         n = N if nodes is None else nodes.shape[1]
         args = (self._h, cache._ref, *_rows(k, "k"), *_rows(v, "v"), S, N, n, _i32(nodes, "nodes", (S, n)), _i32(start, "start", (S,)), _i32(count, "count", (S,)))
@@ -644,6 +646,7 @@ class SpecContext:
     def cache_read(self, cache: KVCache, start: torch.Tensor, n: int, count: torch.Tensor | None = None, out=None):
         """Positions ``start[s] + i``, ``i < count[s]`` (``n``), as bfloat16 ``(k, v)`` ``[S, n, heads, D]``; zeros beyond."""
         S = cache.sequences
+        _need(cache._device == self._device, "cache_read: the cache is on another device")
         if out is None:
             k = torch.empty((S, n, cache.heads, cache.head_dim), dtype=torch.bfloat16, device=cache.k.device)
             out = (k, torch.empty_like(k))
@@ -716,6 +719,7 @@ class SpecContext:
         Returns ``(out[S, N, Hq, D] bfloat16, lse[S, N, Hq] float32 or None)``; ``scale`` defaults to ``D ** -0.5``.
         """
         S, N, Hq, D = q.shape
+        _need(cache._device == self._device, "tree_attention: the cache is on another device")
         _need(k.shape == v.shape and k.shape == (S, N, cache.heads, cache.head_dim) and D == cache.head_dim and S == cache.sequences,
               "tree_attention: q must be [S, N, Hq, head_dim], k and v [S, N, heads, head_dim] of the cache")
         if out is None:

@@ -8,11 +8,13 @@
 //
 //   rotary positions        y0 = (x0 cos a - x1 sin a) f, y1 = (x0 sin a + x1 cos a) f, a = pos * freq, in fp32, rounded once
 //   E4M3 vector             scale = the smallest 2^e with max |x| <= 448 * 2^e, code = E4M3 nearest to x / scale
+//   E2M1, 16 elements       scale = the smallest of 227 (four significant bits) with max |x| <= 6 * scale, code = E2M1 nearest to x / scale
 //
 // On a B200 (copies 6.5 TB/s), 8 prompts of 4001 tokens, 8 heads of 128, keys rotated on the way: written to an E4M3 cache
 // in 57 us (197 MB, 3.5 TB/s; 44 without rotation, and 44 rotated into a bfloat16 cache: only the sine and cosine of each
-// token and the conversions together are more than the loads hide), read back in 44 us (197 MB, 4.5 TB/s).  Rotation of 32001 tokens,
-// 32 + 8 heads of 128, half of each: 122 us (656 MB, 5.4 TB/s); of 32000 tokens with 3 + 1 heads of 64 or 1 + 1 of 128: 34 us
+// token and the conversions together are more than the loads hide), read back in 44 us (197 MB, 4.5 TB/s).  Without
+// rotation, to a 4-bit cache: written in 30 us, read back in 29 (168 MB each, 26 us at a copy's rate).  Rotation of 32001 tokens,
+// 32 + 8 heads of 128, half of each: 122 us (656 MB, 5.4 TB/s); 28 + 4 heads, all of each, three axes: 91 us (524 MB, 5.8 TB/s); of 32000 tokens with 3 + 1 heads of 64 or 1 + 1 of 128: 34 us
 // (33 MB, 1 TB/s: a CTA of one or two warps for each token's table).  A decode step's 48 tokens: 2 to 4 us, the launch.  Masks of 64 x 144
 // nodes: 10 us; of one chain of 4096: 242 us.
 #include <cuda_bf16.h>

@@ -22,9 +22,11 @@
 // an (s, h) leaves fp32 partial rows and their (m, l), which a second kernel joins in a fixed order.  Any mixture of
 // lengths thus occupies all SMs to within a tile, and nothing about the lengths is needed on the host.
 //
+// A 4-bit cache is read here if more than a few rows share a key head (tree_attention_few.cu has the others).
+//
 // Warps (896 threads, which share the registers unevenly): 0-7 and 8-15 softmax of stream 0 and 1 (a row's 128 scores
 // belong to two threads, of warps w and w + 4: a single warp per scheduler leaves the special function unit waiting);
-// 16-23 turn an E4M3 cache's tiles into bfloat16 (code * scale, which is exact) and mend value tiles (zeros after the
+// 16-23 turn the tiles of an E4M3 or E2M1 cache into bfloat16 (code * scale, which is exact) and mend value tiles (zeros after the
 // end of a context, and in place of what is not finite in the block); 24 TMA; 25 issues the products; 26 walks the CTA's
 // range and tells the others; 27 writes the rows of nodes that are not live.
 //
@@ -34,12 +36,15 @@
 //                               cycles for 128 vectors of 128, of which integer instructions alone would take 430 (but 11
 //                               more of them for 16 codes made 102 us 123): 16 x 8192 keys, 102 us, 2.6 TB/s of codes, no
 //                               faster than a bfloat16 cache (92 us) yet
-//   many rows, long contexts    a stream's chain scores -> weights -> outputs, of which two overlap (a key tile per 4100
-//                               cycles), and the power cap: 4 x 704 nodes, 16384 keys, 690-820 us, 0.92-1.09 PFLOP/s
+//   many rows, long contexts    a stream's chain scores -> weights -> outputs, of which two overlap (a key tile per 3300 - 4100
+//                               cycles), and the power cap: 4 x 704 nodes, 16384 keys, 670-820 us, 0.92-1.13 PFLOP/s
+//   the same, 4-bit cache       817-850 us: 4150 cycles to a key tile, of which the products' issue has 2600 (81 cycles each, 65 over a
+//                               bfloat16 cache: the loaders' reads and writes of shared memory come between its operands), weights that are not
+//                               there yet 980, tiles that are not converted yet 550.  (Without any exponential 816, without conversion 847.)
 //   prompts                     the same, with masks in every tile of the block: a chain of 4096 nodes, 32 / 8 heads, 508 us,
 //                               0.27 PFLOP/s of what is visible; 32 / 32 heads, 618 us (hidden tiles are not left out there)
 //   short contexts              a segment's beginning and end, 6-10 us where a tile takes 2: 64 x 144 nodes, 2048 keys,
-//                               bfloat16 470 us, E4M3 550-575 us
+//                               bfloat16 470 us, E4M3 545-575 us, E2M1 572 us
 //   one short call              two launches and a segment: 10-15 us
 #include <cuda_bf16.h>
 #include <math.h>
@@ -245,6 +250,8 @@ __device__ __forceinline__ uint32_t scale_bf16x2(uint32_t exp) {
 // leave bfloat16, so the tiles of a 4-bit cache hold their values times UNIT4 = 2^-20, exactly, and so do the block's beside them
 // (of which only what is below 2^-106 loses bits).  The order of elements is the one that takes no instructions (10 of the integer
 // pipe for 8 codes): queries and the block's tiles are brought into it where they are loaded, outputs back where they are stored.
+// (Half precision instead, which an instruction makes of two codes: fewer instructions, but a power of two for each query and each
+// of the block's keys, and code for both kinds of weights: 844 us at 4 x 704 nodes where this takes 849, 600 - 668 at 64 x 144 where it takes 572.)
 constexpr float UNIT4 = 0x1p-20f;
 __device__ __forceinline__ uint4 e2m1x8_bf16x8(uint32_t w, uint32_t f) {
     uint32_t a, b, c, d, e;

@@ -103,6 +103,21 @@ def test_scale_argument(ctx, N):
     run(ctx, 1, N, 2, 1, 64, [300], 16, scale=0.02)
 
 
+@pytest.mark.parametrize("N,Hq,length", [(415, 7, 0), (700, 4, 1), (1100, 1, 64)])
+def test_wide_blocks_of_rows(ctx, N, Hq, length):
+    """Blocks of many tiles of which a row attends to one or two, from the front, the middle or the end."""
+    run(ctx, 2, N, Hq, 1, 64, [length, length + 200], 32, kind="rows", seed=N, live=[N, N - 130])
+
+
+@pytest.mark.parametrize("D,N", [(64, 9), (128, 5), (64, 2)])
+def test_rows_on_both_sides_of_the_two_forms(ctx, D, N):
+    """One row tile, two, and the first sizes that the form for many rows takes."""
+    for Hq in (7, 8, 9):
+        run(ctx, 2, N, Hq, 1, D, [333, 40], 16, seed=Hq)
+    run(ctx, 3, 1, 16 if D == 128 else 32, 1, D, [333, 0, 16], 16, seed=3)
+    run(ctx, 3, 1, 17 if D == 128 else 33, 1, D, [333, 0, 16], 16, seed=3)
+
+
 @pytest.mark.parametrize("N", [5, 40])
 def test_empty_rows(ctx, N):
     """No context and a mask without a bit: zeros and -inf; other rows of the tile as usual."""
