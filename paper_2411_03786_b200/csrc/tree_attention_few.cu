@@ -59,7 +59,7 @@ struct Few {
     static constexpr int ROW = D + 4;                               // floats of a row that waits to be joined (conflict-free)
     static constexpr int RING = WARPS * STAGES * STEP * STAGE, JOIN = (WARPS + 1) * ROWS * ROW * 4;
     static constexpr int SMEM = RING > JOIN ? RING : JOIN;
-    static_assert(CTAS * (SMEM + 3072) <= 228 * 1024, "shared memory");
+    static_assert(CTAS * (SMEM + 2816) <= 228 * 1024, "shared memory");
 };
 
 struct FewSegment {
