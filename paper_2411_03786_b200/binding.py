@@ -232,10 +232,10 @@ class KVCache:
             self.head_dim *= 2
         self.sequences = int(table.shape[0])
         self._device = k.device.index or 0
+        self._dtype, self._capacity = SPEC_E2M1 if four else (SPEC_E4M3 if codes else SPEC_BF16), int(table.shape[1]) * self.page
         ptr = lambda t: None if t is None else t.data_ptr()
         self._struct = _KVCacheStruct(ptr(k), ptr(v), ptr(k_scale if four else k_exp), ptr(v_scale if four else v_exp), ptr(table),
-                                      SPEC_E2M1 if four else (SPEC_E4M3 if codes else SPEC_BF16),
-                                      self.n_pages, int(table.shape[1]), self.page, self.heads, self.head_dim)
+                                      self._dtype, self.n_pages, int(table.shape[1]), self.page, self.heads, self.head_dim)
         self._ref = C.byref(self._struct)
 
     @classmethod
@@ -730,7 +730,7 @@ class SpecContext:
             if out[1] is not None:
                 _out(out[1], q.shape[:3], torch.float32, "tree_attention: lse")
         if work is None:
-            key = (S, N, Hq, cache.heads, D, cache._struct.dtype)
+            key = (S, N, Hq, cache.heads, D, cache._dtype, cache._capacity)
             need = self._work_bytes.get(key)
             if need is None:
                 need = self._lib.spec_tree_attention_bytes(self._h, cache._ref, S, N, Hq)

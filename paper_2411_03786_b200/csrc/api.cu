@@ -741,7 +741,7 @@ static int check_block(spec_ctx* ctx, const spec_kv_cache* cache, int S, int N, 
 size_t spec_tree_attention_bytes(spec_ctx* ctx, const spec_kv_cache* cache, int S, int N, int Hq) {
     CacheArgs c;
     if (!ctx || check_block(ctx, cache, S, N, Hq, "spec_tree_attention_bytes", &c) || S == 0 || N == 0) return 0;
-    return tree_attention_bytes(ctx->num_sms, S, N, Hq, c.heads, c.head_dim, c.dtype);
+    return tree_attention_bytes(ctx->num_sms, S, N, Hq, c);
 }
 
 int spec_tree_attention(spec_ctx* ctx, const spec_kv_cache* cache, const void* d_q, long long q_tok, long long q_head, const void* d_k,
@@ -763,7 +763,7 @@ int spec_tree_attention(spec_ctx* ctx, const spec_kv_cache* cache, const void* d
     if ((a.cache.heads > 1 && (k_head <= 0 || v_head <= 0)) || ((long long)S * N > 1 && (k_tok <= 0 || v_tok <= 0)) || k_head >= (1ll << 38) ||
         v_head >= (1ll << 38) || k_tok >= (1ll << 38) || v_tok >= (1ll << 38))
         return fail(ctx, SPEC_ERR_ARG, "%s: strides of k and v must be positive and below 2^38", who);
-    const size_t need = tree_attention_bytes(ctx->num_sms, S, N, Hq, a.cache.heads, a.cache.head_dim, a.cache.dtype);
+    const size_t need = tree_attention_bytes(ctx->num_sms, S, N, Hq, a.cache);
     if (work_bytes < need) return fail(ctx, SPEC_ERR_ARG, "%s: %zu bytes of scratch given, %zu needed", who, work_bytes, need);
     a.q = d_q; a.k = d_k; a.v = d_v;
     a.q_tok = q_tok; a.q_head = q_head;

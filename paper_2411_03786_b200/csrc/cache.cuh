@@ -63,7 +63,7 @@ struct TreeAttnArgs {
     void* work;
     int* status;
 };
-size_t tree_attention_bytes(int num_sms, int S, int N, int Hq, int heads, int head_dim, int dtype);
+size_t tree_attention_bytes(int num_sms, int S, int N, int Hq, const CacheArgs& c);
 int launch_tree_attention(spec_ctx* ctx, const TreeAttnArgs& a, cudaStream_t st);
 
 }  // namespace ngs

@@ -1215,11 +1215,11 @@ int launch_join(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
     return check_cuda(ctx, e, "spec_tree_attention join launch");
 }
 
-size_t tree_attention_bytes(int num_sms, int S, int N, int Hq, int heads, int head_dim, int dtype) {
-    if (dtype == SPEC_E2M1 && few_rows(N, Hq, heads, head_dim)) return few_rows_bytes(num_sms, N, Hq, heads, head_dim);
+size_t tree_attention_bytes(int num_sms, int S, int N, int Hq, const CacheArgs& c) {
+    if (c.dtype == SPEC_E2M1 && few_rows(N, Hq, c.heads, c.head_dim)) return few_rows_bytes(num_sms, S, N, Hq, c);
     AttParams p;
     size_t bytes;
-    plan(num_sms, S, N, Hq, heads, head_dim, p, bytes);
+    plan(num_sms, S, N, Hq, c.heads, c.head_dim, p, bytes);
     return bytes;
 }
 

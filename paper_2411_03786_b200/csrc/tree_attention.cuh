@@ -49,7 +49,7 @@ int launch_join(spec_ctx* ctx, const AttParams& p, cudaStream_t st);
 
 // tree_attention_few.cu: few rows for each key head over a 4-bit cache
 bool few_rows(int N, int Hq, int heads, int head_dim);
-size_t few_rows_bytes(int num_sms, int N, int Hq, int heads, int head_dim);
+size_t few_rows_bytes(int num_sms, int S, int N, int Hq, const CacheArgs& c);
 int launch_few_rows(spec_ctx* ctx, const TreeAttnArgs& a, cudaStream_t st);
 
 }  // namespace ngs

@@ -18,7 +18,7 @@
 //   the block           a warp for each row, on the CUDA cores in fp32: few rows have few nodes, and what a row does not attend to is
 //                       not even read.
 //
-// Work is cut as in tree_attention.cu, with 16 keys as the unit; the warps of a CTA take its units in turn, two at a step, each
+// Work is cut as in tree_attention.cu, with 16 keys as the unit (passes = 0: a CTA for each (s, h) instead, where sequences cannot be long); the warps of a CTA take its units in turn, two at a step, each
 // with references, sums and outputs of its own, which are joined in shared memory at the end of an (s, h).  Copies (cp.async, by the warp
 // that needs them: a warp that fetches for all, with bulk copies of a page's 16 keys, came to 184 us below, 50 cycles for each copy) run
 // STAGES - 1 steps ahead.
@@ -192,9 +192,24 @@ __global__ void __launch_bounds__(F::THREADS, F::CTAS) few_rows_kernel(const __g
     grid_dependency_wait();
     grid_launch_dependents();
 
-    // ---- this CTA's range
+    // ---- this CTA's range, or its (s, h)
     FewWalk w;  // (of thread 0)
-    if (warp == 0) {
+    if (p.passes == 0) {
+        if (threadIdx.x == 0) {
+            FewSegment& seg = segments[0];
+            const int all = cache.heads * p.n_qtiles, hq = (int)(blockIdx.x % all);
+            seg.s = (int)(blockIdx.x / all);
+            seg.h = hq / p.n_qtiles;
+            seg.row0 = (hq - seg.h * p.n_qtiles) * ROWS;
+            seg.t0 = 0;
+            seg.n_units = few_units(a, seg.s, seg.len, seg.live);
+            seg.t1 = seg.n_units + 1;
+            seg.whole = 1;
+            seg.rows = min(ROWS, seg.live * p.G - seg.row0);
+            seg.more = seg.rows > 0;
+            w.pos = w.hi = 0;  // nothing else
+        }
+    } else if (warp == 0) {
         int len, live;
         long long sum = 0;
         const int all = cache.heads * p.n_qtiles;
@@ -697,25 +712,38 @@ __global__ void __launch_bounds__(F::THREADS, F::CTAS) few_rows_kernel(const __g
 // head size 128: 8 rows 50 us against 135, 16 rows 84 against 137, 24 rows 170 against 138; head size 64: 28 rows 99 against 102, 56 rows
 // 191 against 104.
 constexpr int FEW_ROWS = 16;
+// Positions that a sequence's pages can hold at most where a CTA takes the whole of an (s, h), so that nothing is joined: with a CTA for every SM or so
+// twice as many.  One token, 8 key heads with 4 queries each of 128, CTAs for wholes against ranges: 1 sequence of 1024 keys 9.8 us against 10.5, of 2048 14.7
+// against 11.3; 16 sequences of 2048 15.3 against 18.2, of 4096 26.0 against 23.8; 64 of 512 17.5 against 23.8.
+constexpr int FEW_WHOLE = 1024;
 bool few_rows(int N, int Hq, int heads, int head_dim) { return (long long)N * (Hq / heads) <= (head_dim == 64 ? 2 * FEW_ROWS : FEW_ROWS); }
 
-static void few_plan(int num_sms, int N, int Hq, int heads, int head_dim, AttParams& p, size_t& bytes) {
-    p.G = Hq / heads;
+static void few_plan(int num_sms, int S, int N, int Hq, const CacheArgs& c, AttParams& p, size_t& bytes) {
+    p.G = Hq / c.heads;
     const int rows = N * p.G, tile = rows <= 8 ? 8 : 16;
     p.n_qtiles = (rows + tile - 1) / tile;
     p.side = p.passes = 1;
     p.n_groups = num_sms * (rows <= 8 ? 2 : 1);
     p.rows_cap = std::min(tile, rows);
-    const size_t parts = (size_t)p.n_groups * 2 * p.rows_cap, tasks = (size_t)p.n_groups * sizeof(JoinTask);
     p.tasks = nullptr;
+    p.part_o = nullptr;
+    p.part_ml = nullptr;
+    const long long whole = (long long)S * c.heads * p.n_qtiles, room = (long long)c.max_pages << c.page_shift;
+    if (whole <= (1 << 30) && (room <= FEW_WHOLE || (room <= 2 * FEW_WHOLE && 4 * whole >= 3 * num_sms))) {
+        p.passes = 0;
+        p.n_groups = (int)whole;
+        bytes = 16;
+        return;
+    }
+    const size_t parts = (size_t)p.n_groups * 2 * p.rows_cap, tasks = (size_t)p.n_groups * sizeof(JoinTask);
     p.part_o = reinterpret_cast<float*>(tasks);
-    p.part_ml = reinterpret_cast<float2*>(tasks + parts * head_dim * 4);
-    bytes = tasks + parts * (head_dim * 4 + 8);
+    p.part_ml = reinterpret_cast<float2*>(tasks + parts * c.head_dim * 4);
+    bytes = tasks + parts * (c.head_dim * 4 + 8);
 }
-size_t few_rows_bytes(int num_sms, int N, int Hq, int heads, int head_dim) {
+size_t few_rows_bytes(int num_sms, int S, int N, int Hq, const CacheArgs& c) {
     AttParams p;
     size_t bytes;
-    few_plan(num_sms, N, Hq, heads, head_dim, p, bytes);
+    few_plan(num_sms, S, N, Hq, c, p, bytes);
     return bytes;
 }
 
@@ -736,6 +764,7 @@ static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
     const int rc = check_cuda(ctx, e, "spec_tree_attention launch");
     if (rc) return rc;
     ++ctx->launches;
+    if (p.passes == 0) return SPEC_OK;  // nothing is spread
     AttParams j = p;
     j.c = 1.0f;  // (references are in powers of two here)
     return launch_join(ctx, j, st);
@@ -744,7 +773,7 @@ static int launch(spec_ctx* ctx, const AttParams& p, cudaStream_t st) {
 int launch_few_rows(spec_ctx* ctx, const TreeAttnArgs& a, cudaStream_t st) {
     AttParams p;
     size_t bytes;
-    few_plan(ctx->num_sms, a.N, a.Hq, a.cache.heads, a.cache.head_dim, p, bytes);
+    few_plan(ctx->num_sms, a.S, a.N, a.Hq, a.cache, p, bytes);
     p.a = a;
     p.c = a.scale * LOG2E;
     p.tasks = reinterpret_cast<JoinTask*>(a.work);
